@@ -24,6 +24,9 @@
  *     focus_update_sparse_layer   = focus_cache_update + focus_sparse_layer of one layer, in one call
  *     focus_cache_refresh    block entry: new K/V states of every position -> KV cache and K_bar in one pass
  *     focus_block_entry      = focus_cache_refresh + focus_refresh_attn of one layer, in one call
+ * and for a KV cache of eight-bit values:
+ *     focus_quant_update, focus_quant_refresh, focus_quant_read   write and read such a cache
+ *     focus_quant_attn, focus_quant_layer                         focus_sparse_attn and focus_sparse_layer over it
  *
  * Conventions shared by every entry point
  *  - Pointers marked [dev] are device (HBM) addresses, [host] are host addresses.  The caller owns every
@@ -85,7 +88,9 @@ typedef enum focus_fn {
   FOCUS_FN_FIND_SINKS = 2,
   FOCUS_FN_SPARSE_ATTN = 3,
   FOCUS_FN_SPARSE_LAYER = 4,
-  FOCUS_FN_PROBE_LAYER = 5
+  FOCUS_FN_PROBE_LAYER = 5,
+  FOCUS_FN_QUANT_ATTN = 6,
+  FOCUS_FN_QUANT_LAYER = 7
 } focus_fn;
 
 /*
@@ -318,6 +323,54 @@ int focus_cache_refresh(void* K_cache, void* V_cache, const focus_shape* shape, 
 int focus_block_entry(void* K_cache, void* V_cache, const focus_shape* shape, const void* Q, const void* K_new,
                       const void* V_new, int64_t new_stride_h, int64_t new_stride_n, float* kbar, void* out, float* lse,
                       void* stream);
+
+/*
+ * KV cache of eight-bit values: half the memory and half the traffic of a bf16 one.  A row of one head is d codes in the e4m3
+ * format (OCP, no infinities) and one power of two: code c with the row's exponent byte e stands for c * 2^(e - 127).
+ * Writing takes the smallest 2^E with which the largest finite magnitude of the row is at most 448, -110 <= E <= 119, and
+ * rounds to the nearest code, ties to even (magnitudes past 448 * 2^119 to that; infinities and NaN take the NaN code; a row of zeros
+ * has E = -110).  What a row reads back as is exact in bf16: every entry point over such a cache computes what its bf16
+ * counterpart computes over the bf16 cache that focus_quant_read gives, to rounding of the sums.
+ * A cache of zero bytes reads back as zeros.  An exponent byte of 255 is not a number that these calls write or take.
+ *   shape   k_/v_stride_* are the strides of the codes, in bytes, multiples of 16 (rows 16-byte aligned); the others as everywhere
+ */
+typedef struct focus_quant_cache {
+  void* k;        /* [dev] codes uint8 [H, M+N, d] */
+  void* v;
+  uint8_t* k_exp; /* [dev] exponent bytes uint8 [H, M+N] */
+  uint8_t* v_exp;
+  int64_t exp_stride_h, exp_stride_n; /* strides of both, in bytes; exp_stride_n >= 1 */
+} focus_quant_cache;
+
+/* focus_cache_update into a quantised cache (arguments as there).  A position that is listed more than once takes the state of its last
+ * entry. */
+int focus_quant_update(const focus_quant_cache* cache, const focus_shape* shape, const void* K_new, const void* V_new,
+                       int64_t new_stride_h, int64_t new_stride_n, const int32_t* active_idx, const int32_t* counts,
+                       int32_t max_active, int32_t row_base, void* stream);
+
+/* focus_cache_refresh into a quantised cache (arguments as there): all M + N rows, and with kbar the block means of the values
+ * that the rows read back as, bit-identical to focus_block_means of those. */
+int focus_quant_refresh(const focus_quant_cache* cache, const focus_shape* shape, const void* K_new, const void* V_new,
+                        int64_t new_stride_h, int64_t new_stride_n, float* kbar, void* stream);
+
+/* Rows first_row .. first_row + n_rows - 1 of a quantised cache as bf16: K_out, V_out [dev] [H, n_rows, d], strides out_stride_h /
+ * out_stride_n (elements, multiples of 8).  0 <= first_row, first_row + n_rows <= M + N; n_rows = 0 does nothing. */
+int focus_quant_read(const focus_quant_cache* cache, const focus_shape* shape, int32_t first_row, int32_t n_rows, void* K_out,
+                     void* V_out, int64_t out_stride_h, int64_t out_stride_n, void* stream);
+
+/* focus_sparse_attn over a quantised cache; the other arguments, their limits and the results as there.  Workspace:
+ * FOCUS_FN_QUANT_ATTN. */
+int focus_quant_attn(const void* Q, const int32_t* active_idx, const int32_t* counts, int32_t max_active,
+                     const focus_quant_cache* cache, const focus_shape* shape, const int32_t* kept_blocks, int32_t n_keep,
+                     const int32_t* sink_idx, int32_t n_sink, void* out, float* lse, void* workspace, size_t ws_bytes,
+                     void* stream);
+
+/* focus_sparse_layer over a quantised cache: focus_block_scores from kbar (required: such a cache is not scanned for its means) and
+ * focus_quant_attn, with the same results bit for bit.  Workspace: FOCUS_FN_QUANT_LAYER. */
+int focus_quant_layer(const void* Q, const int32_t* focus_idx, const int32_t* active_idx, const int32_t* counts,
+                      int32_t n_focus_max, int32_t max_active, const focus_quant_cache* cache, const float* kbar,
+                      const focus_shape* shape, int32_t n_keep, const int32_t* sink_idx, int32_t n_sink, float* scores,
+                      int32_t* kept_blocks, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
 
 /*
  * Bytes of workspace `fn` needs for this shape; 0 on invalid arguments.  [host] only.  With less a call is refused

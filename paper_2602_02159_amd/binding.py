@@ -16,12 +16,13 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfocus_hip.so")
 
 FOCUS_OK, FOCUS_EINVAL, FOCUS_EUNSUPPORTED, FOCUS_EWORKSPACE, FOCUS_ELAUNCH = 0, -1, -2, -3, -4
-FN_BLOCK_SCORES, FN_FIND_SINKS, FN_SPARSE_ATTN, FN_SPARSE_LAYER, FN_PROBE_LAYER = 1, 2, 3, 4, 5
+FN_BLOCK_SCORES, FN_FIND_SINKS, FN_SPARSE_ATTN, FN_SPARSE_LAYER, FN_PROBE_LAYER, FN_QUANT_ATTN, FN_QUANT_LAYER = 1, 2, 3, 4, 5, 6, 7
 
 EXPORTS = ("focus_select_queries", "focus_expand_groups", "focus_block_means", "focus_block_scores", "focus_find_sinks", "focus_select_and_find_sinks",
            "focus_sparse_attn",
            "focus_sparse_layer", "focus_sparse_layer_static", "focus_block_partials", "focus_top_blocks", "focus_probe_layer", "focus_refresh_attn", "focus_cache_refresh", "focus_block_entry",
            "focus_token_confidence", "focus_token_confidence_workspace", "focus_cache_update", "focus_update_sparse_layer",
+           "focus_quant_update", "focus_quant_refresh", "focus_quant_read", "focus_quant_attn", "focus_quant_layer",
            "focus_workspace_bytes", "focus_helper_k", "focus_helper_n_keep", "focus_helper_n_sink", "focus_last_error",
            "focus_version")
 
@@ -38,6 +39,12 @@ class Shape(C.Structure):
                 ("block", C.c_int32), ("n_gen", C.c_int32),
                 ("q_stride_h", C.c_int64), ("q_stride_n", C.c_int64), ("k_stride_h", C.c_int64), ("k_stride_n", C.c_int64),
                 ("v_stride_h", C.c_int64), ("v_stride_n", C.c_int64), ("o_stride_h", C.c_int64), ("o_stride_n", C.c_int64)]
+
+
+class QuantCache(C.Structure):
+    """Mirror of `focus_quant_cache`."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("exp_stride_h", C.c_int64), ("exp_stride_n", C.c_int64)]
 
 
 _lib = None
@@ -72,7 +79,14 @@ def lib() -> C.CDLL:
         L.focus_update_sparse_layer.argtypes = [p, p, p, p, C.c_int64, C.c_int64, i32, p, p, p, p, i32, i32, p, sp, i32, p, i32, p, p, p, p, p, sz, p]
         L.focus_block_partials.argtypes = [p, p, p, i32, p, p, sp, p, p]
         L.focus_top_blocks.argtypes = [p, i32, p, i32, i32, i32, p, p, p]
-        for name in ("focus_select_queries", "focus_expand_groups", "focus_block_means", "focus_block_scores", "focus_find_sinks",
+        qp = C.POINTER(QuantCache)
+        L.focus_quant_update.argtypes = [qp, sp, p, p, C.c_int64, C.c_int64, p, p, i32, i32, p]
+        L.focus_quant_refresh.argtypes = [qp, sp, p, p, C.c_int64, C.c_int64, p, p]
+        L.focus_quant_read.argtypes = [qp, sp, i32, i32, p, p, C.c_int64, C.c_int64, p]
+        L.focus_quant_attn.argtypes = [p, p, p, i32, qp, sp, p, i32, p, i32, p, p, p, sz, p]
+        L.focus_quant_layer.argtypes = [p, p, p, p, i32, i32, qp, p, sp, i32, p, i32, p, p, p, p, p, sz, p]
+        for name in ("focus_quant_update", "focus_quant_refresh", "focus_quant_read", "focus_quant_attn", "focus_quant_layer",
+                     "focus_select_queries", "focus_expand_groups", "focus_block_means", "focus_block_scores", "focus_find_sinks",
                      "focus_select_and_find_sinks", "focus_sparse_attn", "focus_sparse_layer", "focus_sparse_layer_static", "focus_block_partials", "focus_top_blocks",
                      "focus_probe_layer", "focus_refresh_attn", "focus_token_confidence", "focus_cache_update", "focus_update_sparse_layer", "focus_cache_refresh", "focus_block_entry"):
             getattr(L, name).restype = C.c_int
@@ -317,3 +331,66 @@ def sparse_layer_static(q, focus_idx, active_idx, counts, k, v, kbar, shape: Sha
                                            active_idx.numel(), _ptr(k), _ptr(v), _ptr(kbar), C.byref(shape), n_keep,
                                            _ptr(sink_idx), n_sink, _ptr(scores), _ptr(kept_blocks), _ptr(out), _ptr(lse),
                                            _stream()))
+
+
+def make_quant_cache(k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_exp: torch.Tensor) -> QuantCache:
+    """focus_quant_cache from the codes uint8 [H, M+N, d] (their strides go into the shape: make_shape takes them for k and v) and
+    the exponent bytes uint8 [H, M+N], which share their strides.  The tensors have to outlive the description."""
+    for t, name in ((k, "k"), (v, "v"), (k_exp, "k_exp"), (v_exp, "v_exp")):
+        _need(t, torch.uint8, name)
+    if k.shape != v.shape or k_exp.shape != k.shape[:2] or v_exp.shape != k.shape[:2]:
+        raise ValueError("codes [H, rows, d] and exponents [H, rows] must agree")
+    if k_exp.stride() != v_exp.stride():
+        raise ValueError("k_exp and v_exp must share their strides")
+    return QuantCache(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), k_exp.stride(0), k_exp.stride(1))
+
+
+def quant_update(cache: QuantCache, shape: Shape, k_new, v_new, active_idx, counts, row_base: int) -> None:
+    """cache_update into a quantised cache: k_new, v_new bf16 [H, max_active, d]."""
+    for t, name in ((k_new, "K_new"), (v_new, "V_new")):
+        _need(t, torch.bfloat16, name)
+    if k_new.stride() != v_new.stride() or k_new.stride(2) != 1:
+        raise ValueError("K_new and V_new must share their strides, innermost 1")
+    _check(lib().focus_quant_update(C.byref(cache), C.byref(shape), _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _ptr(active_idx),
+                                    _ptr(counts), active_idx.numel(), row_base, _stream()))
+
+
+def quant_refresh(cache: QuantCache, shape: Shape, k_new, v_new, kbar) -> None:
+    """cache_refresh into a quantised cache; kbar fp32 [H, n_b, d] (or None): block means of the values it reads back as."""
+    for t, name in ((k_new, "K_new"), (v_new, "V_new")):
+        _need(t, torch.bfloat16, name)
+    if kbar is not None:
+        _need(kbar, torch.float32, "kbar")
+    if k_new.stride() != v_new.stride() or k_new.stride(2) != 1:
+        raise ValueError("K_new and V_new must share their strides, innermost 1")
+    _check(lib().focus_quant_refresh(C.byref(cache), C.byref(shape), _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _ptr(kbar), _stream()))
+
+
+def quant_read(cache: QuantCache, shape: Shape, first_row: int, k_out, v_out) -> None:
+    """Rows first_row, ... of a quantised cache into k_out, v_out bf16 [H, rows, d]."""
+    for t, name in ((k_out, "K_out"), (v_out, "V_out")):
+        _need(t, torch.bfloat16, name)
+    if k_out.shape != v_out.shape or k_out.stride() != v_out.stride() or k_out.stride(2) != 1:
+        raise ValueError("K_out and V_out must share their shape and strides, innermost 1")
+    _check(lib().focus_quant_read(C.byref(cache), C.byref(shape), first_row, k_out.shape[1], _ptr(k_out), _ptr(v_out), k_out.stride(0), k_out.stride(1),
+                                  _stream()))
+
+
+def quant_attn(q, active_idx, counts, cache: QuantCache, shape: Shape, kept_blocks, n_keep: int, sink_idx, n_sink: int, out, lse, workspace) -> None:
+    """sparse_attn over a quantised cache."""
+    _need(q, torch.bfloat16, "Q")
+    _need(out, torch.bfloat16, "out")
+    _check(lib().focus_quant_attn(_ptr(q), _ptr(active_idx), _ptr(counts), active_idx.numel(), C.byref(cache), C.byref(shape), _ptr(kept_blocks), n_keep,
+                                  _ptr(sink_idx), n_sink, _ptr(out), _ptr(lse), _ptr(workspace),
+                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+
+
+def quant_layer(q, focus_idx, active_idx, counts, cache: QuantCache, kbar, shape: Shape, n_keep: int, sink_idx, n_sink: int, scores, kept_blocks, out,
+                lse, workspace) -> None:
+    """sparse_layer over a quantised cache, from the block means that the block entry left behind."""
+    _need(q, torch.bfloat16, "Q")
+    _need(out, torch.bfloat16, "out")
+    _need(kbar, torch.float32, "kbar")
+    _check(lib().focus_quant_layer(_ptr(q), _ptr(focus_idx), _ptr(active_idx), _ptr(counts), focus_idx.numel(), active_idx.numel(), C.byref(cache),
+                                   _ptr(kbar), C.byref(shape), n_keep, _ptr(sink_idx), n_sink, _ptr(scores), _ptr(kept_blocks), _ptr(out), _ptr(lse),
+                                   _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))

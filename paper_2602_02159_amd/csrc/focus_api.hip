@@ -96,6 +96,20 @@ SplitPlan plan_attention(const focus_shape& s, int max_active, int n_keep, int n
   return p;
 }
 
+// Over the quantised cache: up to four 16-query tiles share the widened rows.
+constexpr int kQuantGroups = 512;
+SplitPlan plan_quant_attention(const focus_shape& s, int max_active, int n_keep, int n_sink) {
+  SplitPlan p;
+  p.q_tiles = ceil_div(max_active, kQTile);
+  p.q_tiles_per_group = p.q_tiles <= 2 ? p.q_tiles : kMaxQTilesPerGroup;
+  p.q_groups = ceil_div(p.q_tiles, p.q_tiles_per_group);
+  p.q_pad = p.q_groups * p.q_tiles_per_group * kQTile;
+  p.n_sub = n_keep * ceil_div(s.block, kSubTile) + ceil_div(s.n_resp, kSubTile) + ceil_div(n_sink, kSubTile);
+  plan_splits(p, s.n_heads, p.q_groups, kQuantGroups);
+  p.pipelined = p.n_split * kWavesPerGroup < p.n_sub;
+  return p;
+}
+
 SplitPlan plan_attention_dense(const focus_shape& s, int max_active) {
   SplitPlan p;
   plan_queries(p, max_active, max_active <= 64 ? 4 : 2);
@@ -460,6 +474,47 @@ static int sparse_layer_impl(const char* who, const void* Q, const int32_t* focu
   return FOCUS_OK;
 }
 
+static int check_quant(const char* who, const focus_quant_cache* cache, const focus_shape* shape) {
+  if (!cache || !cache->k || !cache->v || !cache->k_exp || !cache->v_exp) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
+  if (!aligned16(cache->k) || !aligned16(cache->v)) return fail(FOCUS_EINVAL, "%s: pointers must be 16-byte aligned", who);
+  if (((shape->k_stride_h | shape->k_stride_n | shape->v_stride_h | shape->v_stride_n) & 15) != 0)
+    return fail(FOCUS_EINVAL, "%s: strides of the codes must be multiples of 16", who);
+  if (cache->exp_stride_h < 0 || cache->exp_stride_n < 1) return fail(FOCUS_EINVAL, "%s: strides of the exponents invalid", who);
+  if (shape->n_heads > 65535) return fail(FOCUS_EUNSUPPORTED, "%s: more than 65535 heads", who);
+  return FOCUS_OK;
+}
+static QuantCache quant_cache(const focus_quant_cache& c) {
+  QuantCache q;
+  q.K = static_cast<uint8_t*>(c.k);
+  q.V = static_cast<uint8_t*>(c.v);
+  q.k_exp = c.k_exp;
+  q.v_exp = c.v_exp;
+  q.esh = c.exp_stride_h;
+  q.esn = c.exp_stride_n;
+  return q;
+}
+
+static LayerWs ws_quant_layer(const focus_shape& s, const SplitPlan& p) {  // the two parts always have places of their own
+  LayerWs w;
+  w.sc = ws_block_scores(s);
+  w.at = ws_attn(s, p);
+  w.attn = w.sc.total;
+  w.need = w.total = w.attn + w.at.total;
+  return w;
+}
+
+static int check_attention(const char* who, const focus_shape* shape, const void* Q, const int32_t* active_idx, int32_t max_active, int32_t n_keep,
+                           const int32_t* kept_blocks, int32_t n_sink, const int32_t* sink_idx, const void* out) {
+  if (!Q || !active_idx || !out) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
+  const int n_b = ceil_div(shape->n_ctx, shape->block);
+  if (max_active < 1 || max_active > shape->n_gen) return fail(FOCUS_EINVAL, "%s: max_active=%d not in [1, n_gen]", who, max_active);
+  if (n_keep < 0 || n_keep > n_b) return fail(FOCUS_EINVAL, "%s: n_keep=%d not in [0, n_b=%d]", who, n_keep, n_b);
+  if (n_sink < 0 || n_sink > shape->n_ctx) return fail(FOCUS_EINVAL, "%s: n_sink=%d not in [0, n_ctx]", who, n_sink);
+  if ((n_keep > 0 && !kept_blocks) || (n_sink > 0 && !sink_idx)) return fail(FOCUS_EINVAL, "%s: index array is NULL", who);
+  if (!aligned16(Q) || !aligned16(out)) return fail(FOCUS_EINVAL, "%s: pointers must be 16-byte aligned", who);
+  return FOCUS_OK;
+}
+
 }  // namespace focus
 
 using namespace focus;
@@ -495,6 +550,12 @@ size_t focus_workspace_bytes(int32_t fn, const focus_shape* shape, int32_t max_a
           n_sink > shape->n_ctx)
         return 0;
       return ws_layer(*shape, plan_attention(*shape, max_active, n_keep, n_sink)).total;
+    case FOCUS_FN_QUANT_ATTN:
+    case FOCUS_FN_QUANT_LAYER: {
+      if (max_active < 1 || max_active > shape->n_gen || n_keep < 0 || n_keep > n_b || n_sink < 0 || n_sink > shape->n_ctx) return 0;
+      const SplitPlan p = plan_quant_attention(*shape, max_active, n_keep, n_sink);
+      return fn == FOCUS_FN_QUANT_ATTN ? ws_attn(*shape, p).total : ws_quant_layer(*shape, p).total;
+    }
     default:
       fail(FOCUS_EINVAL, "focus_workspace_bytes: unknown function id %d", fn);
       return 0;
@@ -798,6 +859,116 @@ int focus_sparse_layer_static(const void* Q, const int32_t* focus_idx, const int
                               float* scores, int32_t* kept_blocks, void* out, float* lse, void* stream) {
   return sparse_layer_impl("focus_sparse_layer_static", Q, focus_idx, active_idx, counts, n_focus_max, max_active, K, V, kbar,
                            shape, n_keep, sink_idx, n_sink, scores, kept_blocks, out, lse, nullptr, 0, true, stream);
+}
+
+int focus_quant_update(const focus_quant_cache* cache, const focus_shape* shape, const void* K_new, const void* V_new, int64_t new_stride_h,
+                       int64_t new_stride_n, const int32_t* active_idx, const int32_t* counts, int32_t max_active, int32_t row_base,
+                       void* stream) {
+  const char* who = "focus_quant_update";
+  if (int rc = check_shape(shape, false, true, true, false)) return rc;
+  if (int rc = check_quant(who, cache, shape)) return rc;
+  if (int rc = check_cache_update(who, cache->k, cache->v, shape, K_new, V_new, new_stride_h, new_stride_n, active_idx, max_active)) return rc;
+  const CacheUpdate u = cache_update_args(nullptr, nullptr, *shape, K_new, V_new, new_stride_h, new_stride_n, active_idx, counts, max_active, row_base);
+  hipError_t e = launch_quant_update(u, quant_cache(*cache), shape->head_dim, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return launch_fail(who, e);
+  return FOCUS_OK;
+}
+
+int focus_quant_refresh(const focus_quant_cache* cache, const focus_shape* shape, const void* K_new, const void* V_new, int64_t new_stride_h,
+                        int64_t new_stride_n, float* kbar, void* stream) {
+  const char* who = "focus_quant_refresh";
+  if (int rc = check_shape(shape, false, true, true, false)) return rc;
+  if (int rc = check_quant(who, cache, shape)) return rc;
+  if (int rc = check_cache_refresh(who, cache->k, cache->v, shape, K_new, V_new, new_stride_h, new_stride_n, kbar)) return rc;
+  const CacheRefresh p = cache_refresh_args(nullptr, nullptr, *shape, K_new, V_new, new_stride_h, new_stride_n, kbar);
+  hipError_t e = launch_quant_refresh(p, quant_cache(*cache), shape->head_dim, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return launch_fail(who, e);
+  return FOCUS_OK;
+}
+
+int focus_quant_read(const focus_quant_cache* cache, const focus_shape* shape, int32_t first_row, int32_t n_rows, void* K_out, void* V_out,
+                     int64_t out_stride_h, int64_t out_stride_n, void* stream) {
+  const char* who = "focus_quant_read";
+  if (int rc = check_shape(shape, false, true, true, false)) return rc;
+  if (int rc = check_quant(who, cache, shape)) return rc;
+  if (first_row < 0 || n_rows < 0 || (int64_t)first_row + n_rows > (int64_t)shape->n_ctx + shape->n_resp)
+    return fail(FOCUS_EINVAL, "%s: rows [%d, %d + %d) not inside the cache", who, first_row, first_row, n_rows);
+  if (out_stride_n < shape->head_dim || (out_stride_n & 7) || out_stride_h < 0 || (out_stride_h & 7))
+    return fail(FOCUS_EINVAL, "%s: output strides invalid or not multiples of 8", who);
+  if (n_rows == 0) return FOCUS_OK;
+  if (!K_out || !V_out) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
+  if (!aligned16(K_out) || !aligned16(V_out)) return fail(FOCUS_EINVAL, "%s: pointers must be 16-byte aligned", who);
+  QuantRead r;
+  r.ksh = shape->k_stride_h; r.ksn = shape->k_stride_n;
+  r.vsh = shape->v_stride_h; r.vsn = shape->v_stride_n;
+  r.osh = out_stride_h; r.osn = out_stride_n;
+  r.K_out = static_cast<uint16_t*>(K_out);
+  r.V_out = static_cast<uint16_t*>(V_out);
+  r.row0 = first_row;
+  r.n_rows = n_rows;
+  hipError_t e = launch_quant_read(r, quant_cache(*cache), shape->n_heads, shape->head_dim, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return launch_fail(who, e);
+  return FOCUS_OK;
+}
+
+int focus_quant_attn(const void* Q, const int32_t* active_idx, const int32_t* counts, int32_t max_active, const focus_quant_cache* cache,
+                     const focus_shape* shape, const int32_t* kept_blocks, int32_t n_keep, const int32_t* sink_idx, int32_t n_sink, void* out,
+                     float* lse, void* workspace, size_t ws_bytes, void* stream) {
+  const char* who = "focus_quant_attn";
+  if (int rc = check_shape(shape, true, true, true, true)) return rc;
+  if (int rc = check_quant(who, cache, shape)) return rc;
+  if (int rc = check_attention(who, shape, Q, active_idx, max_active, n_keep, kept_blocks, n_sink, sink_idx, out)) return rc;
+  const SplitPlan p = plan_quant_attention(*shape, max_active, n_keep, n_sink);
+  const AttnWs w = ws_attn(*shape, p);
+  if (p.n_split > 1 && (!workspace || ws_bytes < w.total || !aligned16(workspace)))
+    return fail(FOCUS_EWORKSPACE, "%s: workspace needs %zu bytes, 16-byte aligned", who, w.total);
+  char* ws = static_cast<char*>(workspace);
+  hipError_t e = launch_quant_attn(Q, active_idx, counts, max_active, quant_cache(*cache), *shape, kept_blocks, n_keep, sink_idx, n_sink, p, out, lse,
+                                   ws ? reinterpret_cast<float*>(ws + w.part_o) : nullptr, ws ? reinterpret_cast<float*>(ws + w.part_ml) : nullptr,
+                                   nullptr, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return launch_fail(who, e);
+  return FOCUS_OK;
+}
+
+int focus_quant_layer(const void* Q, const int32_t* focus_idx, const int32_t* active_idx, const int32_t* counts, int32_t n_focus_max,
+                      int32_t max_active, const focus_quant_cache* cache, const float* kbar, const focus_shape* shape, int32_t n_keep,
+                      const int32_t* sink_idx, int32_t n_sink, float* scores, int32_t* kept_blocks, void* out, float* lse, void* workspace,
+                      size_t ws_bytes, void* stream) {
+  const char* who = "focus_quant_layer";
+  if (int rc = check_shape(shape, true, true, true, true)) return rc;
+  if (int rc = check_quant(who, cache, shape)) return rc;
+  if (!focus_idx || !kbar) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
+  if (n_focus_max < 1 || n_focus_max > shape->n_gen) return fail(FOCUS_EINVAL, "%s: n_focus_max=%d not in [1, n_gen]", who, n_focus_max);
+  if (int rc = check_attention(who, shape, Q, active_idx, max_active, n_keep, kept_blocks, n_sink, sink_idx, out)) return rc;
+  if (!aligned16(kbar)) return fail(FOCUS_EINVAL, "%s: pointers must be 16-byte aligned", who);
+  const SplitPlan p = plan_quant_attention(*shape, max_active, n_keep, n_sink);
+  const LayerWs w = ws_quant_layer(*shape, p);
+  if (!workspace || ws_bytes < w.need || !aligned16(workspace))
+    return fail(FOCUS_EWORKSPACE, "%s: workspace needs %zu bytes, 16-byte aligned", who, w.need);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  const int n_b = ceil_div(shape->n_ctx, shape->block);
+  float* part = reinterpret_cast<float*>(ws + w.sc.part);
+  float* R = scores ? scores : reinterpret_cast<float*>(ws + w.sc.scores);
+  float* part_o = reinterpret_cast<float*>(ws + w.attn + w.at.part_o);
+  float* part_ml = reinterpret_cast<float*>(ws + w.attn + w.at.part_ml);
+  hipError_t e = launch_block_relevance(Q, focus_idx, counts, n_focus_max, kbar, *shape, part, false, st);
+  if (e != hipSuccess) return launch_fail("focus_quant_layer(relevance)", e);
+  FusedTopC f;
+  f.rel_part = part;
+  f.per_head = false;
+  f.scores_out = R;
+  f.kept_out = kept_blocks;
+  f.n_focus_max = n_focus_max;
+  const bool fused = n_b <= kFusedMaxBlocks && n_keep > 0;
+  if (!fused) {
+    e = launch_reduce_topk(part, ceil_div(shape->n_heads, kRelGroup), shape->n_heads, counts, n_focus_max, R, n_b, n_keep, kept_blocks, st);
+    if (e != hipSuccess) return launch_fail("focus_quant_layer(top-C)", e);
+  }
+  e = launch_quant_attn(Q, active_idx, counts, max_active, quant_cache(*cache), *shape, fused ? nullptr : kept_blocks, n_keep, sink_idx, n_sink, p, out,
+                        lse, part_o, part_ml, fused ? &f : nullptr, st);
+  if (e != hipSuccess) return launch_fail("focus_quant_layer(attention)", e);
+  return FOCUS_OK;
 }
 
 }  // extern "C"

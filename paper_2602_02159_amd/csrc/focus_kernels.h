@@ -142,6 +142,30 @@ CacheRefresh cache_refresh_args(void* K_cache, void* V_cache, const focus_shape&
                                 int64_t new_stride_h, int64_t new_stride_n, float* kbar);
 hipError_t launch_cache_refresh(const CacheRefresh& p, int head_dim, hipStream_t st);
 
+// ---- quantised cache (focus_quant.hip).  The row strides of the codes, in bytes, are those of the shape.
+struct QuantCache {
+  uint8_t* K;      // codes [H, M + N, d]
+  uint8_t* V;
+  uint8_t* k_exp;  // exponents [H, M + N]
+  uint8_t* v_exp;
+  int64_t esh, esn;
+};
+struct QuantRead {
+  int64_t ksh, ksn, vsh, vsn, osh, osn;
+  uint16_t* K_out;
+  uint16_t* V_out;
+  int row0, n_rows;
+};
+// (the cache pointers of the bf16 forms' arguments are not used; their strides are those of the codes)
+hipError_t launch_quant_update(const CacheUpdate& u, const QuantCache& q, int head_dim, hipStream_t st);
+hipError_t launch_quant_refresh(const CacheRefresh& p, const QuantCache& q, int head_dim, hipStream_t st);
+hipError_t launch_quant_read(const QuantRead& p, const QuantCache& q, int n_heads, int head_dim, hipStream_t st);
+SplitPlan plan_quant_attention(const focus_shape& s, int max_active, int n_keep, int n_sink);
+struct FusedTopC;
+hipError_t launch_quant_attn(const void* Q, const int32_t* active_idx, const int32_t* counts, int max_active, const QuantCache& q, const focus_shape& s,
+                             const int32_t* kept_blocks, int n_keep, const int32_t* sink_idx, int n_sink, const SplitPlan& p, void* out, float* lse,
+                             float* part_o, float* part_ml, const FusedTopC* fused, hipStream_t st);
+
 // ---- MFMA kernels (focus_mfma.hip)
 // mode 0: logits [H, ceil(L / 4), 16, 4] + part_ml out (at most 16 queries); mode 1: part_ml out only; mode 2: lse2 in, or part_ml of
 // mode 1 (not null; lse_in_logits), colpart [q_groups * H, L] out
