@@ -20,6 +20,7 @@
  *     focus_refresh_attn     dense attention of every position (block entry)
  * and, around the step (Sec. 3):
  *     focus_token_confidence vocabulary logits -> predicted tokens, confidences (Eq. 2): the input of the selection
+ *     focus_sample_tokens    the same from logits with temperature, top-k, top-p, min-p and random numbers
  *     focus_cache_update     new K/V states of the active positions -> KV cache (Eq. 3)
  *     focus_update_sparse_layer   = focus_cache_update + focus_sparse_layer of one layer, in one call
  *     focus_cache_refresh    block entry: new K/V states of every position -> KV cache and K_bar in one pass
@@ -282,6 +283,38 @@ int focus_token_confidence(const void* logits, int64_t row_stride, const uint8_t
                            void* stream);
 /* Bytes of workspace focus_token_confidence needs; 0 on invalid arguments.  [host] only. */
 size_t focus_token_confidence_workspace(int32_t n_rows, int32_t vocab);
+
+/* Type of the logits of focus_sample_tokens. */
+typedef enum focus_dtype { FOCUS_BF16 = 0, FOCUS_F32 = 1 } focus_dtype;
+
+/*
+ * Tokens drawn from vocabulary logits.  The tokens of a row are ordered by (logit descending, id ascending), a token's weight is
+ * w = exp((logit - max) / temperature), and of the order is kept
+ *   top_k   the first top_k tokens (<= 0: all),
+ *   top_p   of those the shortest prefix whose weight is at least top_p of theirs (>= 1: all; <= 0: the first),
+ *   min_p   of those the tokens with w >= min_p (<= 0: all);
+ * the first one always.  The token drawn is the first one, in the order of the ids, at which the cumulative weight of the kept
+ * tokens exceeds uniform[i] times their sum.  temperature <= 0 or NaN: the first of the order (focus_token_confidence's token); a NaN
+ * elsewhere switches that filter off.  Weights are held to 2^-42 of the largest: a token below half of that is not drawn.
+ *   logits   [dev] bf16 or fp32 (`dtype`) [n_rows, vocab], row i at logits + i * row_stride (elements), rows 16-byte aligned; NaN counts
+ *            as -inf (never drawn), +inf as the largest number
+ *   masked   [dev] uint8[n_rows] or NULL (= all): rows with masked[i] == 0 get tokens[i] = -1, conf[i] = prob[i] = 0; so do rows
+ *            without a logit above -inf
+ *   uniform  [dev] fp32[n_rows] in [0, 1)
+ *   temperature, top_k, top_p, min_p   [dev] one value per row each (fp32, int32, fp32, fp32), or NULL: 1, all, 1, 0
+ *   tokens   [dev] int32[n_rows] out
+ *   conf     [dev] fp32[n_rows] out or NULL: softmax probability of the token over the whole row at temperature 1 (Eq. 2), the
+ *            confidence that focus_select_queries ranks
+ *   prob     [dev] fp32[n_rows] out or NULL: probability with which it was drawn, among the kept tokens
+ *   workspace  [dev] focus_sample_tokens_workspace(n_rows, vocab) bytes, 16-byte aligned; nothing is assumed about its contents
+ * Results are the same from call to call.  1 <= n_rows <= 65535, 1 <= vocab <= 2097152.
+ */
+int focus_sample_tokens(const void* logits, int32_t dtype, int64_t row_stride, const uint8_t* masked, const float* uniform,
+                        const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t n_rows,
+                        int32_t vocab, int32_t* tokens, float* conf, float* prob, void* workspace, size_t ws_bytes,
+                        void* stream);
+/* Bytes of workspace focus_sample_tokens needs; 0 on invalid arguments.  [host] only. */
+size_t focus_sample_tokens_workspace(int32_t n_rows, int32_t vocab);
 
 /*
  * Approximate KV cache update (Sec. 3, Eq. 3; the cache-update step that ends each layer of Alg. 1): the cache rows of

@@ -23,6 +23,7 @@ EXPORTS = ("focus_select_queries", "focus_expand_groups", "focus_block_means", "
            "focus_sparse_layer", "focus_sparse_layer_static", "focus_block_partials", "focus_top_blocks", "focus_probe_layer", "focus_refresh_attn", "focus_cache_refresh", "focus_block_entry",
            "focus_token_confidence", "focus_token_confidence_workspace", "focus_cache_update", "focus_update_sparse_layer",
            "focus_quant_update", "focus_quant_refresh", "focus_quant_read", "focus_quant_attn", "focus_quant_layer",
+           "focus_sample_tokens", "focus_sample_tokens_workspace",
            "focus_workspace_bytes", "focus_helper_k", "focus_helper_n_keep", "focus_helper_n_sink", "focus_last_error",
            "focus_version")
 
@@ -85,7 +86,10 @@ def lib() -> C.CDLL:
         L.focus_quant_read.argtypes = [qp, sp, i32, i32, p, p, C.c_int64, C.c_int64, p]
         L.focus_quant_attn.argtypes = [p, p, p, i32, qp, sp, p, i32, p, i32, p, p, p, sz, p]
         L.focus_quant_layer.argtypes = [p, p, p, p, i32, i32, qp, p, sp, i32, p, i32, p, p, p, p, p, sz, p]
-        for name in ("focus_quant_update", "focus_quant_refresh", "focus_quant_read", "focus_quant_attn", "focus_quant_layer",
+        L.focus_sample_tokens.argtypes = [p, i32, C.c_int64, p, p, p, p, p, p, i32, i32, p, p, p, p, sz, p]
+        L.focus_sample_tokens_workspace.argtypes = [i32, i32]
+        L.focus_sample_tokens_workspace.restype = sz
+        for name in ("focus_sample_tokens", "focus_quant_update", "focus_quant_refresh", "focus_quant_read", "focus_quant_attn", "focus_quant_layer",
                      "focus_select_queries", "focus_expand_groups", "focus_block_means", "focus_block_scores", "focus_find_sinks",
                      "focus_select_and_find_sinks", "focus_sparse_attn", "focus_sparse_layer", "focus_sparse_layer_static", "focus_block_partials", "focus_top_blocks",
                      "focus_probe_layer", "focus_refresh_attn", "focus_token_confidence", "focus_cache_update", "focus_update_sparse_layer", "focus_cache_refresh", "focus_block_entry"):
@@ -261,6 +265,27 @@ def token_confidence(logits, masked, tokens, conf, workspace) -> None:
     _check(lib().focus_token_confidence(_ptr(logits), logits.stride(0), _ptr(masked), logits.shape[0], logits.shape[1],
                                         _ptr(tokens), _ptr(conf), _ptr(workspace),
                                         0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+
+
+def sample_tokens_workspace(n_rows: int, vocab: int) -> int:
+    return int(lib().focus_sample_tokens_workspace(n_rows, vocab))
+
+
+def sample_tokens(logits, masked, uniform, temperature, top_k, top_p, min_p, tokens, conf, prob, workspace) -> None:
+    """logits bf16 or fp32 [n_rows, vocab] (rows 16-byte aligned); uniform, temperature, top_p, min_p fp32 and top_k int32 [n_rows] (all
+    but uniform may be None, as may masked, conf and prob); workspace of sample_tokens_workspace() bytes."""
+    if not logits.is_cuda or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"logits: expected a CUDA tensor of bfloat16 or float32, got {logits.dtype} on {logits.device}")
+    if logits.stride(1) != 1:
+        raise ValueError("logits: innermost stride must be 1")
+    for t, dtype, name in ((uniform, torch.float32, "uniform"), (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+                           (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"), (tokens, torch.int32, "tokens"), (conf, torch.float32, "conf"),
+                           (prob, torch.float32, "prob")):
+        if t is not None:
+            _need(t, dtype, name)
+    _check(lib().focus_sample_tokens(_ptr(logits), int(logits.dtype == torch.float32), logits.stride(0), _ptr(masked), _ptr(uniform), _ptr(temperature),
+                                     _ptr(top_k), _ptr(top_p), _ptr(min_p), logits.shape[0], logits.shape[1], _ptr(tokens), _ptr(conf), _ptr(prob),
+                                     _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
 
 
 def cache_update(k_cache, v_cache, shape: Shape, k_new, v_new, active_idx, counts, row_base: int) -> None:

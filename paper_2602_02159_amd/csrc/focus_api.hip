@@ -748,6 +748,29 @@ int focus_token_confidence(const void* logits, int64_t row_stride, const uint8_t
   return FOCUS_OK;
 }
 
+size_t focus_sample_tokens_workspace(int32_t n_rows, int32_t vocab) {
+  if (n_rows < 1 || n_rows > 65535 || vocab < 1 || vocab > kSampleMaxVocab) return 0;
+  return sample_tokens_workspace(n_rows, vocab);
+}
+
+int focus_sample_tokens(const void* logits, int32_t dtype, int64_t row_stride, const uint8_t* masked, const float* uniform, const float* temperature,
+                        const int32_t* top_k, const float* top_p, const float* min_p, int32_t n_rows, int32_t vocab, int32_t* tokens, float* conf,
+                        float* prob, void* workspace, size_t ws_bytes, void* stream) {
+  const char* who = "focus_sample_tokens";
+  if (!logits || !uniform || !tokens) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
+  if (dtype != FOCUS_BF16 && dtype != FOCUS_F32) return fail(FOCUS_EUNSUPPORTED, "%s: dtype=%d", who, dtype);
+  if (n_rows < 1 || n_rows > 65535) return fail(FOCUS_EINVAL, "%s: n_rows=%d not in [1, 65535]", who, n_rows);
+  if (vocab < 1 || vocab > kSampleMaxVocab) return fail(FOCUS_EINVAL, "%s: vocab=%d not in [1, %d]", who, vocab, kSampleMaxVocab);
+  if (row_stride < vocab || (row_stride & (dtype == FOCUS_F32 ? 3 : 7)) || !aligned16(logits))
+    return fail(FOCUS_EINVAL, "%s: rows must be 16-byte aligned, row_stride >= vocab", who);
+  const size_t need = sample_tokens_workspace(n_rows, vocab);
+  if (!workspace || ws_bytes < need || !aligned16(workspace)) return fail(FOCUS_EWORKSPACE, "%s: workspace needs %zu bytes, 16-byte aligned", who, need);
+  hipError_t e = launch_sample_tokens(logits, dtype, row_stride, masked, uniform, temperature, top_k, top_p, min_p, n_rows, vocab, tokens, conf, prob,
+                                      workspace, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return launch_fail(who, e);
+  return FOCUS_OK;
+}
+
 int focus_cache_update(void* K_cache, void* V_cache, const focus_shape* shape, const void* K_new, const void* V_new,
                        int64_t new_stride_h, int64_t new_stride_n, const int32_t* active_idx, const int32_t* counts,
                        int32_t max_active, int32_t row_base, void* stream) {

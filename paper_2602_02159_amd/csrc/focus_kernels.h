@@ -126,6 +126,12 @@ hipError_t launch_sink_final(const int32_t* cand, const uint32_t* cand_keys, int
 size_t token_confidence_workspace(int n_rows, int vocab);
 hipError_t launch_token_confidence(const void* logits, int64_t row_stride, const uint8_t* masked, int n_rows, int vocab,
                                    int32_t* tokens, float* conf, void* workspace, hipStream_t st);
+// Sampling (focus_sample.hip): masses are whole numbers of 42 bits below the point, a row's sum has 64
+constexpr int kSampleMaxVocab = 1 << 21;
+size_t sample_tokens_workspace(int n_rows, int vocab);
+hipError_t launch_sample_tokens(const void* logits, int dtype, int64_t row_stride, const uint8_t* masked, const float* uniform, const float* temperature,
+                                const int32_t* top_k, const float* top_p, const float* min_p, int n_rows, int vocab, int32_t* tokens, float* conf,
+                                float* prob, void* workspace, hipStream_t st);
 hipError_t launch_cache_update(const CacheUpdate& u, int head_dim, hipStream_t st);
 // block entry: every cache row takes its new state; block means of the prompt keys from the same pass (kbar may be null)
 struct CacheRefresh {
