@@ -134,6 +134,7 @@ __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int row) {
   p.min_p = a.min_p ? a.min_p[row] : 0.f;
   p.top_k = a.top_k ? a.top_k[row] : 0;
   p.u = fmaxf(a.uniform[row], 0.f);  // NaN: 0
+  if (p.top_k == 1 || p.top_p <= 0.f || p.min_p > 1.f) p.temperature = 0.f;  // only the first stays
   return p;
 }
 __device__ __forceinline__ void write_row(const SampleArgs& a, int row, int token, float conf, float prob) {
@@ -152,19 +153,12 @@ __device__ __forceinline__ uint32_t min_p_key(float min_p, float temperature, fl
 }
 
 // The whole row by one workgroup that walks it as often as it takes: the order is searched bit by bit.  What is kept is
-// {key > cut} and of {key == cut} the ids up to `last_id`.
+// {key > cut} and of {key == cut} the ids up to `last_id`.  For the rows that the lists below do not hold (hundreds of microseconds).
 constexpr int kRowThreads = 1024;
 template <class T>
-__global__ __launch_bounds__(kRowThreads) void sample_row_kernel(const SampleArgs a) {
+__device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t* sh2, uint64_t* wave_mass, int* found) {
   constexpr int E = Chunk<T>::E;
-  __shared__ uint64_t sh[kRowThreads / 64], sh2[kRowThreads / 64];
-  __shared__ uint64_t wave_mass[kRowThreads / 64];
-  __shared__ int found_sh;
-  const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (a.masked != nullptr && a.masked[row] == 0) {
-    if (tid == 0) write_row(a, row, -1, 0.f, 0.f);
-    return;
-  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const T* z = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
   const int n_chunks = (a.vocab + E - 1) / E;
   const RowParams p = row_params(a, row);
@@ -262,9 +256,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(const SampleArg
   const uint32_t m_key = min(min_p_key(p.min_p, p.temperature, top), top_key);
   if (m_key > cut) {
     cut = m_key;
-    ties = p.min_p > 1.f ? 1 : ~(uint64_t)0;
-  } else if (m_key == cut && p.min_p > 1.f) {
-    ties = 1;
+    ties = ~(uint64_t)0;
   }
   int last_id = a.vocab;
   if (ties != ~(uint64_t)0) {  // the largest id up to which at most `ties` tokens have the key
@@ -287,7 +279,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(const SampleArg
   each([&](int id, float v) { total += held(id, v); });
   total = block_reduce64<kRowThreads>(total, sh, Add64());
   const double want = (double)p.u * (double)total;
-  if (tid == 0) found_sh = -1;
+  if (tid == 0) (*found) = -1;
   uint64_t base = 0;
   for (int c0 = 0; c0 < n_chunks; c0 += kRowThreads) {
     uint64_t m[E], mine = 0;
@@ -318,14 +310,14 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(const SampleArg
     for (int e = 0; e < E; ++e) {  // (the last token with a mass takes what rounding leaves)
       const uint64_t after = before + m[e];
       if (m[e] > 0 && (double)before <= want && (!((double)after <= want) || after == total)) {
-        atomicMax(&found_sh, ch * E + e);
+        atomicMax(found, ch * E + e);
       }
       before = after;
     }
     base += round;
   }
   __syncthreads();
-  const int token = found_sh;
+  const int token = (*found);
   if (tid == 0) {
     const float v = token < 0 ? top : clean(sizeof(T) == 4 ? reinterpret_cast<const float*>(z)[token] : bf16_lo(reinterpret_cast<const uint16_t*>(z)[token]));
     const double w1 = weight(v, top, s1), w = weight(v, top, s);
@@ -333,17 +325,576 @@ __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(const SampleArg
   }
 }
 
-size_t sample_tokens_workspace(int, int) { return 256; }
+// =====================================================================================================
+// The ordinary way: three launches, the first two with a workgroup per slice of a row.
+//   sample_scan_kernel   the slice's largest logit and masses, and a histogram of the order: kBins bins of 1/16 in logit / T from the
+//                        largest down, counts and masses.  Bins are counted from zero logit up (floor(z * bins per unit)), so that those of
+//                        all slices are the same; a bin more than kBins below the largest has no mass.
+//   sample_cut_kernel    from the row's histogram the bins in which top_k and top_p end.  Tokens above them are kept whatever comes:
+//                        their masses are summed per segment of 64 chunks.  Tokens in them are listed.
+//   sample_pick_kernel   a workgroup per row orders the list, finds the end of what is kept in it, adds the kept ones to their segments, and
+//                        walks down: segment, chunk, token.
+// The row is read twice, the second time from a cache.  Where a bin holds more tokens than the lists do, or the bins do not resolve the
+// logits (2^18 and more, at T = 1), the last launch searches the row instead.
+// =====================================================================================================
+constexpr int kBins = 512;
+constexpr int kScanThreads = 256, kSliceLogits = 64 * kScanThreads;
+constexpr int kSliceList = 2048, kRowList = 4096;  // entries of a slice, of a row
+constexpr int kSegChunks = 64;
+constexpr int kMaxSlices = kSampleMaxVocab / kSliceLogits;
+constexpr float kMostBin = 4194304.f;  // beyond, floats would not hold bin numbers and their neighbours
+
+struct SliceStat {
+  float top;   // -inf: no number
+  int id;      // the first with it
+  double at1;  // mass at T = 1 and at T, relative to `top`
+  double atT;
+};
+struct SampleWs {
+  SliceStat* stat;   // [rows, slices]
+  uint64_t* mass;    // [rows, slices, kBins]
+  uint32_t* count;   // [rows, slices, kBins]
+  uint32_t* listed;  // [rows, slices]
+  uint64_t* list;    // [rows, slices, kSliceList]  order_of() each
+  struct RowCut* cut;  // [rows]
+  uint64_t* seg;     // [rows, segments]
+  int slices, segs;
+};
+__device__ __forceinline__ uint64_t order_of(uint32_t key, int id) { return ((uint64_t)~key << 32) | (uint32_t)id; }  // ascending: first to last
+__device__ __forceinline__ uint32_t key_in(uint64_t order) { return ~(uint32_t)(order >> 32); }
+__device__ __forceinline__ float bins_per_unit(float temperature) { return fminf(16.f / temperature, 8192.f); }
+constexpr double kMassUnit = 1.0 / (double)((uint64_t)1 << kMassBits);
+__device__ __forceinline__ bool needs_order(const RowParams& p) { return p.top_k > 0 || p.top_p < 1.f; }
+
+template <class T>
+__global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleArgs a, const SampleWs ws, int row0) {
+  constexpr int E = Chunk<T>::E, N = kSliceLogits / E / kScanThreads, kCopies = 4;
+  __shared__ unsigned long long mass_sh[kCopies][kBins];
+  __shared__ uint32_t count_sh[kCopies][kBins];
+  __shared__ uint64_t sh[kScanThreads / 64], sh2[kScanThreads / 64];
+  __shared__ float top_sh[kScanThreads / 64];
+  __shared__ int id_sh;
+  const int slice = blockIdx.x, r = blockIdx.y, row = row0 + r, tid = threadIdx.x;
+  if (a.masked != nullptr && a.masked[row] == 0) return;
+  const T* z = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
+  const int c0 = slice * (kSliceLogits / E) + tid, n_chunks = (a.vocab + E - 1) / E;
+  Chunk<T> x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) load_chunk(x[i], z, min(c0 + i * kScanThreads, n_chunks), a.vocab);
+  const RowParams p = row_params(a, row);
+  for (int i = tid; i < kCopies * kBins; i += kScanThreads) {
+    (&mass_sh[0][0])[i] = 0;
+    (&count_sh[0][0])[i] = 0;
+  }
+  if (tid == 0) id_sh = 0x7fffffff;
+  float mine = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < E; ++e) mine = fmaxf(mine, x[i].z[e]);
+  float top = mine;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+  if ((tid & 63) == 0) top_sh[tid >> 6] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kScanThreads / 64; ++w) top = fmaxf(top, top_sh[w]);
+  SliceStat* stat = ws.stat + (int64_t)r * ws.slices + slice;
+  if (top == -INFINITY) {
+    if (tid == 0) *stat = SliceStat{top, 0, 0.0, 0.0};
+    return;
+  }
+  if (mine == top) {
+    int id = 0x7fffffff;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (x[i].z[e] == top) id = min(id, (c0 + i * kScanThreads) * E + e);
+    atomicMin(&id_sh, id);
+  }
+  const bool drawn = p.temperature > 0.f, order = drawn && needs_order(p);
+  const Scale s1 = scale_of(1.f), s = scale_of(drawn ? p.temperature : 1.f);
+  const float per_unit = bins_per_unit(drawn ? p.temperature : 1.f), first = floorf(top * per_unit);
+  uint64_t at1 = 0, atT = 0;
+  if (a.conf != nullptr) {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) at1 += mass(x[i].z[e], top, s1);
+  }
+  if (order) {  // uniform over the workgroup
+    const int copy = tid & (kCopies - 1);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float b = first - floorf(x[i].z[e] * per_unit);
+        if (b < (float)kBins) {
+          const uint64_t m = mass(x[i].z[e], top, s);
+          atT += m;
+          atomicAdd(&mass_sh[copy][(int)b], (unsigned long long)m);
+          atomicAdd(&count_sh[copy][(int)b], 1u);
+        }
+      }
+  }
+  at1 = block_reduce64<kScanThreads>(at1, sh, Add64());
+  atT = block_reduce64<kScanThreads>(atT, sh2, Add64());
+  if (tid == 0) *stat = SliceStat{top, id_sh, (double)at1 * kMassUnit, (double)atT * kMassUnit};
+  if (order) {
+    const int64_t to = ((int64_t)r * ws.slices + slice) * kBins;
+    for (int b = tid; b < kBins; b += kScanThreads) {
+      uint64_t m = 0;
+      uint32_t c = 0;
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) {
+        m += mass_sh[i][b];
+        c += count_sh[i][b];
+      }
+      ws.mass[to + b] = m;
+      ws.count[to + b] = c;
+    }
+  }
+}
+
+// Where the bins of a row are cut.  Every workgroup of the second launch works it out, in the same operations; the third reads it.
+struct RowCut {
+  float top, per_unit, first_bin;  // the largest logit and its bin
+  int first_id;
+  bool slow;                       // not resolved by the bins
+  double at1, atT;                 // mass of the row at T = 1 and at T
+  int k_bin, p_lo, p_hi;           // bins in which top_k and top_p end: k_bin, and one of [p_lo, p_hi]; kNoBin: not cut
+  int sure;                        // bins below this one are kept but for min_p
+  float least;                     // min_p: no logit below this one
+  uint32_t least_key;
+  double mass_sure, mass_k;        // masses and numbers of tokens in front of bins `sure` and k_bin
+  uint32_t count_sure, count_k;
+  uint32_t n_first;                // tokens of the bins [p_lo, p_hi]
+};
+constexpr int kNoBin = 4 * kBins;
+struct CutShared {
+  double scale[kMaxSlices];
+  int shift[kMaxSlices];
+  double mass[kBins + 1];  // of the bins in front
+  uint32_t count[kBins + 1];
+  double wave_mass[kScanThreads / 64];
+  uint32_t wave_count[kScanThreads / 64];
+  int k_bin, p_lo, p_hi;
+};
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+__device__ __forceinline__ RowCut cut_row(const SampleWs& ws, int r, const RowParams& p, CutShared& sh) {
+  static_assert(kBins == 2 * kScanThreads, "two bins a thread");
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const SliceStat* stat = ws.stat + (int64_t)r * ws.slices;
+  RowCut c;
+  uint64_t best = 0;  // the first of the order, in every wavefront
+  for (int i = lane; i < ws.slices; i += kWave) {
+    const uint64_t t = ((uint64_t)key_of(stat[i].top) << 32) | (uint32_t)~stat[i].id;
+    best = t > best ? t : best;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) best = Max64()(best, shfl_xor64(best, o));
+  c.top = of_key((uint32_t)(best >> 32));
+  c.first_id = (int)~(uint32_t)best;
+  const bool drawn = p.temperature > 0.f, some = c.top > -INFINITY;
+  const float T = drawn ? p.temperature : 1.f;
+  c.per_unit = bins_per_unit(T);
+  c.first_bin = floorf(c.top * c.per_unit);
+  c.slow = drawn && some && !(fabsf(c.first_bin) <= kMostBin);
+  c.k_bin = c.p_lo = c.p_hi = c.sure = kNoBin;
+  c.least_key = some ? min_p_key(p.min_p, T, c.top) : 0u;
+  c.least = c.least_key > kKeyNone ? of_key(c.least_key) : -INFINITY;
+  c.at1 = c.atT = c.mass_sure = c.mass_k = 0.0;
+  c.count_sure = c.count_k = c.n_first = 0;
+  if (!some || c.slow) return c;  // uniform over the workgroup, like the others
+  for (int i = lane; i < ws.slices; i += kWave) {
+    const SliceStat t = stat[i];
+    const double down = (double)t.top - (double)c.top, f = exp(down / (double)T);  // (no number in the slice: 0)
+    const float shift = c.first_bin - floorf(t.top * c.per_unit);
+    c.at1 += t.at1 * exp(down);
+    c.atT += t.atT * f;
+    if (wave == 0) {
+      sh.scale[i] = f;
+      sh.shift[i] = shift < (float)kBins ? (int)shift : kBins;
+    }
+  }
+  c.at1 = wave_sum(c.at1);
+  c.atT = wave_sum(c.atT);
+  if (!drawn || !needs_order(p)) return c;
+  if (tid == 0) sh.k_bin = sh.p_lo = sh.p_hi = kNoBin;
+  __syncthreads();
+  double m[2] = {0.0, 0.0};
+  uint32_t n[2] = {0, 0};
+  for (int i = 0; i < ws.slices; ++i) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int from = 2 * tid + u - sh.shift[i];
+      if (from >= 0) {
+        const int64_t at = ((int64_t)r * ws.slices + i) * kBins + from;
+        m[u] += (double)ws.mass[at] * sh.scale[i];
+        n[u] += ws.count[at];
+      }
+    }
+  }
+  double im = m[0] + m[1];
+  uint32_t in = n[0] + n[1];
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const double om = __shfl_up(im, o, kWave);
+    const uint32_t on = __shfl_up(in, o, kWave);
+    if (lane >= o) {
+      im += om;
+      in += on;
+    }
+  }
+  if (lane == 63) {
+    sh.wave_mass[wave] = im;
+    sh.wave_count[wave] = in;
+  }
+  __syncthreads();
+  for (int w = 0; w < wave; ++w) {
+    im += sh.wave_mass[w];
+    in += sh.wave_count[w];
+  }
+  if (tid == 0) {
+    sh.mass[0] = 0.0;
+    sh.count[0] = 0;
+  }
+  sh.mass[2 * tid + 1] = im - m[1];
+  sh.count[2 * tid + 1] = in - n[1];
+  sh.mass[2 * tid + 2] = im;
+  sh.count[2 * tid + 2] = in;
+  __syncthreads();
+  if (p.top_k > 0) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (sh.count[2 * tid + u + 1] >= (uint32_t)p.top_k) atomicMin(&sh.k_bin, 2 * tid + u);
+    __syncthreads();
+    c.k_bin = sh.k_bin;
+  }
+  if (p.top_p < 1.f) {
+    // the masses here are good to 2^-23; which bin holds the end is left open by twice as much
+    constexpr double kLess = 1.0 - 1.0 / (1 << 22), kMore = 1.0 + 1.0 / (1 << 22);
+    const bool cut = c.k_bin < kBins;
+    const double lo = (double)p.top_p * (cut ? sh.mass[c.k_bin] : sh.mass[kBins]) * kLess;
+    const double hi = (double)p.top_p * (cut ? sh.mass[c.k_bin + 1] : sh.mass[kBins]) * kMore;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int b = 2 * tid + u;
+      if (sh.mass[b + 1] * kMore >= lo) atomicMin(&sh.p_lo, b);
+      if (sh.mass[b + 1] * kLess >= hi) atomicMin(&sh.p_hi, b);
+    }
+    __syncthreads();
+    c.p_hi = min(sh.p_hi, cut ? c.k_bin : kBins - 1);
+    c.p_lo = min(sh.p_lo, c.p_hi);
+  }
+  c.sure = min(c.k_bin, c.p_lo);
+  // where min_p ends in front of that, nothing else matters
+  if (c.least > -INFINITY && c.first_bin - floorf(c.least * c.per_unit) < (float)c.sure) c.k_bin = c.p_lo = c.p_hi = c.sure = kNoBin;
+  if (c.sure < kBins) {
+    c.mass_sure = sh.mass[c.sure];
+    c.count_sure = sh.count[c.sure];
+  }
+  if (c.k_bin < kBins) {
+    c.mass_k = sh.mass[c.k_bin];
+    c.count_k = sh.count[c.k_bin];
+  }
+  if (c.p_lo < kBins) c.n_first = sh.count[c.p_hi + 1] - sh.count[c.p_lo];
+  return c;
+}
+__device__ __forceinline__ bool is_sure(const RowCut& c, float bin, float z) { return bin < (float)c.sure && z >= c.least; }
+__device__ __forceinline__ float bin_of(const RowCut& c, float z) { return c.first_bin - floorf(z * c.per_unit); }
+
+template <class T>
+__global__ __launch_bounds__(kScanThreads) void sample_cut_kernel(const SampleArgs a, const SampleWs ws, int row0) {
+  constexpr int E = Chunk<T>::E, N = kSliceLogits / E / kScanThreads;
+  __shared__ CutShared sh;
+  __shared__ uint32_t listed;
+  const int slice = blockIdx.x, r = blockIdx.y, row = row0 + r, tid = threadIdx.x;
+  if (a.masked != nullptr && a.masked[row] == 0) return;
+  const RowParams p = row_params(a, row);
+  if (!(p.temperature > 0.f) && slice > 0) return;
+  const T* z = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
+  const int c0 = slice * (kSliceLogits / E) + tid, n_chunks = (a.vocab + E - 1) / E;
+  Chunk<T> x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) load_chunk(x[i], z, min(c0 + i * kScanThreads, n_chunks), a.vocab);
+  if (tid == 0) listed = 0;
+  const RowCut c = cut_row(ws, r, p, sh);
+  if (slice == 0 && tid == 0) ws.cut[r] = c;
+  if (c.top == -INFINITY || c.slow || !(p.temperature > 0.f)) return;  // uniform over the workgroup
+  const Scale s = scale_of(p.temperature);
+  uint64_t* list = ws.list + ((int64_t)r * ws.slices + slice) * kSliceList;
+  const float p_lo = (float)c.p_lo, p_hi = (float)c.p_hi, k_bin = (float)c.k_bin;
+  const bool lists = c.sure < kBins;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int chunk = c0 + i * kScanThreads;
+    uint64_t m = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float v = x[i].z[e], b = bin_of(c, v);
+      if (is_sure(c, b, v)) m += mass(v, c.top, s);
+      if (lists && ((b >= p_lo && b <= p_hi) || b == k_bin)) {
+        const uint32_t at = atomicAdd(&listed, 1u);
+        if (at < (uint32_t)kSliceList) list[at] = order_of(key_of(v), chunk * E + e);
+      }
+    }
+    if (__ballot(m != 0) != 0ull) {
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) m += shfl_xor64(m, o);
+    }
+    const int seg = chunk / kSegChunks;
+    if ((tid & 63) == 0 && seg < ws.segs) ws.seg[(int64_t)r * ws.segs + seg] = m;
+  }
+  __syncthreads();
+  if (tid == 0) ws.listed[(int64_t)r * ws.slices + slice] = listed;
+}
+
+constexpr int kMaxSegs = kSampleMaxVocab / (kSegChunks * 4);
+template <class T>
+__global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleArgs a, const SampleWs ws, int row0) {
+  constexpr int E = Chunk<T>::E;
+  __shared__ unsigned long long list[kRowList];
+  __shared__ unsigned long long seg[kMaxSegs];
+  __shared__ uint64_t sum_a[kRowThreads / 64], sum_b[kRowThreads / 64], wave_mass[kRowThreads / 64];
+  __shared__ int found, n_kept;
+  __shared__ uint64_t found_base;
+  const int r = blockIdx.x, row = row0 + r, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (a.masked != nullptr && a.masked[row] == 0) {
+    if (tid == 0) write_row(a, row, -1, 0.f, 0.f);
+    return;
+  }
+  const RowParams p = row_params(a, row);
+  const RowCut c = ws.cut[r];
+  if (c.top == -INFINITY) {
+    if (tid == 0) write_row(a, row, -1, 0.f, 0.f);
+    return;
+  }
+  if (!(p.temperature > 0.f)) {
+    if (tid == 0) write_row(a, row, c.first_id, (float)(1.0 / c.at1), 1.f);
+    return;
+  }
+  const Scale s = scale_of(p.temperature);
+  const bool lists = !c.slow && c.sure < kBins;
+  uint32_t n = 0;
+  bool slow = c.slow;
+  if (lists) {
+    for (int i = 0; i < ws.slices; ++i) {  // the slices' lists one behind the other
+      const uint32_t k = ws.listed[(int64_t)r * ws.slices + i];
+      slow = slow || k > (uint32_t)kSliceList || n + k > (uint32_t)kRowList;
+      if (slow) break;
+      for (uint32_t j = tid; j < k; j += kRowThreads) list[n + j] = ws.list[((int64_t)r * ws.slices + i) * kSliceList + j];
+      n += k;
+    }
+  }
+  if (slow) {  // uniform over the workgroup
+    search_row<T>(a, row, sum_a, sum_b, wave_mass, &found);
+    return;
+  }
+  for (int i = tid; i < ws.segs; i += kRowThreads) seg[i] = ws.seg[(int64_t)r * ws.segs + i];
+  uint64_t last = ~(uint64_t)0;  // the last token kept, if the list decides that
+  bool by_order = false;
+  if (lists) {
+    int pad = 1;
+    while (pad < (int)n) pad <<= 1;
+    for (int i = (int)n + tid; i < pad; i += kRowThreads) list[i] = ~0ull;
+    __syncthreads();
+    for (int size = 2; size <= pad; size <<= 1)  // bitonic
+      for (int step = size >> 1; step > 0; step >>= 1) {
+        for (int i = tid; i < pad / 2; i += kRowThreads) {
+          const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
+          const unsigned long long x = list[lo], y = list[hi];
+          if ((x > y) == ((lo & size) == 0)) {
+            list[lo] = y;
+            list[hi] = x;
+          }
+        }
+        __syncthreads();
+      }
+    // masses of the list, each thread a run of it; the list is [sure, ...] and, where top_k ends further down, that bin behind it
+    constexpr int RUN = kRowList / kRowThreads;
+    uint64_t m[RUN], mine = 0;
+    const int j0 = tid * RUN;
+#pragma unroll
+    for (int u = 0; u < RUN; ++u) {
+      m[u] = j0 + u < (int)n ? mass(of_key(key_in(list[j0 + u])), c.top, s) : 0;
+      mine += m[u];
+    }
+    uint64_t before = mine;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const uint32_t lo = (uint32_t)__shfl_up((int)(uint32_t)before, o, kWave), hi = (uint32_t)__shfl_up((int)(uint32_t)(before >> 32), o, kWave);
+      if (lane >= o) before += ((uint64_t)hi << 32) | lo;
+    }
+    if (lane == 63) wave_mass[wave] = before;
+    if (tid == 0) n_kept = 0;
+    __syncthreads();
+    before -= mine;
+    for (int w = 0; w < wave; ++w) before += wave_mass[w];
+    const bool apart = c.k_bin < kBins && c.k_bin > c.p_hi && c.p_lo < kBins;
+    const int n_first = apart ? min((int)c.n_first, (int)n) : (int)n;
+    // tokens in front of the j-th entry: in front of its part of the list, and in the list
+    auto in_front = [&](int j) { return (j < n_first ? c.count_sure : c.count_k - (uint32_t)n_first) + (uint32_t)j; };
+    double all = c.atT / kMassUnit;
+    if (c.k_bin < kBins && p.top_p < 1.f) {  // the mass of the first top_k
+      uint64_t upto = 0;
+#pragma unroll
+      for (int u = 0; u < RUN; ++u) {
+        const int j = j0 + u;
+        if (j < (int)n && (!apart || j >= n_first) && in_front(j) < (uint32_t)p.top_k) upto += m[u];
+      }
+      all = (apart ? c.mass_k : c.mass_sure) + (double)block_reduce64<kRowThreads>(upto, sum_a, Add64());
+    }
+    const double target = p.top_p < 1.f ? (double)p.top_p * all : INFINITY;
+    uint64_t front = before;
+    int mine_kept = 0;
+#pragma unroll
+    for (int u = 0; u < RUN; ++u) {
+      const int j = j0 + u;
+      if (j < n_first) {
+        const bool first = in_front(j) == 0;
+        const bool in_k = p.top_k <= 0 || in_front(j) < (uint32_t)p.top_k, in_p = c.mass_sure + (double)front < target;
+        if (first || (in_k && in_p && key_in(list[j]) >= c.least_key)) mine_kept = j + 1;
+      }
+      front += m[u];
+    }
+    atomicMax(&n_kept, mine_kept);
+    __syncthreads();
+    const int kept = n_kept;  // a prefix
+    by_order = kept > 0;
+    if (by_order) last = list[kept - 1];
+#pragma unroll
+    for (int u = 0; u < RUN; ++u)
+      if (j0 + u < kept) atomicAdd(&seg[(int)(uint32_t)list[j0 + u] / (E * kSegChunks)], (unsigned long long)m[u]);
+  }
+  __syncthreads();
+  // the segment that the random number falls into
+  const int per = (ws.segs + kRowThreads - 1) / kRowThreads, g0 = tid * per;
+  uint64_t mine = 0;
+  for (int g = g0; g < min(g0 + per, ws.segs); ++g) mine += seg[g];
+  uint64_t before = mine;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const uint32_t lo = (uint32_t)__shfl_up((int)(uint32_t)before, o, kWave), hi = (uint32_t)__shfl_up((int)(uint32_t)(before >> 32), o, kWave);
+    if (lane >= o) before += ((uint64_t)hi << 32) | lo;
+  }
+  __syncthreads();
+  if (lane == 63) wave_mass[wave] = before;
+  if (tid == 0) found = -1;
+  __syncthreads();
+  before -= mine;
+  uint64_t total = 0;
+  for (int w = 0; w < kRowThreads / 64; ++w) {
+    if (w < wave) before += wave_mass[w];
+    total += wave_mass[w];
+  }
+  const double want = (double)p.u * (double)total;
+  // the first whose end lies past `want`; the last with a mass takes what rounding leaves
+  auto here = [&](uint64_t from, uint64_t m) { return m > 0 && (double)from <= want && (!((double)(from + m) <= want) || from + m == total); };
+  for (int g = g0; g < min(g0 + per, ws.segs); ++g) {
+    const uint64_t m = seg[g];
+    if (here(before, m)) {
+      found = g;
+      found_base = before;
+    }
+    before += m;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  const int g = found;
+  const T* z = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
+  const int chunk = g * kSegChunks + lane, n_chunks = (a.vocab + E - 1) / E;
+  Chunk<T> x;
+  load_chunk(x, z, min(chunk, n_chunks), a.vocab);
+  uint64_t m[E];
+  mine = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float v = x.z[e];
+    const bool held = by_order ? order_of(key_of(v), chunk * E + e) <= last : is_sure(c, bin_of(c, v), v);
+    m[e] = held ? mass(v, c.top, s) : 0;
+    mine += m[e];
+  }
+  before = mine;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const uint32_t lo = (uint32_t)__shfl_up((int)(uint32_t)before, o, kWave), hi = (uint32_t)__shfl_up((int)(uint32_t)(before >> 32), o, kWave);
+    if (lane >= o) before += ((uint64_t)hi << 32) | lo;
+  }
+  before += found_base - mine;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (here(before, m[e])) {
+      const Scale s1 = scale_of(1.f);
+      write_row(a, row, chunk * E + e, (float)((double)weight(x.z[e], c.top, s1) / c.at1), (float)((double)weight(x.z[e], c.top, s) / ((double)total * kMassUnit)));
+    }
+    before += m[e];
+  }
+}
+
+struct SamplePlan {
+  int slices, segs, rows;  // rows of a pass
+  size_t stat, mass, count, listed, list, cut, seg, total;
+};
+static SamplePlan plan_sample(int n_rows, int vocab) {
+  SamplePlan p;
+  auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  p.slices = ceil_div(vocab, kSliceLogits);
+  p.segs = ceil_div(vocab, kSegChunks * 4);  // of float32, which has the shorter chunks
+  p.rows = std::max(1, std::min({n_rows, 1024, 4096 / p.slices}));
+  const size_t n = (size_t)p.rows * p.slices;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += align(bytes);
+    return at;
+  };
+  p.stat = take(n * sizeof(SliceStat));
+  p.mass = take(n * kBins * sizeof(uint64_t));
+  p.count = take(n * kBins * sizeof(uint32_t));
+  p.listed = take(n * sizeof(uint32_t));
+  p.list = take(n * kSliceList * sizeof(uint64_t));
+  p.cut = take((size_t)p.rows * sizeof(RowCut));
+  p.seg = take((size_t)p.rows * p.segs * sizeof(uint64_t));
+  p.total = off;
+  return p;
+}
+size_t sample_tokens_workspace(int n_rows, int vocab) { return plan_sample(n_rows, vocab).total; }
+
+template <class T>
+static hipError_t launch_sample_t(const SampleArgs& a, const SamplePlan& p, char* w, hipStream_t st) {
+  SampleWs ws;
+  ws.stat = reinterpret_cast<SliceStat*>(w + p.stat);
+  ws.mass = reinterpret_cast<uint64_t*>(w + p.mass);
+  ws.count = reinterpret_cast<uint32_t*>(w + p.count);
+  ws.listed = reinterpret_cast<uint32_t*>(w + p.listed);
+  ws.list = reinterpret_cast<uint64_t*>(w + p.list);
+  ws.cut = reinterpret_cast<RowCut*>(w + p.cut);
+  ws.seg = reinterpret_cast<uint64_t*>(w + p.seg);
+  ws.slices = p.slices;
+  ws.segs = ceil_div(a.vocab, kSegChunks * Chunk<T>::E);
+  for (int row0 = 0; row0 < a.n_rows; row0 += p.rows) {  // the passes use the workspace one after the other
+    const int rows = std::min(p.rows, a.n_rows - row0);
+    hipLaunchKernelGGL(sample_scan_kernel<T>, dim3(p.slices, rows), dim3(kScanThreads), 0, st, a, ws, row0);
+    hipLaunchKernelGGL(sample_cut_kernel<T>, dim3(p.slices, rows), dim3(kScanThreads), 0, st, a, ws, row0);
+    hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(rows), dim3(kRowThreads), 0, st, a, ws, row0);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 
 hipError_t launch_sample_tokens(const void* logits, int dtype, int64_t row_stride, const uint8_t* masked, const float* uniform, const float* temperature,
                                 const int32_t* top_k, const float* top_p, const float* min_p, int n_rows, int vocab, int32_t* tokens, float* conf,
-                                float* prob, void*, hipStream_t st) {
+                                float* prob, void* workspace, hipStream_t st) {
   const SampleArgs a = {logits, row_stride, masked, uniform, temperature, top_k, top_p, min_p, n_rows, vocab, tokens, conf, prob};
-  if (dtype == FOCUS_F32)
-    hipLaunchKernelGGL(sample_row_kernel<float>, dim3(n_rows), dim3(kRowThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL(sample_row_kernel<uint16_t>, dim3(n_rows), dim3(kRowThreads), 0, st, a);
-  return hipGetLastError();
+  const SamplePlan p = plan_sample(n_rows, vocab);
+  return dtype == FOCUS_F32 ? launch_sample_t<float>(a, p, static_cast<char*>(workspace), st) : launch_sample_t<uint16_t>(a, p, static_cast<char*>(workspace), st);
 }
 
 }  // namespace focus
