@@ -122,7 +122,8 @@ def _ptr(t) -> int | None:
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # the handle of torch.cuda.current_stream() without the object around it: 0.1 us instead of 2.7, a quarter of a short call's host time
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _need(t: torch.Tensor, dtype, name: str) -> None:
