@@ -19,11 +19,11 @@ constexpr int kMassBits = 42;
 static_assert(((uint64_t)kSampleMaxVocab << kMassBits) <= ((uint64_t)1 << 63), "the mass of a row fits");
 
 // ---- logits
-// as a float32: NaN counts as -inf, +inf as the largest number, -0 as +0
-__device__ __forceinline__ float clean(float z) { return z == z ? fminf(z, 3.402823466e38f) + 0.f : -INFINITY; }
-// whole numbers in the order of the numbers
+// as a float32: NaN counts as -inf, +inf as the largest number
+__device__ __forceinline__ float clean(float z) { return fminf(fmaxf(z, -INFINITY), 3.402823466e38f); }
+// whole numbers in the order of the numbers, -0 as +0
 __device__ __forceinline__ uint32_t key_of(float z) {
-  const uint32_t u = __float_as_uint(z);
+  const uint32_t u = __float_as_uint(z + 0.f);
   return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float of_key(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
@@ -36,23 +36,74 @@ struct Chunk {
   float z[E];
 };
 template <class T>
-__device__ __forceinline__ void load_chunk(Chunk<T>& x, const T* row, int chunk, int vocab) {
-  constexpr int E = Chunk<T>::E;
-  const int i0 = chunk * E;
-  if (i0 + E <= vocab) {
-    const uint4 w = *reinterpret_cast<const uint4*>(row + i0);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ void unpack(Chunk<T>& x, const uint4& w) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      x.z[e] = clean(sizeof(T) == 4 ? __uint_as_float(u[e & 3]) : ((e & 1) ? bf16_hi(u[(e >> 1) & 3]) : bf16_lo(u[(e >> 1) & 3])));
-  } else {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      float z = -INFINITY;
-      if (i0 + e < vocab) z = sizeof(T) == 4 ? *reinterpret_cast<const float*>(row + i0 + e) : bf16_lo(*reinterpret_cast<const uint16_t*>(row + i0 + e));
-      x.z[e] = clean(z);
+  for (int e = 0; e < Chunk<T>::E; ++e)
+    x.z[e] = clean(sizeof(T) == 4 ? __uint_as_float(u[e & 3]) : ((e & 1) ? bf16_hi(u[(e >> 1) & 3]) : bf16_lo(u[(e >> 1) & 3])));
+}
+template <class T>
+__device__ __forceinline__ float logit_at(const T* row, int id) {
+  return clean(sizeof(T) == 4 ? *reinterpret_cast<const float*>(row + id) : bf16_lo(*reinterpret_cast<const uint16_t*>(row + id)));
+}
+// The N chunks c0, c0 + step, ... of a thread, packed: all requests first, none of them conditional.  A row's last, shorter chunk is read
+// logit by logit, by whoever has it.
+template <class T, int N>
+struct Chunks {
+  uint4 w[N];
+  // f(i, chunk) for each of them, in a loop that is not unrolled: it takes the first and turns the others around.  (These launches
+  // are a few microseconds long and start with a cold instruction cache: 32 logits unrolled took twice as long as four times eight.)
+  template <class F>
+  __device__ __forceinline__ void each(F&& f) {
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
+      Chunk<T> x;
+      unpack(x, w[0]);
+      f(i, x);
+      turn();
     }
   }
+  __device__ __forceinline__ void turn() {
+    const uint4 first = w[0];
+#pragma unroll
+    for (int j = 0; j + 1 < N; ++j) w[j] = w[j + 1];
+    w[N - 1] = first;
+  }
+  __device__ __forceinline__ void load(const T* row, int c0, int step, int vocab) {
+    constexpr int E = Chunk<T>::E;
+    const int whole = vocab / E;
+    if (whole > 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = *reinterpret_cast<const uint4*>(row + (int64_t)min(c0 + i * step, whole - 1) * E);
+    }
+    if (__ballot(c0 + (N - 1) * step >= whole) != 0ull) {
+#pragma unroll 1
+      for (int i = 0; i < N; ++i) {
+        const int ch = c0 + i * step;
+        if (ch >= whole) {
+          uint32_t u[4];
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const bool in = ch == whole && ch * E + e < vocab;
+            if constexpr (sizeof(T) == 4) {
+              u[e] = in ? *reinterpret_cast<const uint32_t*>(row + ch * E + e) : 0xff800000u;
+            } else {
+              const uint32_t b = in ? *reinterpret_cast<const uint16_t*>(row + ch * E + e) : 0xff80u;
+              u[e / 2] = (e & 1) ? u[e / 2] | (b << 16) : b;
+            }
+          }
+          w[0] = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+        turn();
+      }
+    }
+  }
+};
+template <class T>
+__device__ __forceinline__ void load_chunk(Chunk<T>& x, const T* row, int chunk, int vocab) {
+  Chunks<T, 1> c;
+  c.load(row, chunk, 0, vocab);
+  unpack(x, c.w[0]);
 }
 
 // ---- masses
@@ -61,10 +112,11 @@ struct Scale {
   float hi, lo;
 };
 __device__ __forceinline__ Scale scale_of(float temperature) {
-  const double c = fmin(1.4426950408889634 / (double)temperature, 3e38);
+  constexpr float kHi = 1.44269504f, kLo = (float)(1.4426950408889634 - (double)kHi);
   Scale s;
-  s.hi = (float)c;
-  s.lo = (float)(c - (double)s.hi);
+  s.hi = fminf(kHi / temperature, 3e38f);
+  s.lo = (__builtin_fmaf(-s.hi, temperature, kHi) + kLo) / temperature;  // what the division leaves over
+  if (!(s.hi > 1e-30f && s.hi < 1e30f)) s.lo = 0.f;
   return s;
 }
 // 2^-((top - z) * s): the product is taken with what its rounding leaves over (of a difference of 20 and more that would be ten units of
@@ -136,13 +188,23 @@ struct RowParams {
   float temperature, top_p, min_p, u;
   int top_k;
 };
+// the same address for every lane, of memory that nobody writes meanwhile: a scalar load
+template <class V>
+__device__ __forceinline__ V uniform_load(const V* ptr) {
+  typedef const __attribute__((address_space(4))) V* cptr_t;
+  return *(cptr_t)(uintptr_t)ptr;
+}
 __device__ __forceinline__ RowParams row_params(const SampleArgs& a, int row) {
+  // all requests at once: what is not given is read from `uniform` and replaced
+  const float temperature = uniform_load((a.temperature ? a.temperature : a.uniform) + row), top_p = uniform_load((a.top_p ? a.top_p : a.uniform) + row),
+              min_p = uniform_load((a.min_p ? a.min_p : a.uniform) + row), u = uniform_load(a.uniform + row);
+  const int top_k = uniform_load((a.top_k ? a.top_k : reinterpret_cast<const int32_t*>(a.uniform)) + row);
   RowParams p;
-  p.temperature = a.temperature ? a.temperature[row] : 1.f;
-  p.top_p = a.top_p ? a.top_p[row] : 1.f;
-  p.min_p = a.min_p ? a.min_p[row] : 0.f;
-  p.top_k = a.top_k ? a.top_k[row] : 0;
-  p.u = fmaxf(a.uniform[row], 0.f);  // NaN: 0
+  p.temperature = a.temperature ? temperature : 1.f;
+  p.top_p = a.top_p ? top_p : 1.f;
+  p.min_p = a.min_p ? min_p : 0.f;
+  p.top_k = a.top_k ? top_k : 0;
+  p.u = fmaxf(u, 0.f);  // NaN: 0
   if (p.top_k == 1 || p.top_p <= 0.f || p.min_p > 1.f) p.temperature = 0.f;  // only the first stays
   return p;
 }
@@ -151,11 +213,11 @@ __device__ __forceinline__ void write_row(const SampleArgs& a, int row, int toke
   if (a.conf) a.conf[row] = conf;
   if (a.prob) a.prob[row] = prob;
 }
-// the smallest key that min_p keeps: w >= min_p <=> z >= top + T ln(min_p)
-__device__ __forceinline__ uint32_t min_p_key(float min_p, float temperature, float top) {
+// the smallest key that min_p keeps: w >= min_p <=> z >= top + T ln(min_p); `down`: T ln(min_p), of a min_p between 0 and 1
+__device__ __forceinline__ uint32_t min_p_key(float min_p, double down, float top) {
   if (!(min_p > 0.f)) return 0u;
   if (min_p >= 1.f) return key_of(top);
-  const double cut = (double)top + (double)temperature * log((double)min_p);
+  const double cut = (double)top + down;
   float z = (float)cut;
   if ((double)z < cut) z = of_key(key_of(z) + 1u);
   return key_of(clean(z));
@@ -263,7 +325,7 @@ __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t*
       ties = n;
     }
   }
-  const uint32_t m_key = min(min_p_key(p.min_p, p.temperature, top), top_key);
+  const uint32_t m_key = min(min_p_key(p.min_p, (double)p.temperature * log((double)p.min_p), top), top_key);
   if (m_key > cut) {
     cut = m_key;
     ties = ~(uint64_t)0;
@@ -369,14 +431,14 @@ struct RowCut {
   float top;
   int first_id;
   int way;                         // kNone, kFirst, kDraw, kSearch
-  double at1, atT;                 // sum of the weights at T = 1 and at T
   int ends;                        // 0: nothing is cut but by min_p; else the list decides
-  float sure;                      // logits from here on are kept
-  float least;                     // min_p: none below this one
-  uint32_t least_key;
+  float per_unit;                  // bins per unit of logit; the next four are logits times that
+  float sure;                      // tokens from here on are kept
   float p_low, k_high, k_low;      // the list: [p_low, sure) and [k_low, k_high), where top_k ends apart from top_p
   bool apart;
   uint32_t count_sure, count_k;    // tokens above `sure`, above k_high
+  float least;                     // min_p: no logit below this one
+  uint32_t least_key;
 };
 enum { kNone = 0, kFirst = 1, kDraw = 2, kSearch = 3 };
 struct SampleWs {
@@ -394,11 +456,6 @@ __device__ __forceinline__ uint32_t key_in(uint64_t order) { return ~(uint32_t)(
 __device__ __forceinline__ float bins_per_unit(float temperature) { return fminf(kBinsPerNat / temperature, kMostPerUnit); }
 constexpr double kMassUnit = 1.0 / (double)((uint64_t)1 << kMassBits);
 __device__ __forceinline__ bool needs_order(const RowParams& p) { return p.top_k > 0 || p.top_p < 1.f; }
-template <class T>
-__device__ __forceinline__ float logit_at(const void* row, int id) {
-  return clean(sizeof(T) == 4 ? static_cast<const float*>(row)[id] : bf16_lo(static_cast<const uint16_t*>(row)[id]));
-}
-
 template <class T, int SLICE>
 __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleArgs a, const SampleWs ws, int row0) {
   constexpr int E = Chunk<T>::E, N = SLICE / E / kScanThreads, kCopies = 4, kWaves = kScanThreads / 64;
@@ -408,25 +465,24 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleA
   __shared__ double at1_sh[kWaves], atT_sh[kWaves];
   __shared__ int id_sh;
   const int slice = blockIdx.x, r = blockIdx.y, row = row0 + r, tid = threadIdx.x;
-  if (a.masked != nullptr && a.masked[row] == 0) return;
-  const T* z = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
-  const int c0 = slice * (SLICE / E) + tid, n_chunks = (a.vocab + E - 1) / E;
-  Chunk<T> x[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) load_chunk(x[i], z, min(c0 + i * kScanThreads, n_chunks), a.vocab);
   const RowParams p = row_params(a, row);
+  if (a.masked != nullptr && a.masked[row] == 0) return;
+  const int c0 = slice * (SLICE / E) + tid;
+  Chunks<T, N> chunks;
+  chunks.load(static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride, c0, kScanThreads, a.vocab);
   const bool drawn = p.temperature > 0.f, order = drawn && needs_order(p);  // uniform over the workgroup
-  if (order)
-    for (int i = tid; i < kCopies * kBins; i += kScanThreads) (&bins_sh[0][0])[i] = 0;
+  if (order) {
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) bins_sh[i][tid] = 0;
+  }
   if (tid == 0) id_sh = 0x7fffffff;
   float mine = -INFINITY;
+  chunks.each([&](int, const Chunk<T>& x) {
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int e = 0; e < E; ++e) mine = fmaxf(mine, x[i].z[e]);
-  float top = mine;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, kWave));
+    for (int e = 0; e < E; ++e) mine = fmaxf(mine, x.z[e]);
+  });
+  auto larger = [](uint32_t x, uint32_t y) { return x > y ? x : y; };
+  float top = of_key(wave_reduce_u32(key_of(mine), larger));
   if ((tid & 63) == 0) top_sh[tid >> 6] = top;
   __syncthreads();
 #pragma unroll
@@ -438,45 +494,42 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleA
   }
   if (mine == top) {
     int id = 0x7fffffff;
+    chunks.each([&](int i, const Chunk<T>& x) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (x[i].z[e] == top) id = min(id, (c0 + i * kScanThreads) * E + e);
+      for (int e = E - 1; e >= 0; --e)
+        if (x.z[e] == top) id = min(id, (c0 + i * kScanThreads) * E + e);
+    });
     atomicMin(&id_sh, id);
   }
+  // exp(f / 16) - 1 = g(f) / 16 for the place f of a token in its bin: 1 + f / 32 + f^2 / 1536 times f, in units of 2^-17
+  const float T_ = drawn ? p.temperature : 1.f, per_unit = bins_per_unit(T_), first = floorf(top * per_unit);
+  const Scale s = scale_of(T_);
+  const bool all = order && p.top_p < 1.f, conf = a.conf != nullptr;
+  unsigned long long* bins = bins_sh[tid & (kCopies - 1)];
   float at1 = 0.f, atT = 0.f;
-  if (a.conf != nullptr) {
+  chunks.each([&](int, const Chunk<T>& x) {
+    if (conf) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+      for (int e = 0; e < E; ++e) at1 += __builtin_amdgcn_exp2f((x.z[e] - top) * 1.4426950408889634f);
+    }
+    if (all) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) at1 += __builtin_amdgcn_exp2f((x[i].z[e] - top) * 1.4426950408889634f);
-  }
-  if (order && p.top_p < 1.f) {
-    const Scale s = scale_of(p.temperature);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-      for (int e = 0; e < E; ++e) atT += weight<BF16>(x[i].z[e], top, s);
-  }
-  if (order) {
-    // exp(f / 16) - 1 = g(f) / 16 for the place f of a token in its bin: 1 + f / 32 + f^2 / 1536 times f, in units of 2^-17
-    const float per_unit = bins_per_unit(p.temperature), first = floorf(top * per_unit);
-    const int copy = tid & (kCopies - 1);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
+      for (int e = 0; e < E; ++e) atT += weight<BF16>(x.z[e], top, s);
+    }
+    if (order) {
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float t = x[i].z[e] * per_unit, low = floorf(t), b = first - low;
+        const float t = x.z[e] * per_unit, low = floorf(t), b = first - low;
         if (b < (float)kBins) {
           const float f = t - low;
           const uint32_t g = (uint32_t)(f * __builtin_fmaf(f, __builtin_fmaf(f, 131072.f / 1536.f, 131072.f / 32.f), 131072.f));
-          atomicAdd(&bins_sh[copy][(int)b], (1ull << 32) | g);
+          atomicAdd(&bins[(int)b], (1ull << 32) | g);
         }
       }
-  }
+    }
+  });
   double d1 = (double)at1, dT = (double)atT;
-#pragma unroll
+#pragma unroll 1
   for (int o = 32; o > 0; o >>= 1) {
     d1 += __shfl_xor(d1, o, kWave);
     dT += __shfl_xor(dT, o, kWave);
@@ -503,12 +556,16 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleA
   }
 }
 
+constexpr int kNoBin = 4 * kBins;
 struct CutShared {
+  RowCut cut;
   int shift[4 * kMaxSlices];
-  double mass[kBins + 1];  // of the bins in front
+  float mass[kBins + 1];  // of the bins in front
   uint32_t count[kBins + 1];
-  double wave_mass[kScanThreads / 64];
+  unsigned long long above[kBins];
+  float wave_mass[kScanThreads / 64];
   uint32_t wave_count[kScanThreads / 64];
+  double down_min_p;
   int k_bin, p_lo, p_hi;
 };
 __device__ __forceinline__ double wave_sum(double v) {
@@ -516,72 +573,91 @@ __device__ __forceinline__ double wave_sum(double v) {
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
   return v;
 }
-// the smallest logit of the bins up to `last`: floor(z * per_unit) >= first - last
-__device__ __forceinline__ float bin_end(float first, int last, float per_unit) {
-  const float n = first - (float)last;
-  uint32_t k = key_of(clean(n / per_unit));
-  for (int i = 0; i < 4 && floorf(of_key(k) * per_unit) >= n; ++i) --k;
-  for (int i = 0; i < 8 && !(floorf(of_key(k) * per_unit) >= n); ++i) ++k;
-  return of_key(k);
-}
-// Every workgroup of the second launch works this out, in the same operations; the third reads it.
+// Every workgroup of the second launch works this out, in the same operations; the third reads it.  The slices' statistics are one
+// wavefront's work, the logarithm of min_p another's.  Nothing but latency: the
+// histograms are requested beside the statistics, before it is known how far the slices' bins are apart, and meet in LDS.
 __device__ __forceinline__ RowCut cut_row(const SampleWs& ws, int r, const RowParams& p, CutShared& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const SliceStat* stat = ws.stat + (int64_t)r * ws.slices;
-  RowCut c;
-  uint64_t best = 0;  // the first of the order, in every wavefront
-  for (int i = lane; i < ws.slices; i += kWave) {
-    const uint64_t t = ((uint64_t)key_of(stat[i].top) << 32) | (uint32_t)~stat[i].id;
-    best = t > best ? t : best;
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) best = Max64()(best, shfl_xor64(best, o));
-  c.top = of_key((uint32_t)(best >> 32));
-  c.first_id = (int)~(uint32_t)best;
-  const bool drawn = p.temperature > 0.f;
+  const bool drawn = p.temperature > 0.f, order = drawn && needs_order(p);
   const float T = drawn ? p.temperature : 1.f;
-  const float per_unit = bins_per_unit(T), first = floorf(c.top * per_unit);
-  c.way = !(c.top > -INFINITY) ? kNone : (!drawn ? kFirst : (fabsf(first) <= kMostBin ? kDraw : kSearch));
-  c.ends = 0;
-  c.apart = false;
-  c.least_key = c.way == kDraw ? min_p_key(p.min_p, T, c.top) : 0u;
-  c.least = c.least_key > kKeyNone ? of_key(c.least_key) : -INFINITY;
-  c.sure = -3.402823466e38f;
-  c.p_low = c.k_high = c.k_low = INFINITY;
-  c.at1 = c.atT = 0.0;
-  c.count_sure = c.count_k = 0;
-  if (c.way != kFirst && c.way != kDraw) return c;  // uniform over the workgroup, like the others
-  for (int i = lane; i < ws.slices; i += kWave) {
-    const SliceStat t = stat[i];
-    const double down = (double)t.top - (double)c.top;  // (no number in the slice: -inf)
-    const float shift = first - floorf(t.top * per_unit);
-    c.at1 += t.at1 * exp(down);
-    c.atT += t.atT * exp(down / (double)T);
-    if (wave == 0) sh.shift[i] = shift < (float)kBins ? (int)shift : kBins;
+  const float per_unit = bins_per_unit(T);
+  constexpr int kAhead = 8;
+  const uint64_t* bins = ws.bins + (int64_t)r * ws.slices * kBins + tid;
+  uint64_t v[kAhead];
+  if (order) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) v[u] = bins[(int64_t)min(u, ws.slices - 1) * kBins];  // (of a slice without a number: whatever lies there)
   }
-  c.at1 = wave_sum(c.at1);
-  c.atT = wave_sum(c.atT);
-  if (!drawn || !needs_order(p)) return c;
-  constexpr int kNoBin = 4 * kBins;
-  if (tid == 0) sh.k_bin = sh.p_lo = sh.p_hi = kNoBin;
-  __syncthreads();
-  uint32_t n = 0;
-  uint64_t above = 0;
-  for (int i = 0; i < ws.slices; ++i) {
-    const int from = tid - sh.shift[i];
-    if (from >= 0) {
-      const uint64_t v = ws.bins[((int64_t)r * ws.slices + i) * kBins + from];
-      n += (uint32_t)(v >> 32);
-      above += (uint32_t)v;
+  sh.count[tid + 1] = 0;
+  sh.above[tid] = 0;
+  if (wave == 0) {
+    RowCut c;
+    auto larger = [](uint32_t x, uint32_t y) { return x > y ? x : y; };
+    uint32_t key = 0;
+    for (int i0 = 0; i0 < ws.slices; i0 += kWave) {
+      const int i = i0 + lane;
+      key = larger(key, i < ws.slices ? key_of(stat[i].top) : 0u);
+    }
+    key = wave_reduce_u32(key, larger);
+    c.top = of_key(key);
+    const float first = floorf(c.top * per_unit);
+    c.first_id = 0x7fffffff;
+    for (int i0 = 0; i0 < ws.slices; i0 += kWave) {
+      const int i = i0 + lane;
+      const float t = i < ws.slices ? stat[i].top : -INFINITY;
+      const int id = i < ws.slices ? stat[i].id : 0;
+      const unsigned long long at = __ballot(t == c.top);  // (slices are in the order of the ids)
+      if (at != 0ull && c.first_id == 0x7fffffff) c.first_id = __builtin_amdgcn_readlane(id, __ffsll((long long)at) - 1);
+      if (i < ws.slices) {  // (no number in the slice: -inf)
+        const float shift = first - floorf(t * per_unit);
+        sh.shift[i] = shift < (float)kBins ? (int)shift : kBins;
+      }
+    }
+    c.way = !(c.top > -INFINITY) ? kNone : (!drawn ? kFirst : (fabsf(first) <= kMostBin ? kDraw : kSearch));
+    c.ends = 0;
+    c.per_unit = per_unit;
+    c.sure = -INFINITY;
+    c.p_low = c.k_high = c.k_low = INFINITY;
+    c.apart = false;
+    c.count_sure = c.count_k = 0;
+    if (lane == 0) {
+      sh.cut = c;
+      sh.k_bin = sh.p_lo = sh.p_hi = kNoBin;
+      sh.mass[0] = 0.f;
+      sh.count[0] = 0;
     }
   }
-  const double m = exp(((double)first - (double)tid - (double)c.top * (double)per_unit) / (double)kBinsPerNat) *
-                   ((double)n + (double)above / (131072.0 * (double)kBinsPerNat));
-  double im = m;
+  if (wave == 1 && lane == 0) sh.down_min_p = p.min_p > 0.f && p.min_p < 1.f ? (double)T * log((double)p.min_p) : 0.0;
+  __syncthreads();
+  RowCut c = sh.cut;
+  c.least_key = c.way == kDraw ? min_p_key(p.min_p, sh.down_min_p, c.top) : 0u;
+  c.least = c.least_key > kKeyNone ? of_key(c.least_key) : -3.402823466e38f;
+  if (c.way != kDraw || !order) return c;  // uniform over the workgroup, like the others
+  const float first = floorf(c.top * per_unit);
+  for (int i0 = 0; i0 < ws.slices; i0 += kAhead) {
+    if (i0 > 0) {
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) v[u] = bins[(int64_t)min(i0 + u, ws.slices - 1) * kBins];
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (i0 + u >= ws.slices) break;
+      const int to = tid + sh.shift[i0 + u];
+      if (to < kBins && v[u] != 0) {
+        atomicAdd(&sh.count[to + 1], (uint32_t)(v[u] >> 32));
+        atomicAdd(&sh.above[to], (unsigned long long)(uint32_t)v[u]);
+      }
+    }
+  }
+  __syncthreads();
+  const uint32_t n = sh.count[tid + 1];
+  const float down = (first - (float)tid - c.top * per_unit) * (1.4426950408889634f / kBinsPerNat);
+  float im = __builtin_amdgcn_exp2f(down) * ((float)n + (float)sh.above[tid] * (1.f / (131072.f * kBinsPerNat)));
   uint32_t in = n;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
-    const double om = __shfl_up(im, o, kWave);
+    const float om = __shfl_up(im, o, kWave);
     const uint32_t on = __shfl_up(in, o, kWave);
     if (lane >= o) {
       im += om;
@@ -597,27 +673,22 @@ __device__ __forceinline__ RowCut cut_row(const SampleWs& ws, int r, const RowPa
     im += sh.wave_mass[w];
     in += sh.wave_count[w];
   }
-  if (tid == 0) {
-    sh.mass[0] = 0.0;
-    sh.count[0] = 0;
-  }
   sh.mass[tid + 1] = im;
   sh.count[tid + 1] = in;
-  int k_bin = kNoBin, p_lo = kNoBin, p_hi = kNoBin;
-  if (p.top_k > 0) {
-    if (in >= (uint32_t)p.top_k && in - n < (uint32_t)p.top_k) sh.k_bin = tid;  // (the counts ascend: one thread at most)
-    __syncthreads();
-    k_bin = sh.k_bin;
-  }
+  if (p.top_k > 0 && in >= (uint32_t)p.top_k && in - n < (uint32_t)p.top_k) sh.k_bin = tid;  // (the counts ascend: one thread at most)
+  __syncthreads();
+  const int k_bin = sh.k_bin;
+  int p_lo = kNoBin, p_hi = kNoBin;
   if (p.top_p < 1.f) {
-    __syncthreads();
     const bool cut = k_bin < kBins;
     if (per_unit < kMostPerUnit) {
-      // a mass is good to 2^-17 and what the product z * per_unit rounds off; which bin holds the end is left open by more than that
-      const double off = 1.0 / 65536.0 + ((double)fabsf(first) + kBins) / 33554432.0;
-      const double lo = (double)p.top_p * sh.mass[cut ? k_bin : kBins] * (1.0 - off), hi = (double)p.top_p * sh.mass[cut ? k_bin + 1 : kBins] * (1.0 + off);
-      if (im * (1.0 + off) >= lo) atomicMin(&sh.p_lo, tid);
-      if (im * (1.0 - off) >= hi) atomicMin(&sh.p_hi, tid);
+      // a mass is good to 2^-17, a sum of them to 2^-20, and to what the product z * per_unit rounds off; which bin holds the end is left
+      // open by more than that
+      const float off = 1.f / 32768.f + (fabsf(first) + kBins) / 33554432.f;
+      const float lo = p.top_p * sh.mass[cut ? k_bin : kBins] * (1.f - off), hi = p.top_p * sh.mass[cut ? k_bin + 1 : kBins] * (1.f + off);
+      const unsigned long long at_lo = __ballot(im * (1.f + off) >= lo), at_hi = __ballot(im * (1.f - off) >= hi);  // the masses ascend
+      if (lane == 0 && at_lo != 0ull) atomicMin(&sh.p_lo, tid + __ffsll((long long)at_lo) - 1);
+      if (lane == 0 && at_hi != 0ull) atomicMin(&sh.p_hi, tid + __ffsll((long long)at_hi) - 1);
       __syncthreads();
       p_hi = min(sh.p_hi, cut ? k_bin : kBins - 1);
       p_lo = min(sh.p_lo, p_hi);
@@ -628,16 +699,16 @@ __device__ __forceinline__ RowCut cut_row(const SampleWs& ws, int r, const RowPa
   }
   const int sure_bin = min(k_bin, p_lo);
   if (sure_bin >= kBins) return c;
-  const float sure = sure_bin > 0 ? bin_end(first, sure_bin - 1, per_unit) : INFINITY;
-  if (c.least >= sure) return c;  // min_p ends above: nothing else matters
+  const float sure = sure_bin > 0 ? first - (float)(sure_bin - 1) : INFINITY;  // floor(t) >= n <=> t >= n
+  if (c.least * per_unit >= sure) return c;                                    // min_p ends above: nothing else matters
   c.ends = 1;
   c.sure = sure;
   c.count_sure = sh.count[sure_bin];
-  c.p_low = bin_end(first, p_lo < kBins ? p_hi : k_bin, per_unit);
+  c.p_low = first - (float)(p_lo < kBins ? p_hi : k_bin);
   c.apart = p_lo < kBins && k_bin < kBins && k_bin > p_hi;
   if (c.apart) {
-    c.k_high = bin_end(first, k_bin - 1, per_unit);
-    c.k_low = bin_end(first, k_bin, per_unit);
+    c.k_high = first - (float)(k_bin - 1);
+    c.k_low = first - (float)k_bin;
     c.count_k = sh.count[k_bin];
   }
   return c;
@@ -666,50 +737,54 @@ __global__ __launch_bounds__(kScanThreads) void sample_cut_kernel(const SampleAr
   __shared__ uint64_t middle_sh[kScanThreads / 64];
   __shared__ uint32_t listed;
   const int slice = blockIdx.x, r = blockIdx.y, row = row0 + r, tid = threadIdx.x;
-  if (a.masked != nullptr && a.masked[row] == 0) return;
   const RowParams p = row_params(a, row);
+  if (a.masked != nullptr && a.masked[row] == 0) return;
   if (!(p.temperature > 0.f) && slice > 0) return;
-  const T* z = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
-  const int c0 = slice * (SLICE / E) + tid, n_chunks = (a.vocab + E - 1) / E;
-  Chunk<T> x[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) load_chunk(x[i], z, min(c0 + i * kScanThreads, n_chunks), a.vocab);
+  const int c0 = slice * (SLICE / E) + tid;
+  Chunks<T, N> chunks;
+  chunks.load(static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride, c0, kScanThreads, a.vocab);
   if (tid == 0) listed = 0;
   const RowCut c = cut_row(ws, r, p, sh);
   if (slice == 0 && tid == 0) ws.cut[r] = c;
   if (c.way != kDraw) return;  // uniform over the workgroup
   __syncthreads();
   const Scale s = scale_of(p.temperature);
-  const float from = fmaxf(c.sure, c.least);
   uint64_t* list = ws.list + ((int64_t)r * ws.slices + slice) * kSliceList;
   float middle = 0.f;
+  chunks.each([&](int i, const Chunk<T>& x) {
+    const int chunk = c0 + i * kScanThreads, seg = chunk / kSegChunks;
+    uint32_t sure = 0, hits = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int chunk = c0 + i * kScanThreads;
-    bool any = false;
-#pragma unroll
-    for (int e = 0; e < E; ++e) any |= x[i].z[e] >= from;
+    for (int e = 0; e < E; ++e) {
+      const float t = x.z[e] * c.per_unit;
+      sure |= t >= c.sure && x.z[e] >= c.least ? 1u << e : 0u;
+      hits |= (t >= c.p_low && t < c.sure) || (t >= c.k_low && t < c.k_high) ? 1u << e : 0u;
+    }
     uint64_t m = 0;
-    if (__ballot(any) != 0ull) {
+    if (__ballot(sure != 0u) != 0ull) {
       float w = 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) w += x[i].z[e] >= from ? weight<BF16>(x[i].z[e], c.top, s) : 0.f;
+      for (int e = 0; e < E; ++e) w += (sure >> e) & 1u ? weight<BF16>(x.z[e], c.top, s) : 0.f;
       m = wave_mass_sum(mass_of(w));
     }
-    const int seg = chunk / kSegChunks;
     if ((tid & 63) == 0 && seg < ws.segs) ws.seg[(int64_t)r * ws.segs + seg] = m;
-    if (c.ends) {
+    if (hits != 0u) {
+      uint32_t at = atomicAdd(&listed, (uint32_t)__popc(hits));
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if ((hits >> e) & 1u) {
+          if (at < (uint32_t)kSliceList) list[at] = order_of(key_of(x.z[e]), chunk * E + e);
+          ++at;
+        }
+    }
+    if (c.apart) {  // uniform over the workgroup
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const float v = x[i].z[e];
-        if ((v >= c.p_low && v < c.sure) || (v >= c.k_low && v < c.k_high)) {
-          const uint32_t at = atomicAdd(&listed, 1u);
-          if (at < (uint32_t)kSliceList) list[at] = order_of(key_of(v), chunk * E + e);
-        }
-        if (c.apart && v < c.p_low && v >= c.k_high) middle += weight<BF16>(v, c.top, s);
+        const float t = x.z[e] * c.per_unit;
+        if (t >= c.k_high && t < c.p_low) middle += weight<BF16>(x.z[e], c.top, s);
       }
     }
-  }
+  });
   if (c.ends) {  // (a float per thread, which its tokens enter in order; whole numbers from there on)
     uint64_t m = wave_mass_sum(mass_of(middle));
     if ((tid & 63) == 0) middle_sh[tid >> 6] = m;
@@ -723,28 +798,110 @@ __global__ __launch_bounds__(kScanThreads) void sample_cut_kernel(const SampleAr
   }
 }
 
-// sorts list[0, pad) in ascending order; pad a power of two up to 2 * kRowThreads * 2.  Pairs up to 64 apart are a wavefront's own.
-__device__ __forceinline__ void sort_list(unsigned long long* list, int pad) {
-  const int tid = threadIdx.x;
-  for (int size = 2; size <= pad; size <<= 1)
-    for (int step = size >> 1; step > 0; step >>= 1) {
-      if (step > 64) __syncthreads();
-      for (int i = tid; i < pad / 2; i += kRowThreads) {
-        const int lo = 2 * i - (i & (step - 1)), hi = lo + step;
-        const unsigned long long x = list[lo], y = list[hi];
-        if ((x > y) == ((lo & size) == 0)) {
-          list[lo] = y;
-          list[hi] = x;
-        }
+// The end of a prefix of the order.  Every thread holds some tokens: order (order_of) and mass.  Kept are the tokens for which what lies in
+// front of them is below a limit: their number, or their mass.  The last one kept is found by narrowing: a histogram of 128 bins over
+// what is left of the order, and the last bin that begins below the limit is what is left.  Tokens of one logit part by their ids, the
+// lower bits of the order.  A round narrows 64 bits by seven; two to four of them are usual.  Eight copies of the bins: tokens of
+// one logit would otherwise queue for one address, 64 of a wavefront at a time (1024 bins, one copy: 36 us for 64 rows of 126464 bf16
+// logits; sorting the list instead: 18).
+constexpr int kNarrowBins = 128, kNarrowCopies = 8;
+struct NarrowShared {
+  unsigned long long mass[kNarrowCopies][kNarrowBins];
+  uint32_t count[kNarrowCopies][kNarrowBins];
+  uint64_t wave_lo[kRowThreads / 64], wave_hi[kRowThreads / 64];
+  int bin;
+  uint64_t front_mass;
+  uint32_t front_count;
+};
+struct End {
+  uint64_t last;  // 0: nothing is kept
+  uint64_t mass;  // of what is kept
+};
+template <int RUN>
+__device__ __forceinline__ End find_end(const uint64_t (&order)[RUN], const uint64_t (&m)[RUN], uint32_t alive, bool by_count, uint32_t count, uint32_t most,
+                                        uint64_t base, double limit, NarrowShared& sh) {
+  static_assert(kNarrowBins * kNarrowCopies == kRowThreads && kNarrowBins == 2 * kWave, "a cell a thread, two bins a lane");
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, copy = tid & (kNarrowCopies - 1);
+  constexpr int kWaves = kRowThreads / 64;
+  uint64_t front = 0;
+  if (by_count ? count >= most : !((double)base < limit)) return End{0, 0};
+  for (;;) {
+    uint64_t lo = ~(uint64_t)0, hi = 0;
+#pragma unroll
+    for (int u = 0; u < RUN; ++u)
+      if ((alive >> u) & 1u) {
+        lo = order[u] < lo ? order[u] : lo;
+        hi = order[u] > hi ? order[u] : hi;
       }
-      if (step > 64)
-        __syncthreads();
-      else
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (__ballot(alive != 0u) != 0ull) {
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        const uint64_t l = shfl_xor64(lo, o), h = shfl_xor64(hi, o);
+        lo = l < lo ? l : lo;
+        hi = h > hi ? h : hi;
+      }
     }
-  __syncthreads();
+    (&sh.mass[0][0])[tid] = 0;
+    (&sh.count[0][0])[tid] = 0;
+    if (lane == 0) {
+      sh.wave_lo[wave] = lo;
+      sh.wave_hi[wave] = hi;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      lo = sh.wave_lo[w] < lo ? sh.wave_lo[w] : lo;
+      hi = sh.wave_hi[w] > hi ? sh.wave_hi[w] : hi;
+    }
+    if (lo > hi) return End{0, 0};  // (no token at all)
+    const int shift = max(0, 64 - __clzll((long long)((hi - lo) | 1ull)) - 7);
+#pragma unroll
+    for (int u = 0; u < RUN; ++u)
+      if ((alive >> u) & 1u) {
+        const int b = (int)((order[u] - lo) >> shift);
+        atomicAdd(&sh.mass[copy][b], (unsigned long long)m[u]);
+        atomicAdd(&sh.count[copy][b], 1u);
+      }
+    __syncthreads();
+    if (wave == 0) {
+      uint64_t bm[2] = {0, 0};
+      uint32_t bn[2] = {0, 0};
+#pragma unroll
+      for (int i = 0; i < kNarrowCopies; ++i)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          bm[u] += sh.mass[i][2 * lane + u];
+          bn[u] += sh.count[i][2 * lane + u];
+        }
+      uint64_t before = wave_inclusive64(bm[0] + bm[1], lane) - bm[0] - bm[1];
+      uint32_t n_before = bn[0] + bn[1];
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const uint32_t t = __shfl_up(n_before, o, kWave);
+        if (lane >= o) n_before += t;
+      }
+      n_before -= bn[0] + bn[1];
+      auto begins = [&](uint32_t c, uint64_t x) { return by_count ? count + c < most : (double)(base + front + x) < limit; };
+      const bool second = bn[1] > 0 && begins(n_before + bn[0], before + bm[0]);
+      const unsigned long long some = __ballot(second || (bn[0] > 0 && begins(n_before, before)));
+      if (lane == 63 - __clzll((long long)some)) {  // (the first token of all begins below the limit)
+        sh.bin = 2 * lane + (second ? 1 : 0);
+        sh.front_mass = before + (second ? bm[0] : 0) + (lo == hi ? bm[second ? 1 : 0] : 0);
+        sh.front_count = n_before + (second ? bn[0] : 0);
+      }
+    }
+    __syncthreads();
+    front += sh.front_mass;
+    if (lo == hi) return End{lo, front};  // one token is left: it is the last
+    count += sh.front_count;
+    const int bin = sh.bin;
+#pragma unroll
+    for (int u = 0; u < RUN; ++u)
+      if (((alive >> u) & 1u) && (int)((order[u] - lo) >> shift) != bin) alive &= ~(1u << u);
+  }
 }
 
+constexpr int kRankMost = 512;  // tokens that are ranked each against every other
 constexpr int kMaxSegs = kSampleMaxVocab / (kSegChunks * 4);
 template <class T>
 __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleArgs a, const SampleWs ws, int row0) {
@@ -753,8 +910,13 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
   __shared__ unsigned long long list[kRowList];
   __shared__ unsigned long long seg[kMaxSegs];
   __shared__ uint64_t sum_a[kWaves], sum_b[kWaves], wave_mass[kWaves];
-  __shared__ int found, n_kept;
-  __shared__ uint64_t found_base;
+  __shared__ int found, n_first, n_kept;
+  __shared__ double at1_sh, atT_sh;
+  __shared__ uint64_t found_base, last_sh;
+  __shared__ unsigned long long listed_mass;
+  __shared__ uint32_t begin_sh[4 * kMaxSlices];
+  __shared__ uint64_t rank_mass[kRankMost];
+  __shared__ NarrowShared narrow;
   const int r = blockIdx.x, row = row0 + r, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (a.masked != nullptr && a.masked[row] == 0) {
     if (tid == 0) write_row(a, row, -1, 0.f, 0.f);
@@ -762,8 +924,26 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
   }
   const RowParams p = row_params(a, row);
   const RowCut c = ws.cut[r];
-  if (c.way == kNone || c.way == kFirst) {
-    if (tid == 0) write_row(a, row, c.way == kNone ? -1 : c.first_id, c.way == kNone ? 0.f : (float)(1.0 / c.at1), c.way == kNone ? 0.f : 1.f);
+  if (c.way == kNone) {
+    if (tid == 0) write_row(a, row, -1, 0.f, 0.f);
+    return;
+  }
+  if (wave == kWaves - 1) {  // the sums of the weights over the slices, beside what the others do
+    double at1 = 0.0, atT = 0.0;
+    for (int i = lane; i < ws.slices; i += kWave) {
+      const SliceStat t = ws.stat[(int64_t)r * ws.slices + i];
+      if (t.top > -INFINITY) {
+        const double down = (double)t.top - (double)c.top;
+        at1 += t.at1 * exp(down);
+        atT += t.atT * exp(down / (double)p.temperature);
+      }
+    }
+    at1_sh = wave_sum(at1);
+    atT_sh = wave_sum(atT);
+  }
+  if (c.way == kFirst) {
+    __syncthreads();
+    if (tid == 0) write_row(a, row, c.first_id, (float)(1.0 / at1_sh), 1.f);
     return;
   }
   const Scale s = scale_of(p.temperature);
@@ -772,87 +952,141 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
   bool slow = c.way == kSearch;
   if (!slow) {
     for (int i = tid; i < ws.segs; i += kRowThreads) seg[i] = ws.seg[(int64_t)r * ws.segs + i];
-    if (c.ends)
-      for (int i = 0; i < ws.slices; ++i) {  // the slices' lists one behind the other
-        const uint32_t k = ws.listed[(int64_t)r * ws.slices + i];
-        slow = slow || k > (uint32_t)kSliceList || n + k > (uint32_t)kRowList;
-        if (slow) break;
-        for (uint32_t j = tid; j < k; j += kRowThreads) list[n + j] = ws.list[((int64_t)r * ws.slices + i) * kSliceList + j];
-        n += k;
-        middle += ws.middle[(int64_t)r * ws.slices + i];
+    if (c.ends) {  // the slices' lists one behind the other: where each begins, then their entries
+      for (int i0 = 0; i0 < ws.slices; i0 += kWave) {  // (every wavefront)
+        const int i = min(i0 + lane, ws.slices - 1);
+        uint32_t k = ws.listed[(int64_t)r * ws.slices + i];
+        uint64_t mid = ws.middle[(int64_t)r * ws.slices + i];
+        if (i0 + lane >= ws.slices) {
+          k = 0;
+          mid = 0;
+        }
+        slow = slow || __ballot(k > (uint32_t)kSliceList) != 0ull;
+        uint32_t upto = k;
+#pragma unroll
+        for (int o = 1; o < kWave; o <<= 1) {
+          const uint32_t t = __shfl_up(upto, o, kWave);
+          if (lane >= o) upto += t;
+        }
+        if (wave == 0 && i0 + lane < ws.slices) begin_sh[i0 + lane] = n + upto - k;
+        n += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) mid += shfl_xor64(mid, o);
+        middle += mid;
       }
+      slow = slow || n > (uint32_t)kRowList;
+      __syncthreads();
+      for (uint32_t j = tid; !slow && j < n; j += kRowThreads) {
+        int lo = 0, hi = ws.slices - 1;  // the last slice that begins at or in front of j
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) >> 1;
+          if (begin_sh[mid] <= j)
+            lo = mid;
+          else
+            hi = mid - 1;
+        }
+        list[j] = ws.list[((int64_t)r * ws.slices + lo) * kSliceList + (j - begin_sh[lo])];
+      }
+    }
   }
   if (slow) {  // uniform over the workgroup
     search_row<T>(a, row, sum_a, sum_b, wave_mass, &found);
     return;
   }
   uint64_t last = 0;  // the last token kept, if the list decides that
+  if (tid == 0) {
+    n_first = n_kept = 0;
+    listed_mass = 0;
+    last_sh = 0;
+  }
+  __syncthreads();
   if (c.ends) {
-    int pad = 1;
-    while (pad < (int)n) pad <<= 1;
-    for (int i = (int)n + tid; i < pad; i += kRowThreads) list[i] = ~0ull;
-    if (tid == 0) n_kept = 0;
-    __syncthreads();
-    sort_list(list, pad);
-    // the list's masses, a run of it for each thread, and that of everything above it
-    uint64_t m[RUN], mine = 0, sure = 0, first_part = 0, upto = 0;
-    const int j0 = tid * RUN;
-    const uint32_t p_low = key_of(c.p_low);
-    int n_first = (int)n;  // of [p_low, sure); behind them where top_k ends
-    if (c.apart) {
-      int lo = 0, hi = (int)n;
-      while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (key_in(list[mid]) >= p_low)
-          lo = mid + 1;
-        else
-          hi = mid;
-      }
-      n_first = lo;
-    }
-    auto in_front = [&](int j) { return (j < n_first ? c.count_sure : c.count_k - (uint32_t)n_first) + (uint32_t)j; };  // tokens above the j-th entry
-#pragma unroll
-    for (int u = 0; u < RUN; ++u) {
-      const int j = j0 + u;
-      m[u] = j < (int)n ? mass<BF16>(of_key(key_in(list[j])), c.top, s) : 0;
-      mine += m[u];
-      if (j < n_first) first_part += m[u];
-      if (j < (int)n && (!c.apart || j >= n_first) && in_front(j) < (uint32_t)p.top_k) upto += m[u];
-    }
+    uint64_t sure = 0;
     for (int i = tid; i < ws.segs; i += kRowThreads) sure += seg[i];
     sure = block_reduce64<kRowThreads>(sure, sum_a, Add64());
-    double target = INFINITY;
-    if (p.top_p < 1.f) {
-      double all = c.atT / kMassUnit;
-      const bool cut = p.top_k > 0 && (c.apart || c.count_sure + n >= (uint32_t)p.top_k);  // the mass of the first top_k
-      if (cut) {
-        if (c.apart) upto += first_part;
-        all = (double)(sure + middle + block_reduce64<kRowThreads>(upto, sum_b, Add64()));
+    const uint32_t k = (uint32_t)p.top_k;
+    const bool cut = p.top_k > 0 && (c.apart || c.count_sure + n >= k);  // top_k ends in the list
+    const uint64_t least = order_of(c.least_key, -1);                    // the last that min_p leaves
+    auto in_first = [&](uint64_t order) { return !c.apart || of_key(key_in(order)) * c.per_unit >= c.p_low; };  // of [p_low, sure)
+    if (n <= (uint32_t)kRankMost) {  // every token against every other
+      int group = kRowThreads;       // threads per token
+      while (group > 64 || (uint32_t)(kRowThreads / group) < n) group >>= 1;
+      const int e = tid / group;
+      const bool live = e < (int)n, lead = live && (tid & (group - 1)) == 0;
+      if (tid < (int)n) {
+        rank_mass[tid] = mass<BF16>(of_key(key_in(list[tid])), c.top, s);
+        const unsigned long long firsts = __ballot(in_first(list[tid]));
+        if (lane == 0) atomicAdd(&n_first, (int)__popcll(firsts));
       }
-      target = (double)p.top_p * all;
-    }
-    uint64_t front = wave_inclusive64(mine, lane);
-    if (lane == 63) wave_mass[wave] = front;
-    __syncthreads();
-    front += sure - mine;
-    for (int w = 0; w < wave; ++w) front += wave_mass[w];
-    int mine_kept = 0;
-#pragma unroll
-    for (int u = 0; u < RUN; ++u) {
-      const int j = j0 + u;
-      if (j < n_first) {
-        const bool in_k = p.top_k <= 0 || in_front(j) < (uint32_t)p.top_k, in_p = (double)front < target;
-        if (in_front(j) == 0 || (in_k && in_p && key_in(list[j]) >= c.least_key)) mine_kept = j + 1;
+      __syncthreads();
+      const uint64_t order = live ? list[e] : 0;
+      uint64_t front = 0;
+      uint32_t rank = 0;
+      for (uint32_t j = tid & (group - 1); j < n; j += group) {
+        const uint64_t other = list[j], m = rank_mass[j];
+        if (other < order) {
+          ++rank;
+          front += m;
+        }
       }
-      front += m[u];
-    }
-    if (mine_kept > 0) atomicMax(&n_kept, mine_kept);
-    __syncthreads();
-    const int kept = n_kept;  // a prefix
-    if (kept > 0) last = list[kept - 1];
+      for (int o = 1; o < group; o <<= 1) {
+        rank += __shfl_xor(rank, o, kWave);
+        front += shfl_xor64(front, o);
+      }
+      const uint64_t m = lead ? rank_mass[e] : 0;
+      const bool first = lead && in_first(order);
+      const uint32_t in_front = rank < (uint32_t)n_first ? c.count_sure + rank : c.count_k + rank - (uint32_t)n_first;
+      if (cut && p.top_p < 1.f) {  // the mass of the first top_k
+        const bool in_k = lead && in_front < k;
+        if (__ballot(in_k) != 0ull) {
+          uint64_t t = in_k ? m : 0;
 #pragma unroll
-    for (int u = 0; u < RUN; ++u)
-      if (j0 + u < kept) atomicAdd(&seg[(int)(uint32_t)list[j0 + u] / (E * kSegChunks)], (unsigned long long)m[u]);
+          for (int o = 32; o > 0; o >>= 1) t += shfl_xor64(t, o);
+          if (lane == 0) atomicAdd(&listed_mass, (unsigned long long)t);
+        }
+        __syncthreads();
+      }
+      const double target = p.top_p < 1.f ? (double)p.top_p * (cut ? (double)(sure + middle + listed_mass) : atT_sh / kMassUnit) : INFINITY;
+      const bool kept = first && (!cut || in_front < k) && (double)(sure + front) < target && order <= least;
+      const unsigned long long some = __ballot(kept);
+      if (some != 0ull && lane == 0) atomicAdd(&n_kept, (int)__popcll(some));
+      if (kept) atomicAdd(&seg[(int)(uint32_t)order / (E * kSegChunks)], (unsigned long long)m);
+      __syncthreads();
+      if (kept && (int)rank == n_kept - 1) last_sh = order;  // a prefix
+      __syncthreads();
+      last = last_sh;
+    } else {
+      uint64_t order[RUN], m[RUN], first_part = 0;
+      uint32_t first = 0, second = 0;
+#pragma unroll
+      for (int u = 0; u < RUN; ++u) {
+        const int j = tid + u * kRowThreads;
+        order[u] = j < (int)n ? list[j] : 0;
+        m[u] = j < (int)n ? mass<BF16>(of_key(key_in(order[u])), c.top, s) : 0;
+        if (j < (int)n) {
+          if (in_first(order[u])) {
+            first |= 1u << u;
+            first_part += m[u];
+          } else {
+            second |= 1u << u;
+          }
+        }
+      }
+      End end{0, 0};
+      if (cut) end = find_end<RUN>(order, m, c.apart ? second : first, true, c.apart ? c.count_k : c.count_sure, k, 0, 0.0, narrow);
+      if (p.top_p < 1.f) {
+        double all = atT_sh / kMassUnit;
+        if (cut) {
+          all = (double)(sure + middle + end.mass);
+          if (c.apart) all += (double)block_reduce64<kRowThreads>(first_part, sum_b, Add64());
+        }
+        end = find_end<RUN>(order, m, first, false, 0, 0, sure, (double)p.top_p * all, narrow);
+      }
+      last = end.last < least ? end.last : least;
+#pragma unroll
+      for (int u = 0; u < RUN; ++u)
+        if (((first >> u) & 1u) && order[u] <= last) atomicAdd(&seg[(int)(uint32_t)order[u] / (E * kSegChunks)], (unsigned long long)m[u]);
+    }
   }
   if (tid == 0) found = -1;
   __syncthreads();
@@ -886,13 +1120,12 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
   const int chunk = found * kSegChunks + lane, n_chunks = (a.vocab + E - 1) / E;
   Chunk<T> x;
   load_chunk(x, z, min(chunk, n_chunks), a.vocab);
-  const float from = fmaxf(c.sure, c.least);
   uint64_t end[E], extra = 0;  // masses up to each token of the chunk: the sum of the sure ones, as in the second launch, and the listed ones
   float w = 0.f;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const float v = x.z[e];
-    if (v >= from)
+    if (v * c.per_unit >= c.sure && v >= c.least)
       w += weight<BF16>(v, c.top, s);
     else if (c.ends && order_of(key_of(v), chunk * E + e) <= last)
       extra += mass<BF16>(v, c.top, s);
@@ -903,7 +1136,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
   for (int e = 0; e < E; ++e) {
     if (here(before + (e > 0 ? end[e > 0 ? e - 1 : 0] : 0), before + end[e])) {
       const float v = x.z[e];
-      write_row(a, row, chunk * E + e, (float)((double)weight<BF16>(v, c.top, scale_of(1.f)) / c.at1),
+      write_row(a, row, chunk * E + e, (float)((double)weight<BF16>(v, c.top, scale_of(1.f)) / at1_sh),
                 (float)((double)weight<BF16>(v, c.top, s) / ((double)total * kMassUnit)));
     }
   }
