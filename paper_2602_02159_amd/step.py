@@ -201,11 +201,18 @@ class FocusDecoder:
                     probe layer   focus_probe_layer (dense attention + I_sink)
                     sparse layer  focus_update_sparse_layer with the K_bar cached at the block entry -> out[l], kept[l], scores[l]
     `row_base` is the cache row of position 0 of the generation block.
+
+    `quantised`: the caches of all layers but the probe layer, whose logits choose the sinks of the others, hold eight-bit rows
+    (uint8 k_cache[l] / v_cache[l] with k_exp[l] / v_exp[l]); the entry then is focus_refresh_attn and focus_quant_refresh, a step's layers are
+    focus_quant_update and focus_quant_attn (every block kept) or focus_quant_layer.  read_cache(l) gives such rows back as bf16.
+    `sample` (with vocab): the step draws its tokens, focus_sample_tokens in the place of focus_token_confidence, from uniform [n_gen] with
+    temperature, top_k, top_p, min_p [n_gen], which the caller fills (1, 0, 1, 0 at first) -> tokens, conf, prob.
     """
 
     def __init__(self, n_layers: int, l_dense: int, dense_tail: int, n_heads: int, head_dim: int, n_ctx: int, n_resp: int,
                  n_gen: int, row_base: int, block: int, k_focus: int, window: int, n_keep: int, n_sink: int, device,
-                 vocab: int | None = None):
+                 vocab: int | None = None, quantised: bool = False, sample: bool = False):
+        assert vocab is not None or not sample
         assert 0 <= l_dense < n_layers and 0 <= dense_tail <= n_layers - l_dense - 1
         self.n_layers, self.l_dense, self.first_tail = n_layers, l_dense, n_layers - dense_tail
         H, d, L = n_heads, head_dim, n_ctx + n_resp
@@ -215,16 +222,24 @@ class FocusDecoder:
         dev = device
         bf = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16, device=dev)
         i32 = lambda n: torch.full((max(n, 1),), -1, dtype=torch.int32, device=dev)
-        self.k_cache = [bf(H, L, d) for _ in range(n_layers)]
-        self.v_cache = [bf(H, L, d) for _ in range(n_layers)]
+        self.quantised = [quantised and l != l_dense for l in range(n_layers)]
+        u8 = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=dev)
+        self.k_cache, self.v_cache = ([(u8 if quant else bf)(H, L, d) for quant in self.quantised] for _ in range(2))
+        self.k_exp, self.v_exp = ([u8(H, L) if quant else None for quant in self.quantised] for _ in range(2))
+        self.caches = [fb.make_quant_cache(*t) if quant else None
+                       for quant, *t in zip(self.quantised, self.k_cache, self.v_cache, self.k_exp, self.v_exp)]
         self.kbar = [torch.zeros((H, self.n_b, d), dtype=torch.float32, device=dev) if self.is_sparse(l) else None
                      for l in range(n_layers)]
         self.q_all, self.k_all, self.v_all = ([bf(H, L, d) for _ in range(n_layers)] for _ in range(3))
         self.out_all = [bf(H, L, d) for _ in range(n_layers)]
         self.conf = torch.zeros(n_gen, dtype=torch.float32, device=dev)
         self.masked = torch.ones(n_gen, dtype=torch.uint8, device=dev)
-        self.logits = None if vocab is None else torch.zeros((n_gen, vocab), dtype=torch.bfloat16, device=dev)
+        self.logits = None if vocab is None else torch.zeros((n_gen, (vocab + 7) // 8 * 8), dtype=torch.bfloat16, device=dev)[:, :vocab]  # aligned rows
         self.tokens = i32(n_gen)
+        if sample:
+            f32 = lambda value: torch.full((n_gen,), value, dtype=torch.float32, device=dev)
+            self.uniform, self.temperature, self.top_p, self.min_p, self.prob = f32(0.0), f32(1.0), f32(1.0), f32(0.0), f32(0.0)
+            self.top_k = torch.zeros(n_gen, dtype=torch.int32, device=dev)
         self.q = [bf(H, n_gen, d) for _ in range(n_layers)]
         self.k_new = [bf(H, self.max_active, d) for _ in range(n_layers)]
         self.v_new = [bf(H, self.max_active, d) for _ in range(n_layers)]
@@ -251,10 +266,23 @@ class FocusDecoder:
         self.entry_calls, self.step_calls = [], []
         for l in range(n_layers):
             s_all = shape(self.q_all[l], self.k_cache[l], self.v_cache[l], self.out_all[l])
+            if self.quantised[l]:
+                s_new = shape(self.q_all[l], self.k_all[l], self.v_all[l], self.out_all[l])
+                self.entry_calls.append((lib.focus_quant_refresh, (
+                    C.byref(self.caches[l]), C.byref(s_all), p(self.k_all[l]), p(self.v_all[l]), self.k_all[l].stride(0), self.k_all[l].stride(1),
+                    p(self.kbar[l]))))
+                self.entry_calls.append((lib.focus_refresh_attn, (
+                    p(self.q_all[l]), p(self.k_all[l]), p(self.v_all[l]), C.byref(s_new), p(self.out_all[l]), None)))
+                continue
             self.entry_calls.append((lib.focus_block_entry, (
                 p(self.k_cache[l]), p(self.v_cache[l]), C.byref(s_all), p(self.q_all[l]), p(self.k_all[l]), p(self.v_all[l]),
                 self.k_all[l].stride(0), self.k_all[l].stride(1), p(self.kbar[l]), p(self.out_all[l]), None)))
-        if self.logits is not None:
+        if sample:
+            ws_sample = workspace(fb.sample_tokens_workspace(n_gen, vocab))
+            self.step_calls.append((lib.focus_sample_tokens, (
+                p(self.logits), 0, self.logits.stride(0), p(self.masked), p(self.uniform), p(self.temperature), p(self.top_k), p(self.top_p),
+                p(self.min_p), n_gen, vocab, p(self.tokens), p(self.conf), p(self.prob), p(ws_sample), ws_sample.numel())))
+        elif self.logits is not None:
             ws_conf = workspace(fb.token_confidence_workspace(n_gen, vocab))
             self.step_calls.append((lib.focus_token_confidence, (
                 p(self.logits), self.logits.stride(0), p(self.masked), n_gen, vocab, p(self.tokens), p(self.conf), p(ws_conf),
@@ -264,6 +292,9 @@ class FocusDecoder:
             p(self.counts))))
         for l in range(n_layers):
             s = shape(self.q[l], self.k_cache[l], self.v_cache[l], self.out[l])
+            if self.quantised[l]:
+                self.step_calls += self._quantised_layer(l, s, k_focus, n_keep, n_sink, row_base, workspace, p)
+                continue
             if not self.is_sparse(l):
                 self.step_calls.append((lib.focus_cache_update, (
                     p(self.k_cache[l]), p(self.v_cache[l]), C.byref(s), p(self.k_new[l]), p(self.v_new[l]), self.k_new[l].stride(0),
@@ -286,6 +317,31 @@ class FocusDecoder:
                     p(self.q[l]), p(self.active_idx), p(self.counts), self.max_active, p(self.k_cache[l]), p(self.v_cache[l]),
                     C.byref(s), p(self.all_blocks), self.n_b, None, 0, p(self.out[l]), None, p(ws), ws.numel())))
         self._g_entry = self._g_step = None
+
+    def _quantised_layer(self, l, s, k_focus, n_keep, n_sink, row_base, workspace, p):
+        lib, cache = fb.lib(), C.byref(self.caches[l])
+        calls = [(lib.focus_quant_update, (
+            cache, C.byref(s), p(self.k_new[l]), p(self.v_new[l]), self.k_new[l].stride(0), self.k_new[l].stride(1), p(self.active_idx),
+            p(self.counts), self.max_active, row_base))]
+        if self.is_sparse(l):
+            ws = workspace(fb.workspace_bytes(fb.FN_QUANT_LAYER, s, self.max_active, n_keep, n_sink))
+            calls.append((lib.focus_quant_layer, (
+                p(self.q[l]), p(self.focus_idx), p(self.active_idx), p(self.counts), k_focus, self.max_active, cache, p(self.kbar[l]), C.byref(s),
+                n_keep, p(self.sink_idx), n_sink, p(self.scores[l]), p(self.kept[l]), p(self.out[l]), None, p(ws), ws.numel())))
+        else:
+            ws = workspace(fb.workspace_bytes(fb.FN_QUANT_ATTN, s, self.max_active, self.n_b, 0))
+            calls.append((lib.focus_quant_attn, (
+                p(self.q[l]), p(self.active_idx), p(self.counts), self.max_active, cache, C.byref(s), p(self.all_blocks), self.n_b, None, 0,
+                p(self.out[l]), None, p(ws), ws.numel())))
+        return calls
+
+    def read_cache(self, l: int):
+        """K and V of layer l as bf16 [H, M+N, d]: the caches themselves, or new tensors with what quantised ones read back as."""
+        if not self.quantised[l]:
+            return self.k_cache[l], self.v_cache[l]
+        k, v = (torch.empty(self.k_cache[l].shape, dtype=torch.bfloat16, device=self.k_cache[l].device) for _ in range(2))
+        fb.quant_read(self.caches[l], fb.make_shape(k, self.k_cache[l], self.v_cache[l], self.M, self.B), 0, k, v)
+        return k, v
 
     def is_sparse(self, l: int) -> bool:
         return self.l_dense < l < self.first_tail
