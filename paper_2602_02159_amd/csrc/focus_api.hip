@@ -96,17 +96,28 @@ SplitPlan plan_attention(const focus_shape& s, int max_active, int n_keep, int n
   return p;
 }
 
-// Over the quantised cache: up to four 16-query tiles share the widened rows.
-constexpr int kQuantGroups = 512;
+// Over the quantised cache: at most two 16-query tiles share the widened rows; more queries are groups of 32 that read a sub-tile about the
+// same time, the later ones from a cache.  (Groups of 64 hold 512 registers, one workgroup per compute unit: 64 queries, 32 heads, 32 832
+// keys 81.4 -> 96.8 us a call, 175 queries, 4 heads, 125 of 250 blocks 25.4 -> 32.6, 256 queries, 4 heads, 16 448 keys 31.4 -> 38.0.)
+// A sub-tile per wavefront where 512 workgroups give that, two per compute unit, which is what the registers allow.  Key loops at d = 128: one
+// per compute unit, whose half as many partial results outweigh its fewer requests under way (256 and 512 workgroups: 16 queries, 32 heads,
+// 32 832 keys 52.0 and 52.4 us, 16 448 keys 32.6 and 33.5; 28 queries, 32 832 keys 53.5 and 57.3; 25 queries, half of 512 blocks 38.8 and 41.8;
+// 8 heads, 28 queries, 16 448 keys 17.8 and 20.8); d = 64, and query groups, two (d = 64, 32 832 keys 41.9 and 31.7; 175 queries as above 30.1 and 25.8).
+// Rows that are read once and are more than the memory-side cache holds pass the caches by (32 heads, 32 832 keys, 16 queries 56.0 -> 53.9 us, one
+// query 54.6 -> 50.5); fewer may still be there from another call (half of 512 blocks, 139 MB, three layers in turn 41.7 -> 47.3).
+constexpr int kQuantGroups = 512, kQuantGroupsLoop = 256;
+constexpr int64_t kQuantStreamBytes = 200000000;
 SplitPlan plan_quant_attention(const focus_shape& s, int max_active, int n_keep, int n_sink) {
   SplitPlan p;
   p.q_tiles = ceil_div(max_active, kQTile);
-  p.q_tiles_per_group = p.q_tiles <= 2 ? p.q_tiles : kMaxQTilesPerGroup;
+  p.q_tiles_per_group = std::min(p.q_tiles, 2);
   p.q_groups = ceil_div(p.q_tiles, p.q_tiles_per_group);
   p.q_pad = p.q_groups * p.q_tiles_per_group * kQTile;
   p.n_sub = n_keep * ceil_div(s.block, kSubTile) + ceil_div(s.n_resp, kSubTile) + ceil_div(n_sink, kSubTile);
   plan_splits(p, s.n_heads, p.q_groups, kQuantGroups);
   p.pipelined = p.n_split * kWavesPerGroup < p.n_sub;
+  if (p.pipelined && s.head_dim == 128 && p.q_groups == 1) plan_splits(p, s.n_heads, p.q_groups, kQuantGroupsLoop);
+  p.stream = p.pipelined && p.q_groups == 1 && (int64_t)p.n_sub * kSubTile * s.n_heads * s.head_dim * 2 > kQuantStreamBytes;
   return p;
 }
 

@@ -39,6 +39,7 @@ __device__ __forceinline__ int list_index() { return (int)(blockIdx.y * kListSli
 struct SplitPlan {
   int n_sub, n_split;
   bool pipelined = false;  // attention only: wavefronts walk several sub-tiles, use the key loop
+  bool stream = false;     // attention over a quantised cache: rows pass the caches by
   int q_tiles, q_tiles_per_group, q_groups, q_pad;  // q_pad = 16 * q_tiles
 };
 

@@ -222,20 +222,29 @@ struct QuantTile {
   uint32_t e;  // exponent of row lane % 32, of K in the lower half of the wavefront, of V in the upper
 };
 
-template <int D>
+// STREAM: rows that one workgroup alone reads pass the caches by (load_stream16)
+template <bool STREAM, class V>
+__device__ __forceinline__ V load_row_piece(const uint8_t* p) {
+  return STREAM ? __builtin_nontemporal_load(reinterpret_cast<const V*>(p)) : *reinterpret_cast<const V*>(p);
+}
+template <int D, bool STREAM>
 __device__ __forceinline__ void load_codes(uint32_t (&v)[D / 64], const uint8_t* p) {
   if constexpr (D == 128) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
+    const uintx2 w = load_row_piece<STREAM, uintx2>(p);
     v[0] = w.x;
     v[1] = w.y;
   } else {
-    v[0] = *reinterpret_cast<const uint32_t*>(p);
+    v[0] = load_row_piece<STREAM, uint32_t>(p);
   }
+}
+template <bool STREAM>
+__device__ __forceinline__ uint4 load_codes16(const uint8_t* p) {
+  return __builtin_bit_cast(uint4, load_row_piece<STREAM, uintx4>(p));
 }
 
 // `exps`: the exponents of the head, of K or V by the half of the wavefront.  Requires t.vmask != 0; slots without a key read another
 // row of the key set, as in issue_subtile_part.
-template <int D>
+template <int D, bool STREAM>
 __device__ __forceinline__ void load_tile(QuantTile<D>& x, const AttnArgs& p, int64_t esn, const uint8_t* Kh, const uint8_t* Vh, const uint8_t* exps,
                                           const SubTile& t, int lane) {
   const int c = lane & 15, g = lane >> 4;
@@ -247,30 +256,32 @@ __device__ __forceinline__ void load_tile(QuantTile<D>& x, const AttnArgs& p, in
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < D / 64; ++j) x.k[i][j] = *reinterpret_cast<const uint4*>(kt + 16 * i * p.ksn + 64 * j + ko);
+      for (int j = 0; j < D / 64; ++j) x.k[i][j] = load_codes16<STREAM>(kt + 16 * i * p.ksn + 64 * j + ko);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) load_codes<D>(x.v[e], vt + (16 * (e >> 2) + (e & 3)) * p.vsn + vo);
+    for (int e = 0; e < 8; ++e) load_codes<D, STREAM>(x.v[e], vt + (16 * (e >> 2) + (e & 3)) * p.vsn + vo);
     x.e = exps[(row0 + (lane & 31)) * esn];
     return;
   }
-  const int last = 31 - __builtin_clz(t.vmask);
+  // lane i < 32 holds the row of slot i (subtile_row)
+  const int mine = t.kind == 0 ? t.row0 + min(lane & 31, 31 - __builtin_clz(t.vmask)) : __shfl(t.sink_row, lane & 31, kWave);
+  auto row = [&](int slot) __attribute__((always_inline)) { return (int64_t)__shfl(mine, slot, kWave); };
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const uint8_t* row = Kh + (int64_t)subtile_row(t, 16 * i + c, last) * p.ksn + 16 * g;
+    const uint8_t* k = Kh + row(16 * i + c) * p.ksn + 16 * g;
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) x.k[i][j] = *reinterpret_cast<const uint4*>(row + 64 * j);
+    for (int j = 0; j < D / 64; ++j) x.k[i][j] = load_codes16<STREAM>(k + 64 * j);
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) load_codes<D>(x.v[e], Vh + (int64_t)subtile_row(t, 16 * (e >> 2) + 4 * g + (e & 3), last) * p.vsn + c * (D / 16));
-  x.e = exps[(int64_t)subtile_row(t, lane & 31, last) * esn];
+  for (int e = 0; e < 8; ++e) load_codes<D, STREAM>(x.v[e], Vh + row(16 * (e >> 2) + 4 * g + (e & 3)) * p.vsn + c * (D / 16));
+  x.e = exps[(int64_t)mine * esn];
 }
 
-// MODE bit 0: Top-C in the prologue; bit 1: key loop; bits 4, 5: more than 256, 1024 blocks to rank.  NT: 16-query tiles of a query group.
+// MODE bit 0: Top-C in the prologue; bit 1: key loop; bit 3: rows pass the caches by; bits 4, 5: more than 256, 1024 blocks to rank.  NT: 16-query tiles of a query group.
 template <int D, int NT, int MODE>
-__global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void quant_attn_kernel(WIDE_FIRST_PARAMS, const QuantAttnArgs args) {
+__global__ __launch_bounds__(256, 2) void quant_attn_kernel(WIDE_FIRST_PARAMS, const QuantAttnArgs args) {
   AttnArgs p = with_first(args.a, rel_part, active_idx, Q, counts, n_b, H, max_active, args.a.n_gen, n_split, n_sub);
   p.q_groups = q_groups;
-  constexpr bool FUSED = (MODE & 1) != 0, PIPE = (MODE & 2) != 0;
+  constexpr bool FUSED = (MODE & 1) != 0, PIPE = (MODE & 2) != 0, STREAM = (MODE & 8) != 0;
   constexpr int BLOCKS = (MODE & 32) != 0 ? kFusedMaxBlocks : ((MODE & 16) != 0 ? kFusedManyBlocks : 256);
   constexpr int kKS = D / 32, kCT = D / 16;
   __shared__ __attribute__((aligned(16))) char ldsO[kWavesPerGroup * 16 * D * 4];  // the wavefronts' O tiles at the end
@@ -341,12 +352,10 @@ __global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void quant_attn_kernel(WIDE_F
   t.row0 = 0;
   t.vmask = 0u;
   t.sink_row = 0;
-  if (PIPE)
-    t = list.take();
-  else if (split * kWavesPerGroup + wave < p.n_sub)
+  if (!PIPE && split * kWavesPerGroup + wave < p.n_sub)
     t = locate_subtile(split * kWavesPerGroup + wave, lane, p.M, p.N, p.B, p.n_b, p.sub_per_block, kept_blocks, p.n_keep, p.sink_idx, p.n_sink,
                        uni.kept_bits, uni.ascending, 0, FUSED, few_sinks);
-  if (t.vmask != 0u) load_tile<D>(x, p, esn, Kh, Vh, exps, t, lane);
+  if (!PIPE && t.vmask != 0u) load_tile<D, STREAM>(x, p, esn, Kh, Vh, exps, t, lane);
   if (!FUSED) load_q();
   const int n_act = counted.n_active(p);
 #pragma unroll
@@ -423,15 +432,25 @@ __global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void quant_attn_kernel(WIDE_F
   };
   if (!PIPE) {  // one sub-tile per wavefront at most
     if (t.vmask != 0u) consume(x, t.vmask);
-  } else {  // the next sub-tile's rows travel while one is multiplied
-    QuantTile<D> y;
-    for (int i = 0; i < rounds.n_rounds; i += 2) {
-      const SubTile t1 = list.take();
-      if (t1.vmask != 0u) load_tile<D>(y, p, esn, Kh, Vh, exps, t1, lane);
+  } else {
+    // The next sub-tile's rows travel while one is multiplied.  They are requested in any case, past the end those of row 0, so that it is
+    // known how many requests lie behind the ones waited for; and in one place each, because these kernels start with a cold
+    // instruction cache.
+#pragma unroll 1
+    for (int i = -1; i < rounds.n_rounds; ++i) {
+      const SubTile next = list.take();
+      SubTile there = next;
+      if (there.vmask == 0u) {
+        there.kind = 0;
+        there.row0 = 0;
+        there.vmask = 1u;
+      }
+      QuantTile<D> y;
+      load_tile<D, STREAM>(y, p, esn, Kh, Vh, exps, there, lane);
+      __builtin_amdgcn_sched_barrier(0);
       if (t.vmask != 0u) consume(x, t.vmask);
-      t = list.take();
-      if (t.vmask != 0u) load_tile<D>(x, p, esn, Kh, Vh, exps, t, lane);
-      if (t1.vmask != 0u) consume(y, t1.vmask);
+      x = y;
+      t = next;
     }
   }
 
@@ -495,25 +514,31 @@ __global__ __launch_bounds__(256, NT == 4 ? 1 : 2) void quant_attn_kernel(WIDE_F
   hipLaunchKernelGGL(kernel, grid_list(query_group_list(p, (x).a.H)), dim3(256), 0, st, (x).a.rel_part, (x).a.active_idx, (x).a.Q, \
                      (x).a.counts, (x).a.n_b, (x).a.H, (x).a.max_active, (x).a.q_groups, (x).a.n_split, (x).a.n_sub, x)
 
+template <int D, int NT, int STREAM>
+static void launch_quant_loop(const QuantAttnArgs& x, const SplitPlan& p, bool fused, hipStream_t st) {
+  if (!fused)
+    QUANT_LAUNCH((quant_attn_kernel<D, NT, STREAM | 2>), x);
+  else if (x.a.n_b > kFusedManyBlocks)
+    QUANT_LAUNCH((quant_attn_kernel<D, NT, STREAM | 35>), x);
+  else if (x.a.n_b > 256)
+    QUANT_LAUNCH((quant_attn_kernel<D, NT, STREAM | 19>), x);
+  else
+    QUANT_LAUNCH((quant_attn_kernel<D, NT, STREAM | 3>), x);
+}
 template <int D, int NT>
 static void launch_quant_nt(const QuantAttnArgs& x, const SplitPlan& p, bool fused, hipStream_t st) {
-  const bool many = x.a.n_b > 256, most = x.a.n_b > kFusedManyBlocks;
-  if (fused && p.pipelined && most)
-    QUANT_LAUNCH((quant_attn_kernel<D, NT, 35>), x);
-  else if (fused && most)
-    QUANT_LAUNCH((quant_attn_kernel<D, NT, 33>), x);
-  else if (fused && p.pipelined && many)
-    QUANT_LAUNCH((quant_attn_kernel<D, NT, 19>), x);
-  else if (fused && many)
-    QUANT_LAUNCH((quant_attn_kernel<D, NT, 17>), x);
-  else if (fused && p.pipelined)
-    QUANT_LAUNCH((quant_attn_kernel<D, NT, 3>), x);
-  else if (fused)
-    QUANT_LAUNCH((quant_attn_kernel<D, NT, 1>), x);
+  if (p.stream)
+    launch_quant_loop<D, NT, 8>(x, p, fused, st);
   else if (p.pipelined)
-    QUANT_LAUNCH((quant_attn_kernel<D, NT, 2>), x);
-  else
+    launch_quant_loop<D, NT, 0>(x, p, fused, st);
+  else if (!fused)
     QUANT_LAUNCH((quant_attn_kernel<D, NT, 0>), x);
+  else if (x.a.n_b > kFusedManyBlocks)
+    QUANT_LAUNCH((quant_attn_kernel<D, NT, 33>), x);
+  else if (x.a.n_b > 256)
+    QUANT_LAUNCH((quant_attn_kernel<D, NT, 17>), x);
+  else
+    QUANT_LAUNCH((quant_attn_kernel<D, NT, 1>), x);
 }
 template <int D>
 static hipError_t launch_quant_t(const QuantAttnArgs& x, const SplitPlan& p, bool fused, hipStream_t st) {
@@ -521,10 +546,8 @@ static hipError_t launch_quant_t(const QuantAttnArgs& x, const SplitPlan& p, boo
   if (query_group_list(p, x.a.H) > kMaxList) return hipErrorInvalidValue;
   if (p.q_tiles_per_group == 1)
     launch_quant_nt<D, 1>(x, p, fused, st);
-  else if (p.q_tiles_per_group == 2)
-    launch_quant_nt<D, 2>(x, p, fused, st);
   else
-    launch_quant_nt<D, 4>(x, p, fused, st);
+    launch_quant_nt<D, 2>(x, p, fused, st);
   return hipGetLastError();
 }
 
