@@ -225,7 +225,7 @@ __device__ __forceinline__ uint32_t min_p_key(float min_p, double down, float to
 
 // The whole row by one workgroup that walks it as often as it takes: the order is searched bit by bit.  What is kept is
 // {key > cut} and of {key == cut} the ids up to `last_id`.  For the rows that the lists below do not hold (hundreds of microseconds).
-constexpr int kRowThreads = 1024;
+constexpr int kRowThreads = 512;
 template <class T>
 __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t* sh2, uint64_t* wave_mass, int* found) {
   constexpr int E = Chunk<T>::E;
@@ -801,10 +801,9 @@ __global__ __launch_bounds__(kScanThreads) void sample_cut_kernel(const SampleAr
 // The end of a prefix of the order.  Every thread holds some tokens: order (order_of) and mass.  Kept are the tokens for which what lies in
 // front of them is below a limit: their number, or their mass.  The last one kept is found by narrowing: a histogram of 128 bins over
 // what is left of the order, and the last bin that begins below the limit is what is left.  Tokens of one logit part by their ids, the
-// lower bits of the order.  A round narrows 64 bits by seven; two to four of them are usual.  Eight copies of the bins: tokens of
-// one logit would otherwise queue for one address, 64 of a wavefront at a time (1024 bins, one copy: 36 us for 64 rows of 126464 bf16
-// logits; sorting the list instead: 18).
-constexpr int kNarrowBins = 128, kNarrowCopies = 8;
+// lower bits of the order.  A round narrows 64 bits by seven; two to four of them are usual, 3 us each: for lists that are too long
+// to rank.  Copies of the bins: tokens of one logit would otherwise queue for one address, 64 of a wavefront at a time.
+constexpr int kNarrowBins = 128, kNarrowCopies = 4;
 struct NarrowShared {
   unsigned long long mass[kNarrowCopies][kNarrowBins];
   uint32_t count[kNarrowCopies][kNarrowBins];
@@ -901,21 +900,22 @@ __device__ __forceinline__ End find_end(const uint64_t (&order)[RUN], const uint
   }
 }
 
-constexpr int kRankMost = 512;  // tokens that are ranked each against every other
-constexpr int kMaxSegs = kSampleMaxVocab / (kSegChunks * 4);
-template <class T>
+constexpr int kRankMost = 512, kRankAhead = 8;  // tokens that are ranked each against every other; LDS reads under way
+// SEGS: the most segments of a row; fewer leave LDS for a second workgroup per compute unit.
+constexpr int kFewSegs = 1024, kMaxSegs = kSampleMaxVocab / (kSegChunks * 4);
+template <class T, int SEGS>
 __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleArgs a, const SampleWs ws, int row0) {
   constexpr int E = Chunk<T>::E, kWaves = kRowThreads / 64, RUN = kRowList / kRowThreads;
   constexpr bool BF16 = sizeof(T) == 2;
-  __shared__ unsigned long long list[kRowList];
-  __shared__ unsigned long long seg[kMaxSegs];
+  __shared__ __attribute__((aligned(16))) unsigned long long list[kRowList];
+  __shared__ unsigned long long seg[SEGS];
   __shared__ uint64_t sum_a[kWaves], sum_b[kWaves], wave_mass[kWaves];
   __shared__ int found, n_first, n_kept;
   __shared__ double at1_sh, atT_sh;
-  __shared__ uint64_t found_base, last_sh;
+  __shared__ uint64_t found_base;
   __shared__ unsigned long long listed_mass;
   __shared__ uint32_t begin_sh[4 * kMaxSlices];
-  __shared__ uint64_t rank_mass[kRankMost];
+  __shared__ uint64_t sorted[kRankMost];
   __shared__ NarrowShared narrow;
   const int r = blockIdx.x, row = row0 + r, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (a.masked != nullptr && a.masked[row] == 0) {
@@ -997,7 +997,6 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
   if (tid == 0) {
     n_first = n_kept = 0;
     listed_mass = 0;
-    last_sh = 0;
   }
   __syncthreads();
   if (c.ends) {
@@ -1008,53 +1007,46 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
     const bool cut = p.top_k > 0 && (c.apart || c.count_sure + n >= k);  // top_k ends in the list
     const uint64_t least = order_of(c.least_key, -1);                    // the last that min_p leaves
     auto in_first = [&](uint64_t order) { return !c.apart || of_key(key_in(order)) * c.per_unit >= c.p_low; };  // of [p_low, sure)
-    if (n <= (uint32_t)kRankMost) {  // every token against every other
+    if (n <= (uint32_t)kRankMost) {  // every token against every other: its place in the order; then one thread per place
       int group = kRowThreads;       // threads per token
       while (group > 64 || (uint32_t)(kRowThreads / group) < n) group >>= 1;
-      const int e = tid / group;
-      const bool live = e < (int)n, lead = live && (tid & (group - 1)) == 0;
-      if (tid < (int)n) {
-        rank_mass[tid] = mass<BF16>(of_key(key_in(list[tid])), c.top, s);
-        const unsigned long long firsts = __ballot(in_first(list[tid]));
-        if (lane == 0) atomicAdd(&n_first, (int)__popcll(firsts));
-      }
+      const int e = tid / group, unit = tid & (group - 1);
+      const int end = ((int)n + group * kRankAhead - 1) / (group * kRankAhead) * (group * kRankAhead);  // at most 1024
+      for (int j = (int)n + tid; j < end; j += kRowThreads) list[j] = ~0ull;
       __syncthreads();
-      const uint64_t order = live ? list[e] : 0;
-      uint64_t front = 0;
+      const uint64_t mine = list[min(e, kRankMost - 1)];
       uint32_t rank = 0;
-      for (uint32_t j = tid & (group - 1); j < n; j += group) {
-        const uint64_t other = list[j], m = rank_mass[j];
-        if (other < order) {
-          ++rank;
-          front += m;
-        }
-      }
-      for (int o = 1; o < group; o <<= 1) {
-        rank += __shfl_xor(rank, o, kWave);
-        front += shfl_xor64(front, o);
-      }
-      const uint64_t m = lead ? rank_mass[e] : 0;
-      const bool first = lead && in_first(order);
-      const uint32_t in_front = rank < (uint32_t)n_first ? c.count_sure + rank : c.count_k + rank - (uint32_t)n_first;
-      if (cut && p.top_p < 1.f) {  // the mass of the first top_k
-        const bool in_k = lead && in_front < k;
-        if (__ballot(in_k) != 0ull) {
-          uint64_t t = in_k ? m : 0;
+      for (int j = unit * kRankAhead; j < end; j += group * kRankAhead) {  // eight neighbours at a time
+        ulonglong2 other[kRankAhead / 2];
 #pragma unroll
-          for (int o = 32; o > 0; o >>= 1) t += shfl_xor64(t, o);
-          if (lane == 0) atomicAdd(&listed_mass, (unsigned long long)t);
-        }
-        __syncthreads();
+        for (int u = 0; u < kRankAhead / 2; ++u) other[u] = *reinterpret_cast<const ulonglong2*>(list + j + 2 * u);
+#pragma unroll
+        for (int u = 0; u < kRankAhead / 2; ++u) rank += (other[u].x < mine ? 1u : 0u) + (other[u].y < mine ? 1u : 0u);
       }
+      for (int o = 1; o < group; o <<= 1) rank += __shfl_xor(rank, o, kWave);
+      if (e < (int)n && unit == 0) sorted[rank] = mine;
+      __syncthreads();
+      const bool live = tid < (int)n;
+      const uint64_t order = live ? sorted[tid] : ~(uint64_t)0;
+      const uint64_t m = live ? mass<BF16>(of_key(key_in(order)), c.top, s) : 0;
+      const bool first = live && in_first(order);
+      const unsigned long long firsts = __ballot(first);
+      if (lane == 0 && firsts != 0ull) atomicAdd(&n_first, (int)__popcll(firsts));
+      uint64_t front = wave_inclusive64(m, lane);
+      if (lane == 63) sum_b[wave] = front;
+      __syncthreads();
+      front -= m;
+      for (int w = 0; w < wave; ++w) front += sum_b[w];
+      const uint32_t in_front = tid < n_first ? c.count_sure + (uint32_t)tid : c.count_k + (uint32_t)(tid - n_first);  // tokens above
+      if (cut && live && in_front < k && (in_front + 1 == k || tid + 1 == (int)n)) listed_mass = front + m;  // the mass of the first top_k
+      __syncthreads();
       const double target = p.top_p < 1.f ? (double)p.top_p * (cut ? (double)(sure + middle + listed_mass) : atT_sh / kMassUnit) : INFINITY;
       const bool kept = first && (!cut || in_front < k) && (double)(sure + front) < target && order <= least;
       const unsigned long long some = __ballot(kept);
       if (some != 0ull && lane == 0) atomicAdd(&n_kept, (int)__popcll(some));
       if (kept) atomicAdd(&seg[(int)(uint32_t)order / (E * kSegChunks)], (unsigned long long)m);
       __syncthreads();
-      if (kept && (int)rank == n_kept - 1) last_sh = order;  // a prefix
-      __syncthreads();
-      last = last_sh;
+      last = n_kept > 0 ? sorted[n_kept - 1] : 0;  // a prefix
     } else {
       uint64_t order[RUN], m[RUN], first_part = 0;
       uint32_t first = 0, second = 0;
@@ -1195,7 +1187,10 @@ static hipError_t launch_sample_t(const SampleArgs& a, const SamplePlan& p, char
       hipLaunchKernelGGL((sample_scan_kernel<T, kSliceSmall>), grid, block, 0, st, a, ws, row0);
       hipLaunchKernelGGL((sample_cut_kernel<T, kSliceSmall>), grid, block, 0, st, a, ws, row0);
     }
-    hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(rows), dim3(kRowThreads), 0, st, a, ws, row0);
+    if (ws.segs <= kFewSegs)
+      hipLaunchKernelGGL((sample_pick_kernel<T, kFewSegs>), dim3(rows), dim3(kRowThreads), 0, st, a, ws, row0);
+    else
+      hipLaunchKernelGGL((sample_pick_kernel<T, kMaxSegs>), dim3(rows), dim3(kRowThreads), 0, st, a, ws, row0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
