@@ -456,13 +456,20 @@ __device__ __forceinline__ uint32_t key_in(uint64_t order) { return ~(uint32_t)(
 __device__ __forceinline__ float bins_per_unit(float temperature) { return fminf(kBinsPerNat / temperature, kMostPerUnit); }
 constexpr double kMassUnit = 1.0 / (double)((uint64_t)1 << kMassBits);
 __device__ __forceinline__ bool needs_order(const RowParams& p) { return p.top_k > 0 || p.top_p < 1.f; }
+// sum over the wavefront of numbers below 2^48
+__device__ __forceinline__ uint64_t wave_mass_sum(uint64_t m) {
+  auto add = [](uint32_t x, uint32_t y) { return x + y; };
+  const uint32_t lo = wave_reduce_u32((uint32_t)m & 0xffffffu, add), hi = wave_reduce_u32((uint32_t)(m >> 24), add);
+  return ((uint64_t)hi << 24) + lo;
+}
+
 template <class T, int SLICE>
 __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleArgs a, const SampleWs ws, int row0) {
   constexpr int E = Chunk<T>::E, N = SLICE / E / kScanThreads, kCopies = 4, kWaves = kScanThreads / 64;
   constexpr bool BF16 = sizeof(T) == 2;
   __shared__ unsigned long long bins_sh[kCopies][kBins];
   __shared__ float top_sh[kWaves];
-  __shared__ double at1_sh[kWaves], atT_sh[kWaves];
+  __shared__ unsigned long long at1_sh, atT_sh;
   __shared__ int id_sh;
   const int slice = blockIdx.x, r = blockIdx.y, row = row0 + r, tid = threadIdx.x;
   const RowParams p = row_params(a, row);
@@ -475,7 +482,10 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleA
 #pragma unroll
     for (int i = 0; i < kCopies; ++i) bins_sh[i][tid] = 0;
   }
-  if (tid == 0) id_sh = 0x7fffffff;
+  if (tid == 0) {
+    id_sh = 0x7fffffff;
+    at1_sh = atT_sh = 0;
+  }
   float mine = -INFINITY;
   chunks.each([&](int, const Chunk<T>& x) {
 #pragma unroll
@@ -528,25 +538,13 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleA
       }
     }
   });
-  double d1 = (double)at1, dT = (double)atT;
-#pragma unroll 1
-  for (int o = 32; o > 0; o >>= 1) {
-    d1 += __shfl_xor(d1, o, kWave);
-    dT += __shfl_xor(dT, o, kWave);
-  }
+  const uint64_t w1 = wave_mass_sum(mass_of(at1)), wT = wave_mass_sum(mass_of(atT));  // (32 at most each: below 2^48)
   if ((tid & 63) == 0) {
-    at1_sh[tid >> 6] = d1;
-    atT_sh[tid >> 6] = dT;
+    atomicAdd(&at1_sh, (unsigned long long)w1);
+    atomicAdd(&atT_sh, (unsigned long long)wT);
   }
   __syncthreads();
-  if (tid == 0) {
-    d1 = dT = 0.0;
-    for (int w = 0; w < kWaves; ++w) {
-      d1 += at1_sh[w];
-      dT += atT_sh[w];
-    }
-    *stat = SliceStat{top, id_sh, d1, dT};
-  }
+  if (tid == 0) *stat = SliceStat{top, id_sh, (double)at1_sh * kMassUnit, (double)atT_sh * kMassUnit};
   if (order) {
     static_assert(kBins == kScanThreads, "a bin a thread");
     uint64_t v = 0;  // 16384 tokens at most: the lower half holds 16384 * 1.04 * 2^17
@@ -714,12 +712,6 @@ __device__ __forceinline__ RowCut cut_row(const SampleWs& ws, int r, const RowPa
   return c;
 }
 
-// sum over the wavefront of numbers below 2^48
-__device__ __forceinline__ uint64_t wave_mass_sum(uint64_t m) {
-  auto add = [](uint32_t x, uint32_t y) { return x + y; };
-  const uint32_t lo = wave_reduce_u32((uint32_t)m & 0xffffffu, add), hi = wave_reduce_u32((uint32_t)(m >> 24), add);
-  return ((uint64_t)hi << 24) + lo;
-}
 __device__ __forceinline__ uint64_t wave_inclusive64(uint64_t v, int lane) {
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
@@ -730,7 +722,7 @@ __device__ __forceinline__ uint64_t wave_inclusive64(uint64_t v, int lane) {
 }
 
 template <class T, int SLICE>
-__global__ __launch_bounds__(kScanThreads) void sample_cut_kernel(const SampleArgs a, const SampleWs ws, int row0) {
+__global__ __launch_bounds__(kScanThreads, 6) void sample_cut_kernel(const SampleArgs a, const SampleWs ws, int row0) {
   constexpr int E = Chunk<T>::E, N = SLICE / E / kScanThreads;
   constexpr bool BF16 = sizeof(T) == 2;
   __shared__ CutShared sh;
