@@ -126,6 +126,14 @@ def _stream() -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+def _stream_on(t: torch.Tensor) -> int:
+    """_stream() for a call on the tensor `t`: kernels run on the current device, so that is the one it has to be on."""
+    device = torch.cuda.current_device()
+    if t.get_device() != device:
+        raise ValueError(f"tensors on {t.device}, but the current device is cuda:{device}")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
 def _need(t: torch.Tensor, dtype, name: str) -> None:
     if not t.is_cuda or t.dtype != dtype:
         raise TypeError(f"{name}: expected a CUDA tensor of {dtype}, got {t.dtype} on {t.device}")
@@ -277,16 +285,22 @@ def sample_tokens(logits, masked, uniform, temperature, top_k, top_p, min_p, tok
     but uniform may be None, as may masked, conf and prob); workspace of sample_tokens_workspace() bytes."""
     if not logits.is_cuda or logits.dtype not in (torch.bfloat16, torch.float32):
         raise TypeError(f"logits: expected a CUDA tensor of bfloat16 or float32, got {logits.dtype} on {logits.device}")
-    if logits.stride(1) != 1:
-        raise ValueError("logits: innermost stride must be 1")
+    if logits.dim() != 2 or logits.stride(1) != 1:
+        raise ValueError("logits: expected [n_rows, vocab], innermost stride 1")
+    rows, vocab = logits.shape[:1], logits.shape[1]
+    stride = logits.stride(0) if rows[0] > 1 else (vocab + 7) // 8 * 8  # (of one row any will do)
     for t, dtype, name in ((uniform, torch.float32, "uniform"), (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
                            (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"), (tokens, torch.int32, "tokens"), (conf, torch.float32, "conf"),
                            (prob, torch.float32, "prob")):
         if t is not None:
             _need(t, dtype, name)
-    _check(lib().focus_sample_tokens(_ptr(logits), int(logits.dtype == torch.float32), logits.stride(0), _ptr(masked), _ptr(uniform), _ptr(temperature),
-                                     _ptr(top_k), _ptr(top_p), _ptr(min_p), logits.shape[0], logits.shape[1], _ptr(tokens), _ptr(conf), _ptr(prob),
-                                     _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+            if t.shape != rows or not t.is_contiguous():
+                raise ValueError(f"{name}: expected {rows[0]} values next to each other, got shape {tuple(t.shape)}, strides {t.stride()}")
+    if masked is not None and (masked.element_size() != 1 or masked.shape != rows or not masked.is_contiguous()):
+        raise ValueError(f"masked: expected {rows[0]} bytes, got {masked.dtype}, shape {tuple(masked.shape)}")
+    _check(lib().focus_sample_tokens(_ptr(logits), int(logits.dtype == torch.float32), stride, _ptr(masked), _ptr(uniform), _ptr(temperature),
+                                     _ptr(top_k), _ptr(top_p), _ptr(min_p), rows[0], vocab, _ptr(tokens), _ptr(conf), _ptr(prob),
+                                     _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_on(logits)))
 
 
 def cache_update(k_cache, v_cache, shape: Shape, k_new, v_new, active_idx, counts, row_base: int) -> None:
@@ -378,7 +392,7 @@ def quant_update(cache: QuantCache, shape: Shape, k_new, v_new, active_idx, coun
     if k_new.stride() != v_new.stride() or k_new.stride(2) != 1:
         raise ValueError("K_new and V_new must share their strides, innermost 1")
     _check(lib().focus_quant_update(C.byref(cache), C.byref(shape), _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _ptr(active_idx),
-                                    _ptr(counts), active_idx.numel(), row_base, _stream()))
+                                    _ptr(counts), active_idx.numel(), row_base, _stream_on(k_new)))
 
 
 def quant_refresh(cache: QuantCache, shape: Shape, k_new, v_new, kbar) -> None:
@@ -389,7 +403,7 @@ def quant_refresh(cache: QuantCache, shape: Shape, k_new, v_new, kbar) -> None:
         _need(kbar, torch.float32, "kbar")
     if k_new.stride() != v_new.stride() or k_new.stride(2) != 1:
         raise ValueError("K_new and V_new must share their strides, innermost 1")
-    _check(lib().focus_quant_refresh(C.byref(cache), C.byref(shape), _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _ptr(kbar), _stream()))
+    _check(lib().focus_quant_refresh(C.byref(cache), C.byref(shape), _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _ptr(kbar), _stream_on(k_new)))
 
 
 def quant_read(cache: QuantCache, shape: Shape, first_row: int, k_out, v_out) -> None:
@@ -399,7 +413,7 @@ def quant_read(cache: QuantCache, shape: Shape, first_row: int, k_out, v_out) ->
     if k_out.shape != v_out.shape or k_out.stride() != v_out.stride() or k_out.stride(2) != 1:
         raise ValueError("K_out and V_out must share their shape and strides, innermost 1")
     _check(lib().focus_quant_read(C.byref(cache), C.byref(shape), first_row, k_out.shape[1], _ptr(k_out), _ptr(v_out), k_out.stride(0), k_out.stride(1),
-                                  _stream()))
+                                  _stream_on(k_out)))
 
 
 def quant_attn(q, active_idx, counts, cache: QuantCache, shape: Shape, kept_blocks, n_keep: int, sink_idx, n_sink: int, out, lse, workspace) -> None:
@@ -408,7 +422,7 @@ def quant_attn(q, active_idx, counts, cache: QuantCache, shape: Shape, kept_bloc
     _need(out, torch.bfloat16, "out")
     _check(lib().focus_quant_attn(_ptr(q), _ptr(active_idx), _ptr(counts), active_idx.numel(), C.byref(cache), C.byref(shape), _ptr(kept_blocks), n_keep,
                                   _ptr(sink_idx), n_sink, _ptr(out), _ptr(lse), _ptr(workspace),
-                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_on(q)))
 
 
 def quant_layer(q, focus_idx, active_idx, counts, cache: QuantCache, kbar, shape: Shape, n_keep: int, sink_idx, n_sink: int, scores, kept_blocks, out,
@@ -419,4 +433,4 @@ def quant_layer(q, focus_idx, active_idx, counts, cache: QuantCache, kbar, shape
     _need(kbar, torch.float32, "kbar")
     _check(lib().focus_quant_layer(_ptr(q), _ptr(focus_idx), _ptr(active_idx), _ptr(counts), focus_idx.numel(), active_idx.numel(), C.byref(cache),
                                    _ptr(kbar), C.byref(shape), n_keep, _ptr(sink_idx), n_sink, _ptr(scores), _ptr(kept_blocks), _ptr(out), _ptr(lse),
-                                   _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream()))
+                                   _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_on(q)))

@@ -387,6 +387,31 @@ def test_layer_is_scores_then_attention_bit_for_bit(H, d, M, N, B, gen, n_act, k
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,M,N,B,n_act,keep,n_sink", [
+    (128, 26000, 77, 128, 16, 204, 0), (128, 26000, 0, 64, 28, 400, 3), (128, 27000, 9, 16, 3, 1640, 2), (64, 53000, 40, 256, 32, 200, 50),
+    (64, 52000, 40, 64, 7, 812, 0)])
+def test_caches_of_more_than_two_hundred_megabytes(d, M, N, B, n_act, keep, n_sink):
+    """Such rows pass the caches by.  The number of blocks passes 256 and 1024."""
+    H, n_b, some = 32, -(-M // B), [0, 17, 31]
+    c = Cache(H, M + N, d, B, M)
+    g = torch.Generator(device=DEV).manual_seed(d + B)
+    kbar = torch.empty((H, n_b, d), device=DEV)
+    k, v = (torch.randn((H, M + N, d), generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    fb.quant_refresh(c.struct, c.shape(), k, v, kbar)
+    q = torch.randn((H, 40, d), generator=g, device=DEV).to(torch.bfloat16)
+    focus, active, counts, sinks = i32(range(6)), i32(range(n_act)), i32([6, n_act]), i32(np.linspace(0, M - 1, n_sink).astype(int))
+    out, lse = torch.full((H, n_act, d), math.nan, dtype=torch.bfloat16, device=DEV), torch.full((H, n_act), math.nan, device=DEV)
+    scores, kept = torch.empty(n_b, device=DEV), i32([-7] * keep)
+    s = c.shape(q, out)
+    ws = torch.full((fb.workspace_bytes(fb.FN_QUANT_LAYER, s, n_act, keep, n_sink),), 0xcd, dtype=torch.uint8, device=DEV)
+    fb.quant_layer(q, focus, active, counts, c.struct, kbar, s, keep, sinks, n_sink, scores, kept, out, lse, ws)
+    ref = attn(c, q, active, counts, kept, sinks)
+    assert torch.equal(out, ref[0]) and torch.equal(lse, ref[1])
+    k, v = c.read()
+    check_attention(out[some], lse[some], q[some], k[some], v[some], np.arange(n_act), key_set(M, N, B, kept.tolist(), sinks.tolist()))
+
+
+@pytest.mark.gpu
 def test_rows_past_four_gigabytes():
     """One head's codes are 4.6 GB: row offsets pass 32 bits, and so do those of a row stride that is as large."""
     d, B, M = 128, 128, 36_000_000
@@ -454,3 +479,17 @@ def test_another_stream_and_a_captured_call():
         for a, b in zip(got, (out, lse, scores, kept, back)):
             assert torch.equal(a, b)
         check_attention(out, lse, q, back[0], back[1], np.arange(5, 5 + n), key_set(M, N, B, kept.tolist(), [0, 9]))
+
+
+@pytest.mark.gpu
+def test_another_device_than_the_current_one_is_refused(monkeypatch):
+    c = Cache(1, 40, 64, 8, 40)
+    s, rows = c.shape(), torch.zeros((1, 4, 64), dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    s = c.shape(rows, rows)
+    for call in (lambda: fb.quant_update(c.struct, s, rows, rows, i32(range(4)), None, 0), lambda: fb.quant_refresh(c.struct, s, rows, rows, None),
+                 lambda: fb.quant_read(c.struct, s, 0, rows, rows), lambda: fb.quant_attn(rows, i32([0]), None, c.struct, s, i32([0]), 1, None, 0, rows, None, ws),
+                 lambda: fb.quant_layer(rows, i32([0]), i32([0]), None, c.struct, rows.float(), s, 1, None, 0, None, i32([0]), rows, None, ws)):
+        with pytest.raises(ValueError, match="current device"):
+            call()

@@ -193,6 +193,18 @@ def test_large_calls(n, V, sigma):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("V,sigma,top_k,top_p", [(32003, 1.0, 12000, 0.5), (32003, 1.0, 12000, 0.999), (32003, 1.0, 0, 0.6), (20000, 0.6, 9000, 0.4),
+                                                 (126464, 1.5, 30000, 0.8), (32003, 0.02, 9000, 0.9), (126464, 0.02, 0, 0.7)])
+def test_ends_among_many_tokens_of_like_weight(V, sigma, top_k, top_p, dtype):
+    """Some hundred to some thousand tokens lie within a sixteenth of a nat of where top_k and top_p end, and those places apart or not;
+    at last all tokens of the row."""
+    z = _logits(4, V, dtype, V + top_k, sigma, peak=False)
+    check(z, np.array([0.001, 0.3, 0.7, 0.9999], dtype=np.float32), 1.0, top_k, top_p, 0.0)
+    check(z, np.array([0.2, 0.4, 0.6, 0.8], dtype=np.float32), np.array([0.5, 0.9, 1.5, 4.0], dtype=np.float32), top_k, top_p, 1e-3)
+
+
+@pytest.mark.gpu
 def test_the_greedy_token_and_confidence_are_those_of_token_confidence():
     n, V = 40, 30000
     z = _logits(n, V, torch.bfloat16, 9)
@@ -245,3 +257,30 @@ def test_captured_and_on_another_stream():
         call()
         assert all(torch.equal(a, b) for a, b in zip(got, out))
         check(t.cpu(), u.cpu().numpy(), T.cpu().numpy(), k.cpu().numpy(), p.cpu().numpy(), got=[x.cpu().numpy() for x in got])
+
+
+@pytest.mark.gpu
+def test_tensors_that_do_not_fit_the_call_are_refused(monkeypatch):
+    n, V = 4, 64
+    f32 = lambda *s: torch.zeros(s, device=DEV)
+    ok = dict(logits=torch.zeros((n, V), dtype=torch.bfloat16, device=DEV), masked=None, uniform=f32(n), temperature=None, top_k=None, top_p=None, min_p=None,
+              tokens=torch.full((n,), -7, dtype=torch.int32, device=DEV), conf=None, prob=None,
+              workspace=torch.empty(fb.sample_tokens_workspace(n, V), dtype=torch.uint8, device=DEV))
+    bad = [dict(uniform=f32(n - 1)), dict(uniform=f32(2 * n)[::2]), dict(temperature=f32(n, 1)), dict(conf=f32(n - 1)), dict(prob=f32()), dict(logits=f32(n, V, 1)),
+           dict(logits=f32(V, n).T), dict(masked=torch.ones(n, dtype=torch.int32, device=DEV)), dict(masked=torch.ones(n + 1, dtype=torch.uint8, device=DEV))]
+    for b in bad:
+        with pytest.raises(ValueError):
+            fb.sample_tokens(**{**ok, **b})
+    for b in (dict(top_k=f32(n)), dict(uniform=f32(n).double()), dict(uniform=torch.zeros(n)), dict(logits=torch.zeros((n, V), dtype=torch.float16, device=DEV))):
+        with pytest.raises(TypeError):
+            fb.sample_tokens(**{**ok, **b})
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: 1)
+        with pytest.raises(ValueError, match="current device"):
+            fb.sample_tokens(**ok)
+    assert (ok["tokens"] == -7).all()
+    fb.sample_tokens(**ok)
+    assert (ok["tokens"] == 0).all()
+    one = {**ok, "logits": f32(n, 63)[2:3].clone(), "uniform": f32(n, 3)[:1, 0], "tokens": ok["tokens"][:1].fill_(-7)}  # one row: its stride means nothing
+    fb.sample_tokens(**one)
+    assert one["tokens"].item() == 0
