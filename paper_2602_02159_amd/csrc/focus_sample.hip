@@ -170,6 +170,15 @@ struct Max64 {
   __device__ __forceinline__ uint64_t operator()(uint64_t a, uint64_t b) const { return a > b ? a : b; }
 };
 
+__device__ __forceinline__ uint64_t wave_inclusive64(uint64_t v, int lane) {
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const uint32_t lo = (uint32_t)__shfl_up((int)(uint32_t)v, o, kWave), hi = (uint32_t)__shfl_up((int)(uint32_t)(v >> 32), o, kWave);
+    if (lane >= o) v += ((uint64_t)hi << 32) | lo;
+  }
+  return v;
+}
+
 struct SampleArgs {
   const void* logits;
   int64_t row_stride;
@@ -224,7 +233,9 @@ __device__ __forceinline__ uint32_t min_p_key(float min_p, double down, float to
 }
 
 // The whole row by one workgroup that walks it as often as it takes: the order is searched bit by bit.  What is kept is
-// {key > cut} and of {key == cut} the ids up to `last_id`.  For the rows that the lists below do not hold (hundreds of microseconds).
+// {key > cut} and of {key == cut} the ids up to `last_id`.  For the rows that the lists below do not hold: logits so
+// alike that thousands lie within 1/16 of T where an end is.  A pass is bound by what one compute unit computes, so passes are what counts: bf16,
+// 126 464 logits, top_p 550 us a row, as long for 64 (one bit of the order a pass, and of the ids: 1331).
 constexpr int kRowThreads = 512;
 template <class T>
 __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t* sh2, uint64_t* wave_mass, int* found) {
@@ -235,11 +246,14 @@ __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t*
   const int n_chunks = (a.vocab + E - 1) / E;
   const RowParams p = row_params(a, row);
   auto each = [&](auto&& f) {  // f(id, logit) over the row
-    for (int ch = tid; ch < n_chunks; ch += kRowThreads) {
-      Chunk<T> x;
-      load_chunk(x, z, ch, a.vocab);
+    constexpr int kAhead = 8;
+    for (int c0 = tid; c0 < n_chunks; c0 += kAhead * kRowThreads) {
+      Chunks<T, kAhead> chunks;  // (past the row: -inf)
+      chunks.load(z, c0, kRowThreads, a.vocab);
+      chunks.each([&](int i, const Chunk<T>& x) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) f(ch * E + e, x.z[e]);
+        for (int e = 0; e < E; ++e) f((c0 + i * kRowThreads) * E + e, x.z[e]);
+      });
     }
   };
   // the first of the order
@@ -286,15 +300,35 @@ __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t*
   // kept so far: keys above `cut`, and the first `ties` tokens with it
   uint32_t cut = kKeyNone + 1u;
   uint64_t ties = ~(uint64_t)0, kept = all, count, sum;
-  auto search = [&](auto&& enough) {  // the largest key with enough(count, mass of the tokens down to it)
+  // the largest key with enough(count, mass of the tokens down to it), two bits at a time; the lower half of a bf16 number's key follows
+  // from its sign (+inf stands for a float32 that is none)
+  const bool half = BF16 && top < 3.402823466e38f;
+  auto search = [&](auto&& enough) {
     uint32_t k = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-      const uint32_t t = k | (1u << bit);
-      if (t > top_key) continue;
-      at_least(t, count, sum);
-      if (enough(count, sum)) k = t;
+    for (int bit = 30; bit >= (half ? 16 : 0); bit -= 2) {
+      uint32_t c[3] = {0, 0, 0};
+      uint64_t m[3] = {0, 0, 0};
+      each([&](int, float v) {
+        const uint32_t key = key_of(v);
+        if (key > kKeyNone && key >= k + (1u << bit)) {
+          const uint64_t w = mass<BF16>(v, top, s);
+#pragma unroll
+          for (uint32_t j = 0; j < 3; ++j) {
+            const bool in = key >= k + ((j + 1u) << bit);
+            c[j] += in ? 1 : 0;
+            m[j] += in ? w : 0;
+          }
+        }
+      });
+      uint32_t step = 0;
+#pragma unroll
+      for (uint32_t j = 0; j < 3; ++j) {  // (what is enough for one is so for those in front)
+        const uint64_t n = block_reduce64<kRowThreads>(c[j], sh, Add64()), w = block_reduce64<kRowThreads>(m[j], sh2, Add64());
+        if (enough(n, w)) step = j + 1u;
+      }
+      k += step << bit;
     }
-    return k;
+    return half && !(k & 0x80000000u) ? k | 0xffffu : k;
   };
   if (p.top_k > 0) {
     const uint64_t k = (uint64_t)p.top_k;
@@ -330,64 +364,60 @@ __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t*
     cut = m_key;
     ties = ~(uint64_t)0;
   }
-  int last_id = a.vocab;
-  if (ties != ~(uint64_t)0) {  // the largest id up to which at most `ties` tokens have the key
-    int id = -1;
-    for (int bit = 30; bit >= 0; --bit) {
-      const int t = id + (1 << bit);
-      if (t >= a.vocab || t < 0) continue;
-      uint64_t c = 0;
-      each([&](int i, float v) { c += key_of(v) == cut && i <= t; });
-      if (block_reduce64<kRowThreads>(c, sh, Add64()) <= ties) id = t;
+  // f(id, sum of `of(id, logit)` over the ids in front, up to this one), in rounds of the workgroup
+  auto walk = [&](auto&& of, auto&& f) {
+    uint64_t base = 0;
+    for (int c0 = 0; c0 < n_chunks; c0 += kRowThreads) {
+      uint64_t m[E], mine = 0;
+      const int ch = c0 + tid;
+      Chunk<T> x;
+      load_chunk(x, z, ch, a.vocab);  // (past the row: -inf)
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        m[e] = of(ch * E + e, x.z[e]);
+        mine += m[e];
+      }
+      uint64_t before = wave_inclusive64(mine, lane);  // then exclusive over the workgroup
+      __syncthreads();
+      if (lane == 63) wave_mass[wave] = before;
+      __syncthreads();
+      uint64_t round = 0;
+      before += base - mine;
+      for (int w = 0; w < kRowThreads / 64; ++w) {
+        if (w < wave) before += wave_mass[w];
+        round += wave_mass[w];
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        f(ch * E + e, before, before + m[e]);
+        before += m[e];
+      }
+      base += round;
     }
-    last_id = id;
+  };
+  int last_id = a.vocab;
+  if (ties != ~(uint64_t)0) {  // that of the last of them
+    if (tid == 0) (*found) = a.vocab;
+    walk([&](int, float v) -> uint64_t { return key_of(v) == cut ? 1 : 0; },
+         [&](int id, uint64_t before, uint64_t after) {
+           if (before < ties && after == ties) (*found) = id;
+         });
+    __syncthreads();
+    last_id = *found;
+    __syncthreads();
   }
-  // masses by id: rounds of the workgroup, then wavefronts, lanes, logits
   auto held = [&](int id, float v) {
     const uint32_t k = key_of(v);
-    return k > cut || (k == cut && id <= last_id) ? mass<BF16>(v, top, s) : 0;
+    return k > kKeyNone && (k > cut || (k == cut && id <= last_id)) ? mass<BF16>(v, top, s) : (uint64_t)0;
   };
   uint64_t total = 0;
   each([&](int id, float v) { total += held(id, v); });
   total = block_reduce64<kRowThreads>(total, sh, Add64());
   const double want = (double)p.u * (double)total;
   if (tid == 0) (*found) = -1;
-  uint64_t base = 0;
-  for (int c0 = 0; c0 < n_chunks; c0 += kRowThreads) {
-    uint64_t m[E], mine = 0;
-    Chunk<T> x;
-    const int ch = c0 + tid;
-    if (ch < n_chunks) load_chunk(x, z, ch, a.vocab);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      m[e] = ch < n_chunks ? held(ch * E + e, x.z[e]) : 0;
-      mine += m[e];
-    }
-    uint64_t before = mine;  // inclusive over the wavefront, then exclusive over the workgroup
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const uint32_t lo = (uint32_t)__shfl_up((int)(uint32_t)before, o, kWave), hi = (uint32_t)__shfl_up((int)(uint32_t)(before >> 32), o, kWave);
-      if (lane >= o) before += ((uint64_t)hi << 32) | lo;
-    }
-    __syncthreads();
-    if (lane == 63) wave_mass[wave] = before;
-    __syncthreads();
-    uint64_t round = 0;
-    before += base - mine;
-    for (int w = 0; w < kRowThreads / 64; ++w) {
-      if (w < wave) before += wave_mass[w];
-      round += wave_mass[w];
-    }
-#pragma unroll
-    for (int e = 0; e < E; ++e) {  // (the last token with a mass takes what rounding leaves)
-      const uint64_t after = before + m[e];
-      if (m[e] > 0 && (double)before <= want && (!((double)after <= want) || after == total)) {
-        atomicMax(found, ch * E + e);
-      }
-      before = after;
-    }
-    base += round;
-  }
+  walk(held, [&](int id, uint64_t before, uint64_t after) {  // (the last token with a mass takes what rounding leaves)
+    if (before < after && (double)before <= want && (!((double)after <= want) || after == total)) atomicMax(found, id);
+  });
   __syncthreads();
   const int token = (*found);
   if (tid == 0) {
@@ -710,15 +740,6 @@ __device__ __forceinline__ RowCut cut_row(const SampleWs& ws, int r, const RowPa
     c.count_k = sh.count[k_bin];
   }
   return c;
-}
-
-__device__ __forceinline__ uint64_t wave_inclusive64(uint64_t v, int lane) {
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const uint32_t lo = (uint32_t)__shfl_up((int)(uint32_t)v, o, kWave), hi = (uint32_t)__shfl_up((int)(uint32_t)(v >> 32), o, kWave);
-    if (lane >= o) v += ((uint64_t)hi << 32) | lo;
-  }
-  return v;
 }
 
 template <class T, int SLICE>
