@@ -292,12 +292,12 @@ def sample_tokens(logits, masked, uniform, temperature, top_k, top_p, min_p, tok
     for t, dtype, name in ((uniform, torch.float32, "uniform"), (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
                            (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"), (tokens, torch.int32, "tokens"), (conf, torch.float32, "conf"),
                            (prob, torch.float32, "prob")):
-        if t is not None:
+        if t is not None and not (t.dtype == dtype and t.is_cuda and t.shape == rows and t.is_contiguous()):
             _need(t, dtype, name)
             if t.shape != rows or not t.is_contiguous():
                 raise ValueError(f"{name}: expected {rows[0]} values next to each other, got shape {tuple(t.shape)}, strides {t.stride()}")
-    if masked is not None and (masked.element_size() != 1 or masked.shape != rows or not masked.is_contiguous()):
-        raise ValueError(f"masked: expected {rows[0]} bytes, got {masked.dtype}, shape {tuple(masked.shape)}")
+    if masked is not None and (not masked.is_cuda or masked.element_size() != 1 or masked.shape != rows or not masked.is_contiguous()):
+        raise ValueError(f"masked: expected {rows[0]} bytes on the GPU, got {masked.dtype}, shape {tuple(masked.shape)} on {masked.device}")
     _check(lib().focus_sample_tokens(_ptr(logits), int(logits.dtype == torch.float32), stride, _ptr(masked), _ptr(uniform), _ptr(temperature),
                                      _ptr(top_k), _ptr(top_p), _ptr(min_p), rows[0], vocab, _ptr(tokens), _ptr(conf), _ptr(prob),
                                      _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_on(logits)))
