@@ -363,7 +363,8 @@ int focus_block_entry(void* K_cache, void* V_cache, const focus_shape* shape, co
  * Writing takes the smallest 2^E with which the largest finite magnitude of the row is at most 448, -110 <= E <= 119, and
  * rounds to the nearest code, ties to even (magnitudes past 448 * 2^119 to that; infinities and NaN take the NaN code; a row of zeros
  * has E = -110).  What a row reads back as is exact in bf16: every entry point over such a cache computes what its bf16
- * counterpart computes over the bf16 cache that focus_quant_read gives, to rounding of the sums.
+ * counterpart computes over the bf16 cache that focus_quant_read gives, to rounding of the sums (for queries of magnitudes
+ * from 2^-100 to 2^100, and zero: products with the codes are added before the row's power of two enters).
  * A cache of zero bytes reads back as zeros.  An exponent byte of 255 is not a number that these calls write or take.
  *   shape   k_/v_stride_* are the strides of the codes, in bytes, multiples of 16 (rows 16-byte aligned); the others as everywhere
  */

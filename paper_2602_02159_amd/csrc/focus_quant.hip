@@ -72,7 +72,8 @@ __device__ __forceinline__ uint2 store_row(const uint4& x, bool live, uint8_t* c
 }
 
 // Slots a of the list, D / 8 threads each: the rows of K and V, requested together with the position, the count and the entries behind
-// it.  A position that is listed again further down is left to that entry: its codes and its exponent come from one state.
+// it.  A position that is listed again further down is left to that entry: its codes and its exponent come from one state.  One launch and two
+// dependent round trips, nothing else counts (8 rows, 4 heads: 2.5 us a call in a graph, 2.8 traced).
 template <int D>
 __global__ __launch_bounds__(256) void quant_update_kernel(const CacheUpdate u, const QuantCache q) {
   constexpr int kChunks = D / 8, kAhead = 4;
@@ -100,8 +101,55 @@ __global__ __launch_bounds__(256) void quant_update_kernel(const CacheUpdate u, 
   store_row<D>(v, live, q.V + (int64_t)h * u.vsh + at * u.vsn + c * 8, q.v_exp + e, c);
 }
 
+// The same of a long list, which is compared with itself once for several heads: every entry behind the workgroup's first slot is read by
+// one thread and compared with all its slots.
+template <int D>
+__global__ __launch_bounds__(256) void quant_update_many_kernel(const CacheUpdate u, const QuantCache q, int heads) {
+  constexpr int kChunks = D / 8, kSlots = 256 / kChunks, kAhead = 8;
+  __shared__ uint32_t again_sh;
+  const int a0 = blockIdx.x * kSlots, j = (int)threadIdx.x / kChunks, a = a0 + j, c = (int)threadIdx.x % kChunks;
+  const int slot = min(a, u.max_active - 1);
+  if (threadIdx.x == 0) again_sh = 0;
+  const int n_act = u.counts ? min(max(u.counts[1], 0), u.max_active) : u.max_active;
+  if (a0 >= n_act) return;  // whole workgroup
+  const int i = u.active_idx[slot];
+  int mine[kSlots];
+#pragma unroll
+  for (int s = 0; s < kSlots; ++s) mine[s] = uniform_load(u.active_idx + min(a0 + s, u.max_active - 1));
+  uint32_t again = 0;
+  for (int t0 = a0 + 1 + (int)threadIdx.x; t0 < n_act; t0 += 256 * kAhead) {
+    int later[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) later[k] = u.active_idx[min(t0 + k * 256, u.max_active - 1)];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int t = t0 + k * 256;
+      if (t >= n_act) break;
+#pragma unroll
+      for (int s = 0; s < kSlots; ++s) again |= later[k] == mine[s] && t > a0 + s ? 1u << s : 0u;
+    }
+  }
+  __syncthreads();
+  if (again != 0u) atomicOr(&again_sh, again);
+  __syncthreads();
+  const int64_t row = (int64_t)u.row_base + i;
+  const bool live = a < n_act && i >= 0 && row >= 0 && row < u.n_rows && !((again_sh >> j) & 1u);
+  const int64_t at = live ? row : 0;
+  const int h0 = (int)blockIdx.y * heads, h1 = min(h0 + heads, u.n_heads);
+#pragma unroll 2
+  for (int h = h0; h < h1; ++h) {
+    const int64_t src = (int64_t)h * u.nsh + (int64_t)slot * u.nsn + c * 8, e = (int64_t)h * q.esh + at * q.esn;
+    const uint4 k = *reinterpret_cast<const uint4*>(u.Kn + src);
+    const uint4 v = *reinterpret_cast<const uint4*>(u.Vn + src);
+    store_row<D>(k, live, q.K + (int64_t)h * u.ksh + at * u.ksn + c * 8, q.k_exp + e, c);
+    store_row<D>(v, live, q.V + (int64_t)h * u.vsh + at * u.vsn + c * 8, q.v_exp + e, c);
+  }
+}
+
 // One workgroup per (chunk of B rows, head), as in cache_refresh_chunk; the means are those of the values that the rows read back as,
-// accumulated in the order of block_means_kernel.
+// accumulated in the order of block_means_kernel.  Bound by HBM: 538 MB read, 275 written at 32 heads, 32 832 rows of 128 in 148 to 151 us a
+// call = 5.4 TB/s (copying them as bf16: 186 us, 1.08 GB); four rows of K and of V a thread under way, read past the caches because
+// nothing reads them again.
 template <int D>
 __global__ __launch_bounds__(256) void quant_refresh_kernel(const CacheRefresh p, const QuantCache q) {
   constexpr int TPR = D / 8, RPP = 256 / TPR, UNROLL = 4;
@@ -148,6 +196,8 @@ __global__ __launch_bounds__(256) void quant_refresh_kernel(const CacheRefresh p
   }
 }
 
+// Bound by HBM: 271 MB read, 538 written in 115 to 120 us = 6.8 to 7.0 TB/s, part of the codes from the memory-side cache; 131 us a call.
+// Stores pass the caches by.
 constexpr int kReadRows = 4;  // rows of K and of V per thread
 template <int D>
 __global__ __launch_bounds__(256) void quant_read_kernel(const QuantRead p, const QuantCache q) {
@@ -174,11 +224,24 @@ __global__ __launch_bounds__(256) void quant_read_kernel(const QuantRead p, cons
   }
 }
 
+// Long lists: 32 heads, rows of 128, 4096 rows 75.6 -> 26.5 us, 32 768 2854 -> 207 (as bf16 21 and 182); 1024 rows 13.0 -> 10.9; up to 512 rows
+// both are launch and latency, 6 to 8 us.  As many heads a workgroup as leave eight workgroups per compute unit.
+constexpr int kUpdateMany = 512, kUpdateGroups = 2048;
+template <int D>
+static void launch_quant_update_t(const CacheUpdate& u, const QuantCache& q, hipStream_t st) {
+  const int groups = ceil_div(u.max_active, 2048 / D);
+  if (u.max_active <= kUpdateMany) {
+    hipLaunchKernelGGL(quant_update_kernel<D>, dim3(groups, u.n_heads), dim3(256), 0, st, u, q);
+    return;
+  }
+  const int heads = std::max((int)std::min<int64_t>((int64_t)groups * u.n_heads / kUpdateGroups, u.n_heads), 1);
+  hipLaunchKernelGGL(quant_update_many_kernel<D>, dim3(groups, ceil_div(u.n_heads, heads)), dim3(256), 0, st, u, q, heads);
+}
 hipError_t launch_quant_update(const CacheUpdate& u, const QuantCache& q, int head_dim, hipStream_t st) {
   if (head_dim == 128)
-    hipLaunchKernelGGL(quant_update_kernel<128>, dim3(ceil_div(u.max_active, 16), u.n_heads), dim3(256), 0, st, u, q);
+    launch_quant_update_t<128>(u, q, st);
   else
-    hipLaunchKernelGGL(quant_update_kernel<64>, dim3(ceil_div(u.max_active, 32), u.n_heads), dim3(256), 0, st, u, q);
+    launch_quant_update_t<64>(u, q, st);
   return hipGetLastError();
 }
 hipError_t launch_quant_refresh(const CacheRefresh& p, const QuantCache& q, int head_dim, hipStream_t st) {
@@ -210,6 +273,11 @@ hipError_t launch_quant_read(const QuantRead& p, const QuantCache& q, int n_head
 // No stage in LDS, no transposing read, no barrier: a sub-tile is 128 bytes a lane in registers.  The codes are widened
 // without their power of two; 2^E of a K row multiplies its logits and that of a V row its probabilities, eight of each a lane,
 // which takes a sixteenth of the multiplications and is exact.
+//
+// What bounds it (16 queries, 32 heads, d = 128): over every one of 32 832 rows HBM, 271 MB in 46 us = 5.9 TB/s (the bf16 cache: 81 us);
+// half of the blocks, 25 queries, 139 MB in 32 us, of which the key loop runs at 6.7 TB/s and the rest is the start (2.9 us), uneven splits
+// and the states' meeting; seven of 256 blocks, 8 MB in 6.7 to 8.3 us, the chain of dependent round trips, as over a bf16 cache.  With
+// many query groups (175 queries, 4 heads) widening the codes, which every group of 32 repeats: 19 us against 18.5 over the bf16 cache.
 // =====================================================================================================
 struct QuantAttnArgs {
   AttnArgs a;  // K and V: strides in bytes

@@ -173,6 +173,27 @@ def test_update_of_a_long_list_that_repeats_itself():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("H,n,n_act,d", [(7, 9001, 8999, 128), (33, 3000, 3000, 64), (2, 513, 500, 64), (3, 700, 0, 128), (1, 600, 1, 128), (70, 1500, 777, 128)])
+def test_update_of_long_lists_of_many_heads(H, n, n_act, d):
+    M = 9000
+    rng = np.random.default_rng(n)
+    idx = rng.permutation(np.concatenate([rng.permutation(M)[:n - 200], rng.integers(-3, M + 3, 200 + max(0, n - 200 - M))])[:n])
+    c = Cache(H, M, d, 50, M, "padded", fill=0x5a)
+    g = torch.Generator(device=DEV).manual_seed(n)
+    kn, vn = (torch.randn((H, n, d), generator=g, device=DEV).to(torch.bfloat16) for _ in range(2))
+    whole = Cache(H, n, d, 50, n)  # every slot's row
+    fb.quant_refresh(whole.struct, whole.shape(), kn, vn, None)
+    want = [t.copy() for t in c.bytes()]
+    last = {int(i): a for a, i in enumerate(idx[:n_act]) if 0 <= i < M}
+    rows, slots = np.array(list(last), dtype=int), np.array(list(last.values()), dtype=int)
+    for w, x in zip(want, whole.bytes()):
+        w[:, rows] = x[:, slots]
+    fb.quant_update(c.struct, c.shape(), kn, vn, i32(idx), i32([0, n_act]), 0)
+    for got, ref in zip(c.bytes(), want):
+        assert np.array_equal(got, ref)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("d", [64, 128])
 def test_values_at_the_ends_of_the_formats(d):
     big = torch.finfo(torch.bfloat16).max
