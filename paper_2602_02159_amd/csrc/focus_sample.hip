@@ -452,7 +452,7 @@ __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t*
 // last launch searches the row instead.
 //
 // What bounds it.  One row of 126 464: three launches of 3.5, 2.5 and 2.4 us, each a chain of round trips.  64 such rows (bf16, 16 MB, three
-// quarters of them drawn from) 13.4, 15.0 and 10.4 us, 511 rows of 32 003 (float32, 65 MB) 28.4, 30.2 and 15.4: the arithmetic on each logit,
+// quarters of them drawn from) 13.6, 15.0 and 9.9 us, 511 rows of 32 003 (float32, 65 MB) 26.0, 29.0 and 15.4: the arithmetic on each logit,
 // 50 to 60 instructions in either of the first two where the bulk of a row carries the mass, at a quarter to a half of the rate at
 // which HBM would deliver.  One workgroup that keeps a whole row in registers through all three parts (up to 65 536 bf16 logits) saves two
 // launches and the second read, and is slower: it holds 128 registers and 68 KB of LDS and computes the same, with fewer wavefronts to hide
@@ -602,12 +602,13 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleA
 }
 
 constexpr int kNoBin = 4 * kBins;
+constexpr int kEarly = 4;  // slices whose bins are requested beside the statistics, before it is known how far down they begin
 struct CutShared {
   RowCut cut;
   int shift[4 * kMaxSlices];
+  uint64_t early[kEarly][kBins];
   float mass[kBins + 1];  // of the bins in front
   uint32_t count[kBins + 1];
-  unsigned long long above[kBins];
   float wave_mass[kScanThreads / 64];
   uint32_t wave_count[kScanThreads / 64];
   double down_min_p;
@@ -619,23 +620,23 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 // Every workgroup of the second launch works this out, in the same operations; the third reads it.  The slices' statistics are one
-// wavefront's work, the logarithm of min_p another's.  Nothing but latency: the
-// histograms are requested beside the statistics, before it is known how far the slices' bins are apart, and meet in LDS.
+// wavefront's work, the logarithm of min_p another's.  Nothing but latency: the bins of the first slices are requested beside the
+// statistics, before it is known how far down they begin, and wait in LDS; those of the others AHEAD at a time, from where they belong.  (A
+// thread adds up one bin; with atomics into LDS instead a row of 126 464 bf16 logits takes 24.4 us and not 23.4, one of 1 000 000
+// 60 and not 54.)
+template <int AHEAD>
 __device__ __forceinline__ RowCut cut_row(const SampleWs& ws, int r, const RowParams& p, CutShared& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const SliceStat* stat = ws.stat + (int64_t)r * ws.slices;
   const bool drawn = p.temperature > 0.f, order = drawn && needs_order(p);
   const float T = drawn ? p.temperature : 1.f;
   const float per_unit = bins_per_unit(T);
-  constexpr int kAhead = 8;
-  const uint64_t* bins = ws.bins + (int64_t)r * ws.slices * kBins + tid;
-  uint64_t v[kAhead];
+  const uint64_t* bins = ws.bins + (int64_t)r * ws.slices * kBins;
+  uint64_t early[kEarly];
   if (order) {
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) v[u] = bins[(int64_t)min(u, ws.slices - 1) * kBins];  // (of a slice without a number: whatever lies there)
+    for (int u = 0; u < kEarly; ++u) early[u] = bins[(int64_t)min(u, ws.slices - 1) * kBins + tid];  // (of a slice without a number: whatever lies there)
   }
-  sh.count[tid + 1] = 0;
-  sh.above[tid] = 0;
   if (wave == 0) {
     RowCut c;
     auto larger = [](uint32_t x, uint32_t y) { return x > y ? x : y; };
@@ -674,31 +675,41 @@ __device__ __forceinline__ RowCut cut_row(const SampleWs& ws, int r, const RowPa
     }
   }
   if (wave == 1 && lane == 0) sh.down_min_p = p.min_p > 0.f && p.min_p < 1.f ? (double)T * log((double)p.min_p) : 0.0;
+  if (order) {
+#pragma unroll
+    for (int u = 0; u < kEarly; ++u) sh.early[u][tid] = early[u];
+  }
   __syncthreads();
   RowCut c = sh.cut;
   c.least_key = c.way == kDraw ? min_p_key(p.min_p, sh.down_min_p, c.top) : 0u;
   c.least = c.least_key > kKeyNone ? of_key(c.least_key) : -3.402823466e38f;
   if (c.way != kDraw || !order) return c;  // uniform over the workgroup, like the others
   const float first = floorf(c.top * per_unit);
-  for (int i0 = 0; i0 < ws.slices; i0 += kAhead) {
-    if (i0 > 0) {
+  uint32_t n = 0;
+  uint64_t above = 0;
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) v[u] = bins[(int64_t)min(i0 + u, ws.slices - 1) * kBins];
+  for (int u = 0; u < kEarly; ++u) {
+    const int shift = u < ws.slices ? sh.shift[u] : kBins;
+    const uint64_t v = sh.early[u][max(tid - shift, 0)];
+    n += tid >= shift ? (uint32_t)(v >> 32) : 0u;
+    above += tid >= shift ? (uint32_t)v : 0u;
+  }
+  for (int i0 = kEarly; i0 < ws.slices; i0 += AHEAD) {
+    uint64_t v[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {  // all requests first; a slice whose bins lie lower begins further down (shift), one past the last has none
+      const int i = min(i0 + u, ws.slices - 1);
+      v[u] = bins[(int64_t)i * kBins + max(tid - sh.shift[i], 0)];
     }
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (i0 + u >= ws.slices) break;
-      const int to = tid + sh.shift[i0 + u];
-      if (to < kBins && v[u] != 0) {
-        atomicAdd(&sh.count[to + 1], (uint32_t)(v[u] >> 32));
-        atomicAdd(&sh.above[to], (unsigned long long)(uint32_t)v[u]);
-      }
+    for (int u = 0; u < AHEAD; ++u) {
+      const bool in = i0 + u < ws.slices && tid >= sh.shift[min(i0 + u, ws.slices - 1)];
+      n += in ? (uint32_t)(v[u] >> 32) : 0u;
+      above += in ? (uint32_t)v[u] : 0u;
     }
   }
-  __syncthreads();
-  const uint32_t n = sh.count[tid + 1];
   const float down = (first - (float)tid - c.top * per_unit) * (1.4426950408889634f / kBinsPerNat);
-  float im = __builtin_amdgcn_exp2f(down) * ((float)n + (float)sh.above[tid] * (1.f / (131072.f * kBinsPerNat)));
+  float im = __builtin_amdgcn_exp2f(down) * ((float)n + (float)above * (1.f / (131072.f * kBinsPerNat)));
   uint32_t in = n;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
@@ -774,7 +785,7 @@ __global__ __launch_bounds__(kScanThreads, 6) void sample_cut_kernel(const Sampl
   Chunks<T, N> chunks;
   chunks.load(static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride, c0, kScanThreads, a.vocab);
   if (tid == 0) listed = 0;
-  const RowCut c = cut_row(ws, r, p, sh);
+  const RowCut c = cut_row<SLICE == kSlice ? 8 : 16>(ws, r, p, sh);
   if (slice == 0 && tid == 0) ws.cut[r] = c;
   if (c.way != kDraw) return;  // uniform over the workgroup
   __syncthreads();
