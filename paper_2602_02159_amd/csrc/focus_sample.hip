@@ -451,7 +451,8 @@ __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t*
 // to a mass once.  Where the lists do not hold the tokens of a bin, or the bins do not resolve the logits (2^18 and more, at T = 1), the
 // last launch searches the row instead.
 //
-// What bounds it.  One row of 126 464: three launches of 3.5, 2.5 and 2.4 us, each a chain of round trips.  64 such rows (bf16, 16 MB, three
+// What bounds it.  One row of 126 464: three launches of 4.5, 9.9 and 9.2 us, each a chain of round trips (3.5, 2.6 and 2.4 where the largest
+// logit is taken).  64 such rows (bf16, 16 MB, three
 // quarters of them drawn from) 13.6, 15.0 and 9.9 us, 511 rows of 32 003 (float32, 65 MB) 26.0, 29.0 and 15.4: the arithmetic on each logit,
 // 50 to 60 instructions in either of the first two where the bulk of a row carries the mass, at a quarter to a half of the rate at
 // which HBM would deliver.  One workgroup that keeps a whole row in registers through all three parts (up to 65 536 bf16 logits) saves two
