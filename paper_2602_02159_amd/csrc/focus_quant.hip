@@ -105,7 +105,7 @@ __global__ __launch_bounds__(256) void quant_update_kernel(const CacheUpdate u, 
 // one thread and compared with all its slots.
 template <int D>
 __global__ __launch_bounds__(256) void quant_update_many_kernel(const CacheUpdate u, const QuantCache q, int heads) {
-  constexpr int kChunks = D / 8, kSlots = 256 / kChunks, kAhead = 8;
+  constexpr int kChunks = D / 8, kSlots = 256 / kChunks, kAhead = 2;
   __shared__ uint32_t again_sh;
   const int a0 = blockIdx.x * kSlots, j = (int)threadIdx.x / kChunks, a = a0 + j, c = (int)threadIdx.x % kChunks;
   const int slot = min(a, u.max_active - 1);
@@ -124,9 +124,9 @@ __global__ __launch_bounds__(256) void quant_update_many_kernel(const CacheUpdat
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int t = t0 + k * 256;
-      if (t >= n_act) break;
+      const int id = t < n_act ? later[k] : -1;  // (no row)
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s) again |= later[k] == mine[s] && t > a0 + s ? 1u << s : 0u;
+      for (int s = 0; s < kSlots; ++s) again |= id == mine[s] && t > a0 + s ? 1u << s : 0u;
     }
   }
   __syncthreads();

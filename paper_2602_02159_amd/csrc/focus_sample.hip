@@ -431,7 +431,7 @@ __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t*
   __syncthreads();
   const int token = (*found);
   if (tid == 0) {
-    const float v = token < 0 ? top : clean(sizeof(T) == 4 ? reinterpret_cast<const float*>(z)[token] : bf16_lo(reinterpret_cast<const uint16_t*>(z)[token]));
+    const float v = token < 0 ? top : logit_at(z, token);
     const double w1 = weight<BF16>(v, top, s1), w = weight<BF16>(v, top, s);
     write_row(a, row, token < 0 ? first_id : token, (float)(w1 / denom), (float)(w / ((double)total * unit)));
   }
