@@ -145,11 +145,11 @@ __device__ __forceinline__ float weight(float z, float top, const Scale& s) {
   const float w = __builtin_amdgcn_exp2f(-x);
   return x < 60.f ? __builtin_fmaf(w * -0.6931471805599453f, r, w) : 0.f;
 }
-// w < 2^22 in units of 2^-42, to nearest.  Both halves are whole numbers of 32 bits: what is left of w 2^10 has 24 bits and is below 1.
+// 0 <= w < 512 in units of 2^-42, to nearest: the doubles of [1024, 2048) are 2^-42 apart
 __device__ __forceinline__ uint64_t mass_of(float w) {
-  const float x = w * 1024.f;
-  const uint32_t high = (uint32_t)x;
-  return ((uint64_t)high << 32) | (uint32_t)rintf((x - (float)high) * 4294967296.f);
+  constexpr double kAt = 1536.0;
+  static_assert(kMassBits == 42, "the last place of kAt");
+  return (uint64_t)(__double_as_longlong((double)w + kAt) - __double_as_longlong(kAt));
 }
 template <bool BF16>
 __device__ __forceinline__ uint64_t mass(float z, float top, const Scale& s) {
@@ -439,17 +439,19 @@ __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t*
 
 // =====================================================================================================
 // The ordinary way: three launches, the first two with a workgroup per slice of a row.
-//   sample_scan_kernel   the slice's largest logit and weights, and a histogram of the order: bins of 1/16 in logit / T, counts and
+//   sample_scan_kernel   the slice's largest logit and its weights at T = 1, and a histogram of the order: bins of 1/16 in logit / T, counts and
 //                        masses.  Bins are counted from zero logit up (floor(z * bins per unit)), so that those of all slices are the
 //                        same; a bin kBins and more below the largest logit's has no mass.
 //   sample_cut_kernel    from the row's histogram the bins in which top_k and top_p end.  Tokens above them are kept whatever comes:
 //                        their masses are summed per segment of 64 chunks.  Tokens in them are listed.
 //   sample_pick_kernel   a workgroup per row orders the list, finds the end of what is kept in it, adds the kept ones to their segments, and
 //                        walks down: segment, chunk, token.
-// The row is read twice, the second time from a cache.  The histogram only says where to look: ends are decided by the weights, and
-// everything that workgroups add up in no order is a whole number.  A chunk's weights are added as floats, in order, and the sum is rounded
-// to a mass once.  Where the lists do not hold the tokens of a bin, or the bins do not resolve the logits (2^18 and more, at T = 1), the
-// last launch searches the row instead.
+// The row is read twice, the second time from a cache.  The histogram only says where to look: ends and borders are decided by the masses,
+// token for token, so they are the same whichever way a row takes and however it is cut into slices.  (The confidence's sum alone is of
+// floats, 8 or 32 of a thread at a time.  With chunks of weights added as floats rows without a filter took 3 to 4 us less, 64 bf16 rows
+// of 126 464 24.3 -> 26.4, 511 of 32 003 38.8 -> 42.7 and as float32 49.5 -> 52.9, filtered ones up to 2 us less or more; a weight
+// below 2^-24 of its chunk's sum then got no share.)  Where the lists do not hold the tokens of a bin, or the bins do not resolve
+// the logits (2^18 and more, at T = 1), the last launch searches the row instead.
 //
 // What bounds it.  One row of 126 464: three launches of 4.5, 9.9 and 9.2 us, each a chain of round trips (3.5, 2.6 and 2.4 where the largest
 // logit is taken).  64 such rows (bf16, 16 MB, three
@@ -471,8 +473,7 @@ constexpr float kBinsPerNat = 16.f, kMostPerUnit = 8192.f;  // bins per unit of 
 struct SliceStat {
   float top;   // -inf: no number
   int id;      // the first with it
-  double at1;  // sum of the weights at T = 1 and at T, relative to `top`
-  double atT;
+  double at1;  // sum of the weights at T = 1, relative to `top`
 };
 // Where a row is cut.
 struct RowCut {
@@ -483,6 +484,8 @@ struct RowCut {
   float per_unit;                  // bins per unit of logit; the next four are logits times that
   float sure;                      // tokens from here on are kept
   float p_low, k_high, k_low;      // the list: [p_low, sure) and [k_low, k_high), where top_k ends apart from top_p
+  float rest_low, rest_high;       // tokens whose masses top_p counts beside those of the sure and the listed ones that top_k leaves: [k_high, p_low)
+                                   // where that is apart, all but the sure ones where top_k ends nothing, else none
   bool apart;
   uint32_t count_sure, count_k;    // tokens above `sure`, above k_high
   float least;                     // min_p: no logit below this one
@@ -492,7 +495,7 @@ enum { kNone = 0, kFirst = 1, kDraw = 2, kSearch = 3 };
 struct SampleWs {
   SliceStat* stat;   // [rows, slices]
   uint64_t* bins;    // [rows, slices, kBins]  tokens in the upper half, their masses above that of the bin's lower end in the lower half
-  uint64_t* middle;  // [rows, slices]  mass between the two parts of the list
+  uint64_t* rest;    // [rows, slices]  mass of [rest_low, rest_high)
   uint32_t* listed;  // [rows, slices]
   uint64_t* list;    // [rows, slices, kSliceList]  order_of() each
   RowCut* cut;       // [rows]
@@ -514,10 +517,9 @@ __device__ __forceinline__ uint64_t wave_mass_sum(uint64_t m) {
 template <class T, int SLICE>
 __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleArgs a, const SampleWs ws, int row0) {
   constexpr int E = Chunk<T>::E, N = SLICE / E / kScanThreads, kCopies = 4, kWaves = kScanThreads / 64;
-  constexpr bool BF16 = sizeof(T) == 2;
   __shared__ unsigned long long bins_sh[kCopies][kBins];
   __shared__ float top_sh[kWaves];
-  __shared__ unsigned long long at1_sh, atT_sh;
+  __shared__ unsigned long long at1_sh;
   __shared__ int id_sh;
   const int slice = blockIdx.x, r = blockIdx.y, row = row0 + r, tid = threadIdx.x;
   const RowParams p = row_params(a, row);
@@ -532,7 +534,7 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleA
   }
   if (tid == 0) {
     id_sh = 0x7fffffff;
-    at1_sh = atT_sh = 0;
+    at1_sh = 0;
   }
   float mine = -INFINITY;
   chunks.each([&](int, const Chunk<T>& x) {
@@ -547,7 +549,7 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleA
   for (int w = 0; w < kWaves; ++w) top = fmaxf(top, top_sh[w]);
   SliceStat* stat = ws.stat + (int64_t)r * ws.slices + slice;
   if (top == -INFINITY) {
-    if (tid == 0) *stat = SliceStat{top, 0, 0.0, 0.0};
+    if (tid == 0) *stat = SliceStat{top, 0, 0.0};
     return;
   }
   if (mine == top) {
@@ -561,18 +563,13 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleA
   }
   // exp(f / 16) - 1 = g(f) / 16 for the place f of a token in its bin: 1 + f / 32 + f^2 / 1536 times f, in units of 2^-17
   const float T_ = drawn ? p.temperature : 1.f, per_unit = bins_per_unit(T_), first = floorf(top * per_unit);
-  const Scale s = scale_of(T_);
-  const bool all = order && p.top_p < 1.f, conf = a.conf != nullptr;
+  const bool conf = a.conf != nullptr;
   unsigned long long* bins = bins_sh[tid & (kCopies - 1)];
-  float at1 = 0.f, atT = 0.f;
+  float at1 = 0.f;
   chunks.each([&](int, const Chunk<T>& x) {
     if (conf) {
 #pragma unroll
       for (int e = 0; e < E; ++e) at1 += __builtin_amdgcn_exp2f((x.z[e] - top) * 1.4426950408889634f);
-    }
-    if (all) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) atT += weight<BF16>(x.z[e], top, s);
     }
     if (order) {
 #pragma unroll
@@ -586,13 +583,10 @@ __global__ __launch_bounds__(kScanThreads) void sample_scan_kernel(const SampleA
       }
     }
   });
-  const uint64_t w1 = wave_mass_sum(mass_of(at1)), wT = wave_mass_sum(mass_of(atT));  // (32 at most each: below 2^48)
-  if ((tid & 63) == 0) {
-    atomicAdd(&at1_sh, (unsigned long long)w1);
-    atomicAdd(&atT_sh, (unsigned long long)wT);
-  }
+  const uint64_t w1 = wave_mass_sum(mass_of(at1));  // (32 at most each: below 2^48)
+  if ((tid & 63) == 0) atomicAdd(&at1_sh, (unsigned long long)w1);
   __syncthreads();
-  if (tid == 0) *stat = SliceStat{top, id_sh, (double)at1_sh * kMassUnit, (double)atT_sh * kMassUnit};
+  if (tid == 0) *stat = SliceStat{top, id_sh, (double)at1_sh * kMassUnit};
   if (order) {
     static_assert(kBins == kScanThreads, "a bin a thread");
     uint64_t v = 0;  // 16384 tokens at most: the lower half holds 16384 * 1.04 * 2^17
@@ -665,7 +659,8 @@ __device__ __forceinline__ RowCut cut_row(const SampleWs& ws, int r, const RowPa
     c.ends = 0;
     c.per_unit = per_unit;
     c.sure = -INFINITY;
-    c.p_low = c.k_high = c.k_low = INFINITY;
+    c.p_low = c.k_high = c.k_low = c.rest_low = INFINITY;
+    c.rest_high = -INFINITY;
     c.apart = false;
     c.count_sure = c.count_k = 0;
     if (lane == 0) {
@@ -767,6 +762,11 @@ __device__ __forceinline__ RowCut cut_row(const SampleWs& ws, int r, const RowPa
     c.k_high = first - (float)(k_bin - 1);
     c.k_low = first - (float)k_bin;
     c.count_k = sh.count[k_bin];
+    c.rest_low = c.k_high;
+    c.rest_high = c.p_low;
+  } else if (k_bin >= kBins) {
+    c.rest_low = -INFINITY;
+    c.rest_high = c.sure;
   }
   return c;
 }
@@ -776,7 +776,7 @@ __global__ __launch_bounds__(kScanThreads, 6) void sample_cut_kernel(const Sampl
   constexpr int E = Chunk<T>::E, N = SLICE / E / kScanThreads;
   constexpr bool BF16 = sizeof(T) == 2;
   __shared__ CutShared sh;
-  __shared__ uint64_t middle_sh[kScanThreads / 64];
+  __shared__ uint64_t rest_sh[kScanThreads / 64];
   __shared__ uint32_t listed;
   const int slice = blockIdx.x, r = blockIdx.y, row = row0 + r, tid = threadIdx.x;
   const RowParams p = row_params(a, row);
@@ -792,22 +792,27 @@ __global__ __launch_bounds__(kScanThreads, 6) void sample_cut_kernel(const Sampl
   __syncthreads();
   const Scale s = scale_of(p.temperature);
   uint64_t* list = ws.list + ((int64_t)r * ws.slices + slice) * kSliceList;
-  float middle = 0.f;
+  uint64_t rest = 0;
   chunks.each([&](int i, const Chunk<T>& x) {
     const int chunk = c0 + i * kScanThreads, seg = chunk / kSegChunks;
-    uint32_t sure = 0, hits = 0;
+    uint32_t sure = 0, other = 0, hits = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const float t = x.z[e] * c.per_unit;
       sure |= t >= c.sure && x.z[e] >= c.least ? 1u << e : 0u;
+      other |= t >= c.rest_low && t < c.rest_high ? 1u << e : 0u;
       hits |= (t >= c.p_low && t < c.sure) || (t >= c.k_low && t < c.k_high) ? 1u << e : 0u;
     }
     uint64_t m = 0;
-    if (__ballot(sure != 0u) != 0ull) {
-      float w = 0.f;
+    if (__ballot((sure | other) != 0u) != 0ull) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) w += (sure >> e) & 1u ? weight<BF16>(x.z[e], c.top, s) : 0.f;
-      m = wave_mass_sum(mass_of(w));
+      for (int e = 0; e < E; ++e)
+        if (((sure | other) >> e) & 1u) {
+          const uint64_t w = mass<BF16>(x.z[e], c.top, s);
+          m += (sure >> e) & 1u ? w : 0;
+          rest += (sure >> e) & 1u ? 0 : w;
+        }
+      m = wave_mass_sum(m);
     }
     if ((tid & 63) == 0 && seg < ws.segs) ws.seg[(int64_t)r * ws.segs + seg] = m;
     if (hits != 0u) {
@@ -819,22 +824,15 @@ __global__ __launch_bounds__(kScanThreads, 6) void sample_cut_kernel(const Sampl
           ++at;
         }
     }
-    if (c.apart) {  // uniform over the workgroup
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float t = x.z[e] * c.per_unit;
-        if (t >= c.k_high && t < c.p_low) middle += weight<BF16>(x.z[e], c.top, s);
-      }
-    }
   });
-  if (c.ends) {  // (a float per thread, which its tokens enter in order; whole numbers from there on)
-    uint64_t m = wave_mass_sum(mass_of(middle));
-    if ((tid & 63) == 0) middle_sh[tid >> 6] = m;
+  if (c.ends) {
+    uint64_t m = wave_mass_sum(rest);  // (32 tokens of at most 1 each: below 2^48)
+    if ((tid & 63) == 0) rest_sh[tid >> 6] = m;
     __syncthreads();
     if (tid == 0) {
       m = 0;
-      for (int w = 0; w < kScanThreads / 64; ++w) m += middle_sh[w];
-      ws.middle[(int64_t)r * ws.slices + slice] = m;
+      for (int w = 0; w < kScanThreads / 64; ++w) m += rest_sh[w];
+      ws.rest[(int64_t)r * ws.slices + slice] = m;
       ws.listed[(int64_t)r * ws.slices + slice] = listed;
     }
   }
@@ -953,7 +951,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
   __shared__ unsigned long long seg[SEGS];
   __shared__ uint64_t sum_a[kWaves], sum_b[kWaves], wave_mass[kWaves];
   __shared__ int found, n_first, n_kept;
-  __shared__ double at1_sh, atT_sh;
+  __shared__ double at1_sh;
   __shared__ uint64_t found_base;
   __shared__ unsigned long long listed_mass;
   __shared__ uint32_t begin_sh[4 * kMaxSlices];
@@ -970,18 +968,13 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
     if (tid == 0) write_row(a, row, -1, 0.f, 0.f);
     return;
   }
-  if (wave == kWaves - 1) {  // the sums of the weights over the slices, beside what the others do
-    double at1 = 0.0, atT = 0.0;
+  if (wave == kWaves - 1) {  // the sum of the weights at T = 1 over the slices, beside what the others do
+    double at1 = 0.0;
     for (int i = lane; i < ws.slices; i += kWave) {
       const SliceStat t = ws.stat[(int64_t)r * ws.slices + i];
-      if (t.top > -INFINITY) {
-        const double down = (double)t.top - (double)c.top;
-        at1 += t.at1 * exp(down);
-        atT += t.atT * exp(down / (double)p.temperature);
-      }
+      if (t.top > -INFINITY) at1 += t.at1 * exp((double)t.top - (double)c.top);
     }
     at1_sh = wave_sum(at1);
-    atT_sh = wave_sum(atT);
   }
   if (c.way == kFirst) {
     __syncthreads();
@@ -990,7 +983,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
   }
   const Scale s = scale_of(p.temperature);
   uint32_t n = 0;
-  uint64_t middle = 0;
+  uint64_t rest = 0;
   bool slow = c.way == kSearch;
   if (!slow) {
     for (int i = tid; i < ws.segs; i += kRowThreads) seg[i] = ws.seg[(int64_t)r * ws.segs + i];
@@ -998,10 +991,10 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
       for (int i0 = 0; i0 < ws.slices; i0 += kWave) {  // (every wavefront)
         const int i = min(i0 + lane, ws.slices - 1);
         uint32_t k = ws.listed[(int64_t)r * ws.slices + i];
-        uint64_t mid = ws.middle[(int64_t)r * ws.slices + i];
+        uint64_t beside = ws.rest[(int64_t)r * ws.slices + i];
         if (i0 + lane >= ws.slices) {
           k = 0;
-          mid = 0;
+          beside = 0;
         }
         slow = slow || __ballot(k > (uint32_t)kSliceList) != 0ull;
         uint32_t upto = k;
@@ -1013,8 +1006,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
         if (wave == 0 && i0 + lane < ws.slices) begin_sh[i0 + lane] = n + upto - k;
         n += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) mid += shfl_xor64(mid, o);
-        middle += mid;
+        for (int o = 32; o > 0; o >>= 1) beside += shfl_xor64(beside, o);
+        rest += beside;
       }
       slow = slow || n > (uint32_t)kRowList;
       __syncthreads();
@@ -1082,7 +1075,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
       const uint32_t in_front = tid < n_first ? c.count_sure + (uint32_t)tid : c.count_k + (uint32_t)(tid - n_first);  // tokens above
       if (cut && live && in_front < k && (in_front + 1 == k || tid + 1 == (int)n)) listed_mass = front + m;  // the mass of the first top_k
       __syncthreads();
-      const double target = p.top_p < 1.f ? (double)p.top_p * (cut ? (double)(sure + middle + listed_mass) : atT_sh / kMassUnit) : INFINITY;
+      const double target = p.top_p < 1.f ? (double)p.top_p * (double)(sure + rest + (cut ? listed_mass : 0)) : INFINITY;
       const bool kept = first && (!cut || in_front < k) && (double)(sure + front) < target && order <= least;
       const unsigned long long some = __ballot(kept);
       if (some != 0ull && lane == 0) atomicAdd(&n_kept, (int)__popcll(some));
@@ -1109,12 +1102,9 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
       End end{0, 0};
       if (cut) end = find_end<RUN>(order, m, c.apart ? second : first, true, c.apart ? c.count_k : c.count_sure, k, 0, 0.0, narrow);
       if (p.top_p < 1.f) {
-        double all = atT_sh / kMassUnit;
-        if (cut) {
-          all = (double)(sure + middle + end.mass);
-          if (c.apart) all += (double)block_reduce64<kRowThreads>(first_part, sum_b, Add64());
-        }
-        end = find_end<RUN>(order, m, first, false, 0, 0, sure, (double)p.top_p * all, narrow);
+        uint64_t all = sure + rest + end.mass;  // (nothing is cut: end.mass = 0)
+        if (c.apart) all += block_reduce64<kRowThreads>(first_part, sum_b, Add64());
+        end = find_end<RUN>(order, m, first, false, 0, 0, sure, (double)p.top_p * (double)all, narrow);
       }
       last = end.last < least ? end.last : least;
 #pragma unroll
@@ -1154,16 +1144,12 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
   const int chunk = found * kSegChunks + lane, n_chunks = (a.vocab + E - 1) / E;
   Chunk<T> x;
   load_chunk(x, z, min(chunk, n_chunks), a.vocab);
-  uint64_t end[E], extra = 0;  // masses up to each token of the chunk: the sum of the sure ones, as in the second launch, and the listed ones
-  float w = 0.f;
+  uint64_t end[E], upto = 0;  // masses of the kept ones, the sure and the listed, up to each token of the chunk
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const float v = x.z[e];
-    if (v * c.per_unit >= c.sure && v >= c.least)
-      w += weight<BF16>(v, c.top, s);
-    else if (c.ends && order_of(key_of(v), chunk * E + e) <= last)
-      extra += mass<BF16>(v, c.top, s);
-    end[e] = mass_of(w) + extra;
+    if ((v * c.per_unit >= c.sure && v >= c.least) || (c.ends && order_of(key_of(v), chunk * E + e) <= last)) upto += mass<BF16>(v, c.top, s);
+    end[e] = upto;
   }
   before = wave_inclusive64(end[E - 1], lane) - end[E - 1] + found_base;
 #pragma unroll
@@ -1178,7 +1164,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_pick_kernel(const SampleAr
 
 struct SamplePlan {
   int slice, slices, segs, rows;  // logits of a slice; rows of a pass
-  size_t stat, bins, middle, listed, list, cut, seg, total;
+  size_t stat, bins, rest, listed, list, cut, seg, total;
 };
 // Few rows: slices of a quarter, so that more compute units share a row.
 static SamplePlan plan_sample(int n_rows, int vocab) {
@@ -1197,7 +1183,7 @@ static SamplePlan plan_sample(int n_rows, int vocab) {
   };
   p.stat = take(n * sizeof(SliceStat));
   p.bins = take(n * kBins * sizeof(uint64_t));
-  p.middle = take(n * sizeof(uint64_t));
+  p.rest = take(n * sizeof(uint64_t));
   p.listed = take(n * sizeof(uint32_t));
   p.list = take(n * kSliceList * sizeof(uint64_t));
   p.cut = take((size_t)p.rows * sizeof(RowCut));
@@ -1212,7 +1198,7 @@ static hipError_t launch_sample_t(const SampleArgs& a, const SamplePlan& p, char
   SampleWs ws;
   ws.stat = reinterpret_cast<SliceStat*>(w + p.stat);
   ws.bins = reinterpret_cast<uint64_t*>(w + p.bins);
-  ws.middle = reinterpret_cast<uint64_t*>(w + p.middle);
+  ws.rest = reinterpret_cast<uint64_t*>(w + p.rest);
   ws.listed = reinterpret_cast<uint32_t*>(w + p.listed);
   ws.list = reinterpret_cast<uint64_t*>(w + p.list);
   ws.cut = reinterpret_cast<RowCut*>(w + p.cut);

@@ -284,3 +284,58 @@ def test_tensors_that_do_not_fit_the_call_are_refused(monkeypatch):
     one = {**ok, "logits": f32(n, 63)[2:3].clone(), "uniform": f32(n, 3)[:1, 0], "tokens": ok["tokens"][:1].fill_(-7)}  # one row: its stride means nothing
     fb.sample_tokens(**one)
     assert one["tokens"].item() == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("between", [1, 2, 11])
+def test_weights_far_below_the_largest_keep_their_share(between, dtype):
+    """Two tokens of weight 1 and, between them, some of w = exp(-17) = 0.69 * 2^-24 down to exp(-29) = 1.1 * 2^-42: whole numbers of 2^-42, all alike,
+    so half of the mass ends in their middle, however small they are.  exp(-30) is 0.4 of a unit: nothing.  prob: a weight is good
+    to 2^-22 of itself, and rounded."""
+    V = between + 2
+    for T in (1.0, 0.5, 4.0):
+        down = 17.0 + np.arange(14)
+        z = torch.zeros((14, V), dtype=dtype)
+        z[:, 1:-1] = torch.tensor(-down[:, None] * T).to(dtype)
+        tokens, _, prob = run(z, np.float32(0.5), T)
+        assert list(tokens) == [1 + between // 2] * 13 + [V - 1], T
+        w = np.exp(-down[:13])
+        assert (np.abs(prob[:13] - w / (2 + between * w)) <= 2.0 ** -21 * w).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("n", [3, 7, 30, 200])
+def test_top_p_counts_weights_far_below_the_largest(n, dtype):
+    """One token of weight 1 and n of w = exp(-17) = 0.69 * 2^-24: top_p = 1 - 2^-24 leaves one of the n out, by a margin of 0.44 w (their errors
+    are 200 * 2^-23 w and 100 units of 2^-42, of which w has 181 000)."""
+    w, p = math.exp(-17.0), 1.0 - 2.0 ** -24
+    kept = math.ceil((p * (1 + n * w) - 1) / w)
+    assert kept == n - 1
+    for first in (0, n):  # the largest in front, and behind
+        z = torch.full((1, n + 1), -17.0, dtype=dtype)
+        z[0, first] = 0.0
+        cum = np.cumsum([1.0] + [w] * kept if first == 0 else [w] * kept + [1.0])
+        at = int((cum <= p * cum[-1]).sum())
+        want = n if first == n and at == kept else at
+        tokens, _, prob = run(z, np.float32(p), 1.0, 0, np.float32(p))
+        assert tokens[0] == want, first
+        share = (1.0 if want == first else w) / cum[-1]
+        assert abs(prob[0] - share) <= 2.0 ** -21 * share
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("V", [9000, 126464])
+def test_a_row_gives_the_same_token_alone_and_among_others(V, dtype):
+    """The ends and borders do not hang on how a row is cut into slices, which follows from the number of rows."""
+    n = 130 if V == 9000 else 40
+    z = _logits(n, V, dtype, 77, 2.0)
+    rng = np.random.default_rng(6)
+    u, T, k, p = rng.random(n).astype(np.float32), rng.uniform(0.3, 1.5, n), rng.choice([0, 0, 1000], n), rng.choice([0.5, 0.9, 0.99, 1.0], n)
+    tokens, _, prob = run(z, u, T, k, p, 1e-6)
+    for i0 in range(0, n, 5):
+        at = slice(i0, i0 + 5)
+        some = run(z[at], u[at], T[at], k[at], p[at], 1e-6)
+        assert (some[0] == tokens[at]).all() and (some[2] == prob[at]).all()
