@@ -314,7 +314,7 @@ int focus_sample_tokens(const void* logits, int32_t dtype, int64_t row_stride, c
                         const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t n_rows,
                         int32_t vocab, int32_t* tokens, float* conf, float* prob, void* workspace, size_t ws_bytes,
                         void* stream);
-/* Bytes of workspace focus_sample_tokens needs; 0 on invalid arguments.  [host] only. */
+/* Bytes of workspace focus_sample_tokens needs, at least what fewer rows or a smaller vocabulary need; 0 on invalid arguments.  [host] only. */
 size_t focus_sample_tokens_workspace(int32_t n_rows, int32_t vocab);
 
 /*

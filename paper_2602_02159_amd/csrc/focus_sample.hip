@@ -1166,19 +1166,13 @@ struct SamplePlan {
   int slice, slices, segs, rows;  // logits of a slice; rows of a pass
   size_t stat, bins, rest, listed, list, cut, seg, total;
 };
-// Few rows: slices of a quarter, so that more compute units share a row.
-static SamplePlan plan_sample(int n_rows, int vocab) {
-  SamplePlan p;
-  auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  p.slice = (int64_t)n_rows * ceil_div(vocab, kSlice) <= 64 && ceil_div(vocab, kSliceSmall) <= 4 * kMaxSlices ? kSliceSmall : kSlice;
-  p.slices = ceil_div(vocab, p.slice);
-  p.segs = ceil_div(vocab, kSegChunks * 4);  // of float32, which has the shorter chunks
-  p.rows = std::max(1, std::min({n_rows, 1024, 4096 / p.slices}));
-  const size_t n = (size_t)p.rows * p.slices;
+constexpr int kSmallPlans = 64, kMostRows = 1024, kMostRowSlices = 4096;  // slices of kSlice of a call that takes quarters; rows and slices of a pass
+// Where the parts of a workspace lie for so many rows, slices of all rows and segments of all rows.
+static void place_parts(SamplePlan& p, size_t rows, size_t n, size_t segs) {
   size_t off = 0;
   auto take = [&](size_t bytes) {
     const size_t at = off;
-    off += align(bytes);
+    off += (bytes + 255) & ~(size_t)255;
     return at;
   };
   p.stat = take(n * sizeof(SliceStat));
@@ -1186,12 +1180,31 @@ static SamplePlan plan_sample(int n_rows, int vocab) {
   p.rest = take(n * sizeof(uint64_t));
   p.listed = take(n * sizeof(uint32_t));
   p.list = take(n * kSliceList * sizeof(uint64_t));
-  p.cut = take((size_t)p.rows * sizeof(RowCut));
-  p.seg = take((size_t)p.rows * p.segs * sizeof(uint64_t));
+  p.cut = take(rows * sizeof(RowCut));
+  p.seg = take(segs * sizeof(uint64_t));
   p.total = off;
+}
+// Few rows: slices of a quarter, so that more compute units share a row.
+static SamplePlan plan_sample(int n_rows, int vocab) {
+  SamplePlan p;
+  p.slice = (int64_t)n_rows * ceil_div(vocab, kSlice) <= kSmallPlans && ceil_div(vocab, kSliceSmall) <= 4 * kMaxSlices ? kSliceSmall : kSlice;
+  p.slices = ceil_div(vocab, p.slice);
+  p.segs = ceil_div(vocab, kSegChunks * 4);  // of float32, which has the shorter chunks
+  p.rows = std::max(1, std::min({n_rows, kMostRows, kMostRowSlices / p.slices}));
+  place_parts(p, p.rows, (size_t)p.rows * p.slices, (size_t)p.rows * p.segs);
   return p;
 }
-size_t sample_tokens_workspace(int n_rows, int vocab) { return plan_sample(n_rows, vocab).total; }
+// What every plan of up to so many rows and so large a vocabulary fits into, part for part, so that a caller's workspace for its largest call
+// serves the smaller ones: fewer rows can mean more slices.  A quarter's plan has at most 4 * kSmallPlans slices; a slice has
+// kSlice / (4 * kSegChunks) segments.
+size_t sample_tokens_workspace(int n_rows, int vocab) {
+  const size_t rows = std::min(n_rows, kMostRows);
+  const size_t quarters = std::min<size_t>(rows * ceil_div(vocab, kSliceSmall), 4 * kSmallPlans);
+  const size_t slices = std::min<size_t>(rows * ceil_div(vocab, kSlice), kMostRowSlices);
+  SamplePlan p;
+  place_parts(p, rows, std::max(quarters, slices), std::min<size_t>(rows * ceil_div(vocab, kSegChunks * 4), (size_t)kMostRowSlices * (kSlice / (4 * kSegChunks))));
+  return p.total;
+}
 
 template <class T>
 static hipError_t launch_sample_t(const SampleArgs& a, const SamplePlan& p, char* w, hipStream_t st) {

@@ -339,3 +339,34 @@ def test_a_row_gives_the_same_token_alone_and_among_others(V, dtype):
         at = slice(i0, i0 + 5)
         some = run(z[at], u[at], T[at], k[at], p[at], 1e-6)
         assert (some[0] == tokens[at]).all() and (some[2] == prob[at]).all()
+
+
+def test_a_workspace_holds_fewer_rows_and_smaller_vocabularies_too():
+    size = fb.sample_tokens_workspace
+    for V in (1, 1000, 4096, 4097, 16384, 16385, 32003, 126464, 200000, 1 << 20, (1 << 20) + 1, 1 << 21):
+        sizes = [size(n, V) for n in range(1, 140)] + [size(n, V) for n in (1000, 1024, 1025, 4096, 65535)]
+        assert sizes[0] > 0 and all(a <= b for a, b in zip(sizes, sizes[1:])), V
+    rng = np.random.default_rng(2)
+    for n in (1, 2, 3, 7, 8, 9, 16, 31, 64, 65, 1000):
+        vocabs = sorted({int(x) for x in np.exp(rng.uniform(0, math.log(1 << 21), 400))} | {16384 * i + j for i in range(1, 128) for j in (0, 1)})
+        sizes = [size(n, V) for V in vocabs]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])), n
+
+
+@pytest.mark.gpu
+def test_one_workspace_for_every_batch_up_to_the_largest():
+    n, V = 24, 126464
+    z = _logits(n, V, torch.bfloat16, 3).to(DEV)
+    u = torch.rand(n, device=DEV, generator=torch.Generator(device=DEV).manual_seed(4))
+    k = torch.full((n,), 40, dtype=torch.int32, device=DEV)
+    guard = 4096
+    size = fb.sample_tokens_workspace(n, V)
+    ws = torch.full((size + guard,), 0xab, dtype=torch.uint8, device=DEV)
+    want = None
+    for m in (24, 16, 9, 8, 4, 1):
+        out = (torch.full((m,), -7, dtype=torch.int32, device=DEV), torch.zeros(m, device=DEV), torch.zeros(m, device=DEV))
+        fb.sample_tokens(z[:m], None, u[:m], None, k[:m], None, None, *out, ws[:size])
+        want = out if want is None else want
+        assert torch.equal(out[0], want[0][:m]) and torch.equal(out[2], want[2][:m])
+        assert torch.allclose(out[1], want[1][:m], rtol=2.0 ** -19, atol=0)
+    assert (ws[size:] == 0xab).all()
