@@ -121,9 +121,13 @@ def _ptr(t) -> int | None:
     return None if t is None else t.data_ptr()
 
 
-def _stream() -> int:
+def _raw_stream(device: int) -> int:
     # the handle of torch.cuda.current_stream() without the object around it: 0.1 us instead of 2.7, a quarter of a short call's host time
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _stream() -> int:
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _stream_on(t: torch.Tensor) -> int:
@@ -131,7 +135,7 @@ def _stream_on(t: torch.Tensor) -> int:
     device = torch.cuda.current_device()
     if t.get_device() != device:
         raise ValueError(f"tensors on {t.device}, but the current device is cuda:{device}")
-    return torch._C._cuda_getCurrentRawStream(device)
+    return _raw_stream(device)
 
 
 def _need(t: torch.Tensor, dtype, name: str) -> None:
@@ -378,59 +382,148 @@ def make_quant_cache(k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor, v_ex
     the exponent bytes uint8 [H, M+N], which share their strides.  The tensors have to outlive the description."""
     for t, name in ((k, "k"), (v, "v"), (k_exp, "k_exp"), (v_exp, "v_exp")):
         _need(t, torch.uint8, name)
-    if k.shape != v.shape or k_exp.shape != k.shape[:2] or v_exp.shape != k.shape[:2]:
+    if k.dim() != 3 or k.shape != v.shape or k_exp.shape != k.shape[:2] or v_exp.shape != k.shape[:2]:
         raise ValueError("codes [H, rows, d] and exponents [H, rows] must agree")
+    if k.stride(2) != 1 or v.stride(2) != 1:
+        raise ValueError("codes: innermost stride must be 1")
     if k_exp.stride() != v_exp.stride():
         raise ValueError("k_exp and v_exp must share their strides")
-    return QuantCache(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), k_exp.stride(0), k_exp.stride(1))
+    if not k.get_device() == v.get_device() == k_exp.get_device() == v_exp.get_device():
+        raise ValueError("codes and exponents must be on one device")
+    cache = QuantCache(_ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp), k_exp.stride(0), k_exp.stride(1))
+    cache.sizes, cache.strides, cache.device, cache.fits = tuple(k.shape), (k.stride()[:2], v.stride()[:2]), k.get_device(), None
+    return cache
+
+
+# What the calls over such a cache check: that no kernel leaves a tensor.  A comparison each where everything is as it should be, since a step's calls
+# are a few microseconds long; what exactly is wrong, or only larger than it needs to be, is told in functions of their own.
+def _strides_fit(sizes, strides, stride_h: int, stride_n: int) -> bool:
+    """Whether these are the strides of [heads, rows, ...] (that of one head or one row means nothing)."""
+    return (strides[0] == stride_h or sizes[0] == 1) and (strides[1] == stride_n or sizes[1] == 1)
+
+
+def _check_shape(cache: QuantCache, s: Shape, device: int) -> None:
+    """Cache and shape belong together (a cache that a caller filled in by hand is taken as it is)."""
+    sizes = getattr(cache, "sizes", None)
+    if sizes is None:
+        return
+    k, v = cache.strides
+    if (sizes != (s.n_heads, s.n_ctx + s.n_resp, s.head_dim) or not _strides_fit(sizes, k, s.k_stride_h, s.k_stride_n)
+            or not _strides_fit(sizes, v, s.v_stride_h, s.v_stride_n)):
+        raise ValueError(f"shape and cache do not agree: the codes are {list(sizes)}, strides {k} and {v}")
+    if cache.device != device:
+        raise ValueError(f"cache on cuda:{cache.device}, but the current device is cuda:{device}")
+    cache.fits = (bytes(s), device)
+
+
+def _quant_device(cache: QuantCache, s: Shape, t: torch.Tensor) -> int:
+    """The current device, which a call's first tensor and its cache have to be on."""
+    device = torch.cuda.current_device()
+    if t.get_device() != device:
+        raise ValueError(f"tensors on {t.device}, but the current device is cuda:{device}")
+    if getattr(cache, "fits", None) != (bytes(s), device):
+        _check_shape(cache, s, device)
+    return device
+
+
+def _check_rows(device: int, *expected) -> None:
+    """bf16 tensors of at least these sizes, innermost stride 1."""
+    for t, name, sizes in expected:
+        if t.dtype != torch.bfloat16 or t.get_device() != device:
+            raise TypeError(f"{name}: expected a tensor of torch.bfloat16 on cuda:{device}, got {t.dtype} on {t.device}")
+        if t.dim() != 3 or any(n < least for n, least in zip(t.shape, sizes)) or t.stride(2) != 1:
+            raise ValueError(f"{name}: expected {list(sizes)}, innermost stride 1, got {list(t.shape)}, strides {t.stride()}")
+
+
+def _check_pair(device: int, a: torch.Tensor, b: torch.Tensor, names: str, sizes) -> None:
+    """Two such tensors with common strides."""
+    strides = a.stride()
+    if not (a.shape == sizes == b.shape and strides == b.stride() and strides[-1] == 1 and a.dtype == b.dtype == torch.bfloat16 and b.get_device() == device):
+        _check_rows(device, (a, "K_" + names, sizes), (b, "V_" + names, sizes))
+        if strides != b.stride():
+            raise ValueError(f"K_{names} and V_{names} must share their strides")
+
+
+def _check_values(device: int, *expected) -> None:
+    """At least so many values next to each other (None where none are needed)."""
+    for t, name, dtype, least in expected:
+        if t is None:
+            if least > 0:
+                raise ValueError(f"{name}: expected {least} values, got None")
+        elif not (t.dtype == dtype and t.get_device() == device and t.numel() >= least and t.is_contiguous()):
+            if t.dtype != dtype or t.get_device() != device:
+                raise TypeError(f"{name}: expected a tensor of {dtype} on cuda:{device}, got {t.dtype} on {t.device}")
+            raise ValueError(f"{name}: expected {least} values next to each other, got shape {list(t.shape)}, strides {t.stride()}")
+
+
+def _space(workspace: torch.Tensor | None, device: int) -> int:
+    """Bytes of a workspace."""
+    if workspace is None:
+        return 0
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: expected memory without gaps on cuda:{device}, got strides {workspace.stride()} on {workspace.device}")
+    return workspace.numel() * workspace.element_size()
 
 
 def quant_update(cache: QuantCache, shape: Shape, k_new, v_new, active_idx, counts, row_base: int) -> None:
     """cache_update into a quantised cache: k_new, v_new bf16 [H, max_active, d]."""
-    for t, name in ((k_new, "K_new"), (v_new, "V_new")):
-        _need(t, torch.bfloat16, name)
-    if k_new.stride() != v_new.stride() or k_new.stride(2) != 1:
-        raise ValueError("K_new and V_new must share their strides, innermost 1")
+    device, slots = _quant_device(cache, shape, k_new), active_idx.numel()
+    _check_pair(device, k_new, v_new, "new", (shape.n_heads, slots, shape.head_dim))
+    _check_values(device, (active_idx, "active_idx", torch.int32, 0), (counts, "counts", torch.int32, 0 if counts is None else 2))
     _check(lib().focus_quant_update(C.byref(cache), C.byref(shape), _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _ptr(active_idx),
-                                    _ptr(counts), active_idx.numel(), row_base, _stream_on(k_new)))
+                                    _ptr(counts), slots, row_base, _raw_stream(device)))
 
 
 def quant_refresh(cache: QuantCache, shape: Shape, k_new, v_new, kbar) -> None:
     """cache_refresh into a quantised cache; kbar fp32 [H, n_b, d] (or None): block means of the values it reads back as."""
-    for t, name in ((k_new, "K_new"), (v_new, "V_new")):
-        _need(t, torch.bfloat16, name)
-    if kbar is not None:
-        _need(kbar, torch.float32, "kbar")
-    if k_new.stride() != v_new.stride() or k_new.stride(2) != 1:
-        raise ValueError("K_new and V_new must share their strides, innermost 1")
-    _check(lib().focus_quant_refresh(C.byref(cache), C.byref(shape), _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _ptr(kbar), _stream_on(k_new)))
+    device, H, d = _quant_device(cache, shape, k_new), shape.n_heads, shape.head_dim
+    _check_pair(device, k_new, v_new, "new", (H, shape.n_ctx + shape.n_resp, d))
+    _check_values(device, (kbar, "kbar", torch.float32, 0 if kbar is None else H * _n_blocks(shape) * d))
+    _check(lib().focus_quant_refresh(C.byref(cache), C.byref(shape), _ptr(k_new), _ptr(v_new), k_new.stride(0), k_new.stride(1), _ptr(kbar),
+                                     _raw_stream(device)))
 
 
 def quant_read(cache: QuantCache, shape: Shape, first_row: int, k_out, v_out) -> None:
     """Rows first_row, ... of a quantised cache into k_out, v_out bf16 [H, rows, d]."""
-    for t, name in ((k_out, "K_out"), (v_out, "V_out")):
-        _need(t, torch.bfloat16, name)
-    if k_out.shape != v_out.shape or k_out.stride() != v_out.stride() or k_out.stride(2) != 1:
-        raise ValueError("K_out and V_out must share their shape and strides, innermost 1")
-    _check(lib().focus_quant_read(C.byref(cache), C.byref(shape), first_row, k_out.shape[1], _ptr(k_out), _ptr(v_out), k_out.stride(0), k_out.stride(1),
-                                  _stream_on(k_out)))
+    device, rows = _quant_device(cache, shape, k_out), k_out.shape[1]
+    _check_pair(device, k_out, v_out, "out", (shape.n_heads, rows, shape.head_dim))
+    _check(lib().focus_quant_read(C.byref(cache), C.byref(shape), first_row, rows, _ptr(k_out), _ptr(v_out), k_out.stride(0), k_out.stride(1),
+                                  _raw_stream(device)))
+
+
+def _n_blocks(shape: Shape) -> int:
+    return -(-shape.n_ctx // max(shape.block, 1))
+
+
+def _check_attention(device: int, s: Shape, q, active_idx, slots: int, counts, kept_blocks, n_keep: int, sink_idx, n_sink: int, out, lse) -> None:
+    """The tensors of an attention are what its shape and its counts say."""
+    H, d = s.n_heads, s.head_dim
+    if not (q.shape == (H, s.n_gen, d) and out.shape == (H, slots, d) and q.stride() == (s.q_stride_h, s.q_stride_n, 1)
+            and out.stride() == (s.o_stride_h, s.o_stride_n, 1) and q.dtype == out.dtype == torch.bfloat16 and out.get_device() == device):
+        _check_rows(device, (q, "Q", (H, s.n_gen, d)), (out, "out", (H, slots, d)))
+        if not _strides_fit(q.shape, q.stride(), s.q_stride_h, s.q_stride_n) or not _strides_fit(out.shape, out.stride(), s.o_stride_h, s.o_stride_n):
+            raise ValueError("Q and out must have the strides that the shape has for them")
+    i32 = torch.int32
+    _check_values(device, (active_idx, "active_idx", i32, 0), (kept_blocks, "kept_blocks", i32, n_keep), (sink_idx, "sink_idx", i32, n_sink),
+                  (counts, "counts", i32, 0 if counts is None else 2), (lse, "lse", torch.float32, 0 if lse is None else H * slots))
 
 
 def quant_attn(q, active_idx, counts, cache: QuantCache, shape: Shape, kept_blocks, n_keep: int, sink_idx, n_sink: int, out, lse, workspace) -> None:
     """sparse_attn over a quantised cache."""
-    _need(q, torch.bfloat16, "Q")
-    _need(out, torch.bfloat16, "out")
-    _check(lib().focus_quant_attn(_ptr(q), _ptr(active_idx), _ptr(counts), active_idx.numel(), C.byref(cache), C.byref(shape), _ptr(kept_blocks), n_keep,
-                                  _ptr(sink_idx), n_sink, _ptr(out), _ptr(lse), _ptr(workspace),
-                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_on(q)))
+    device, slots = _quant_device(cache, shape, q), active_idx.numel()
+    _check_attention(device, shape, q, active_idx, slots, counts, kept_blocks, n_keep, sink_idx, n_sink, out, lse)
+    _check(lib().focus_quant_attn(_ptr(q), _ptr(active_idx), _ptr(counts), slots, C.byref(cache), C.byref(shape), _ptr(kept_blocks), n_keep,
+                                  _ptr(sink_idx), n_sink, _ptr(out), _ptr(lse), _ptr(workspace), _space(workspace, device), _raw_stream(device)))
 
 
 def quant_layer(q, focus_idx, active_idx, counts, cache: QuantCache, kbar, shape: Shape, n_keep: int, sink_idx, n_sink: int, scores, kept_blocks, out,
                 lse, workspace) -> None:
     """sparse_layer over a quantised cache, from the block means that the block entry left behind."""
-    _need(q, torch.bfloat16, "Q")
-    _need(out, torch.bfloat16, "out")
-    _need(kbar, torch.float32, "kbar")
-    _check(lib().focus_quant_layer(_ptr(q), _ptr(focus_idx), _ptr(active_idx), _ptr(counts), focus_idx.numel(), active_idx.numel(), C.byref(cache),
+    device, slots = _quant_device(cache, shape, q), active_idx.numel()
+    _check_attention(device, shape, q, active_idx, slots, counts, kept_blocks, n_keep, sink_idx, n_sink, out, lse)
+    n_b = _n_blocks(shape)
+    _check_values(device, (focus_idx, "focus_idx", torch.int32, 1), (kbar, "kbar", torch.float32, shape.n_heads * n_b * shape.head_dim),
+                  (scores, "scores", torch.float32, 0 if scores is None else n_b))
+    _check(lib().focus_quant_layer(_ptr(q), _ptr(focus_idx), _ptr(active_idx), _ptr(counts), focus_idx.numel(), slots, C.byref(cache),
                                    _ptr(kbar), C.byref(shape), n_keep, _ptr(sink_idx), n_sink, _ptr(scores), _ptr(kept_blocks), _ptr(out), _ptr(lse),
-                                   _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_on(q)))
+                                   _ptr(workspace), _space(workspace, device), _raw_stream(device)))

@@ -514,3 +514,142 @@ def test_another_device_than_the_current_one_is_refused(monkeypatch):
                  lambda: fb.quant_layer(rows, i32([0]), i32([0]), None, c.struct, rows.float(), s, 1, None, 0, None, i32([0]), rows, None, ws)):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+# ---- what the wrappers refuse, without a GPU: tensors that say that they are on one, and a library that notes its calls
+class _Claims(torch.Tensor):
+    is_cuda = True
+    where = 0
+
+    def get_device(self):
+        return self.where
+
+
+class _Noted:
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        return lambda *a: self.calls.append(name) or fb.FOCUS_OK
+
+
+def _on(t, where=0):
+    t = t.as_subclass(_Claims)
+    t.where = where
+    return t
+
+
+@pytest.fixture
+def noted(monkeypatch):
+    library = _Noted()
+    monkeypatch.setattr(fb, "lib", lambda: library)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    return library.calls
+
+
+H_, M_, N_, D_, B_, GEN_, SLOTS_ = 3, 70, 10, 64, 16, 12, 5
+
+
+def _calls():
+    """Arguments that fit, by name, of every wrapper over one cache."""
+    u8, bf = lambda *s: _on(torch.zeros(s, dtype=torch.uint8)), lambda *s: _on(torch.zeros(s, dtype=torch.bfloat16))
+    i32_, f32 = lambda n: _on(torch.zeros(n, dtype=torch.int32)), lambda *s: _on(torch.zeros(s))
+    k, v, n_b = u8(H_, M_ + N_, D_), u8(H_, M_ + N_, D_), -(-M_ // B_)
+    cache = fb.make_quant_cache(k, v, u8(H_, M_ + N_), u8(H_, M_ + N_))
+    q, out = bf(H_, GEN_, D_), bf(H_, SLOTS_, D_)
+    both = dict(cache=cache, shape=fb.make_shape(q, k, v, M_, B_, out))
+    update = dict(both, k_new=bf(H_, SLOTS_, D_), v_new=bf(H_, SLOTS_, D_), active_idx=i32_(SLOTS_), counts=i32_(2), row_base=M_)
+    refresh = dict(both, k_new=bf(H_, M_ + N_, D_), v_new=bf(H_, M_ + N_, D_), kbar=f32(H_, n_b, D_))
+    read = dict(both, first_row=3, k_out=bf(H_, 9, D_), v_out=bf(H_, 9, D_))
+    attn_ = dict(both, q=q, active_idx=i32_(SLOTS_), counts=i32_(2), kept_blocks=i32_(2), n_keep=2, sink_idx=i32_(3), n_sink=3, out=out, lse=f32(H_, SLOTS_),
+                 workspace=u8(4096))
+    layer = dict(attn_, focus_idx=i32_(4), kbar=f32(H_, n_b, D_), scores=f32(n_b))
+    return k, v, {fb.quant_update: update, fb.quant_refresh: refresh, fb.quant_read: read, fb.quant_attn: attn_, fb.quant_layer: layer}
+
+
+def test_wrappers_take_what_fits(noted):
+    _, _, calls = _calls()
+    for n, (call, args) in enumerate(calls.items()):
+        call(**args)
+        for name, t in args.items():  # more rows than a call needs, and what it does not need
+            if isinstance(t, torch.Tensor) and name in ("k_new", "v_new", "out", "lse", "kept_blocks", "sink_idx", "counts", "kbar", "scores", "workspace"):
+                if name not in ("k_new", "v_new", "out"):
+                    call(**{**args, name: _on(torch.zeros((t.numel() + 8,), dtype=t.dtype))})
+        for name in ("counts", "lse", "scores", "workspace") + (("kbar",) if call is fb.quant_refresh else ()):
+            if name in args:
+                call(**{**args, name: None})
+        if "sink_idx" in args:
+            call(**{**args, "sink_idx": None, "n_sink": 0})
+    rows = _on(torch.zeros((2, H_ + 1, SLOTS_ + 4, D_ + 8), dtype=torch.bfloat16))
+    fb.quant_update(**{**calls[fb.quant_update], "k_new": rows[0], "v_new": rows[1]})
+    assert set(noted) == {c.__name__.replace("quant", "focus_quant") for c in calls}
+
+
+def test_wrappers_refuse_tensors_that_the_kernels_would_leave(noted):
+    """Fewer heads, rows, columns or values than the shape and the lists say, other types, other strides, other devices: nothing is called."""
+    k, v, calls = _calls()
+    bad_calls = []
+    for call, args in calls.items():
+        for name, t in args.items():
+            if not isinstance(t, torch.Tensor):
+                continue
+            bad = [_on(t, 1)]  # another device
+            if t.dtype != torch.uint8:  # (a workspace's type means nothing, its size is the library's to judge)
+                bad.append(_on(torch.zeros(t.shape, dtype=torch.int64)))
+            if t.dim() == 3 and t.dtype == torch.bfloat16:
+                pair = {"k_new": "v_new", "v_new": "k_new", "k_out": "v_out", "v_out": "k_out"}.get(name)
+                for axis in range(3):
+                    if (call is fb.quant_read or name == "q") and axis == 1:
+                        continue  # (its rows are the call's)
+                    less = list(t.shape)
+                    less[axis] -= 1
+                    small = _on(torch.zeros(t.shape, dtype=t.dtype)[:less[0], :less[1], :less[2]])
+                    bad_calls.append((call, {**args, name: small}))
+                    if pair:
+                        bad_calls.append((call, {**args, name: small, pair: small}))
+                bad.append(_on(torch.zeros((*t.shape[:2], 2 * t.shape[2]), dtype=t.dtype)[..., ::2]))
+                bad.append(_on(torch.zeros((t.shape[0], t.shape[1], t.shape[2] + 8), dtype=t.dtype)[..., :-8]))  # not those of the other or of the shape
+                bad.append(t[0])
+            elif name != "workspace" and name not in ("active_idx", "focus_idx"):
+                bad.append(_on(torch.zeros(t.numel() - 1, dtype=t.dtype)))
+                bad.append(_on(torch.zeros(2 * t.numel(), dtype=t.dtype)[::2]))
+            else:
+                bad.append(_on(torch.zeros(2 * t.numel(), dtype=t.dtype)[::2]))
+            bad_calls += [(call, {**args, name: b}) for b in bad]
+        s = args["shape"]
+        for field, value in (("n_heads", H_ + 1), ("n_heads", H_ - 1), ("n_ctx", M_ + 1), ("n_resp", N_ + 7), ("head_dim", 128), ("k_stride_h", 1 << 20),
+                             ("k_stride_n", 128), ("v_stride_h", 16), ("v_stride_n", 192)):
+            other = fb.Shape.from_buffer_copy(s)
+            setattr(other, field, value)
+            bad_calls.append((call, {**args, "shape": other}))
+        if call in (fb.quant_attn, fb.quant_layer):
+            for field, value in (("n_gen", GEN_ + 1), ("q_stride_h", 1 << 20), ("q_stride_n", 128), ("o_stride_h", 1 << 20), ("o_stride_n", 128)):
+                other = fb.Shape.from_buffer_copy(s)
+                setattr(other, field, value)
+                bad_calls.append((call, {**args, "shape": other}))
+            bad_calls += [(call, {**args, "kept_blocks": None}), (call, {**args, "n_keep": 3}), (call, {**args, "sink_idx": None}), (call, {**args, "n_sink": 4}),
+                          (call, {**args, "active_idx": _on(torch.zeros(SLOTS_ + 1, dtype=torch.int32))})]
+        if call is fb.quant_update:
+            bad_calls.append((call, {**args, "active_idx": _on(torch.zeros(SLOTS_ + 1, dtype=torch.int32))}))
+    for call, args in bad_calls:
+        with pytest.raises((TypeError, ValueError)):
+            call(**args)
+    assert noted == [] and len(bad_calls) > 150
+    exps = _on(torch.zeros((H_, M_ + N_), dtype=torch.uint8))
+    for bad in ((k[..., ::2], v[..., ::2], exps, exps), (k, v, exps, _on(exps, 1)), (k, _on(v.clone(), 1), exps, exps), (k, v, exps[:, 1:], exps), (k[0], v[0], exps, exps)):
+        with pytest.raises(ValueError):
+            fb.make_quant_cache(*bad)
+
+
+def test_strides_of_one_head_or_one_row_mean_nothing(noted):
+    u8 = lambda *s: _on(torch.zeros(s, dtype=torch.uint8))
+    k, v, e = u8(1, 40, 64), u8(1, 40, 64), u8(1, 40)
+    cache = fb.make_quant_cache(k, v, e, e)
+    q = _on(torch.zeros((1, 9, 64), dtype=torch.bfloat16))
+    out = _on(torch.zeros((1, 1, 64), dtype=torch.bfloat16))
+    shape = fb.make_shape(q, k, v, 40, 8, out)
+    shape.k_stride_h = shape.q_stride_h = shape.o_stride_h = shape.o_stride_n = 1 << 20
+    one = _on(torch.zeros(1, dtype=torch.int32))
+    fb.quant_attn(q, one, None, cache, shape, one, 1, None, 0, out, None, None)
+    assert noted == ["focus_quant_attn"]
