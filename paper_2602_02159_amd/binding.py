@@ -130,12 +130,12 @@ def _stream() -> int:
     return _raw_stream(torch.cuda.current_device())
 
 
-def _stream_on(t: torch.Tensor) -> int:
-    """_stream() for a call on the tensor `t`: kernels run on the current device, so that is the one it has to be on."""
+def _device_of(t: torch.Tensor, name: str = "tensors") -> int:
+    """The current device: kernels run there, so `t` has to be there."""
     device = torch.cuda.current_device()
     if t.get_device() != device:
-        raise ValueError(f"tensors on {t.device}, but the current device is cuda:{device}")
-    return _raw_stream(device)
+        raise ValueError(f"{name} on {t.device}, but the current device is cuda:{device}")
+    return device
 
 
 def _need(t: torch.Tensor, dtype, name: str) -> None:
@@ -291,20 +291,22 @@ def sample_tokens(logits, masked, uniform, temperature, top_k, top_p, min_p, tok
         raise TypeError(f"logits: expected a CUDA tensor of bfloat16 or float32, got {logits.dtype} on {logits.device}")
     if logits.dim() != 2 or logits.stride(1) != 1:
         raise ValueError("logits: expected [n_rows, vocab], innermost stride 1")
+    device = _device_of(logits)
     rows, vocab = logits.shape[:1], logits.shape[1]
     stride = logits.stride(0) if rows[0] > 1 else (vocab + 7) // 8 * 8  # (of one row any will do)
     for t, dtype, name in ((uniform, torch.float32, "uniform"), (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
                            (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"), (tokens, torch.int32, "tokens"), (conf, torch.float32, "conf"),
                            (prob, torch.float32, "prob")):
-        if t is not None and not (t.dtype == dtype and t.is_cuda and t.shape == rows and t.is_contiguous()):
+        if t is not None and not (t.dtype == dtype and t.get_device() == device and t.shape == rows and t.is_contiguous()):
             _need(t, dtype, name)
+            _device_of(t, name)
             if t.shape != rows or not t.is_contiguous():
                 raise ValueError(f"{name}: expected {rows[0]} values next to each other, got shape {tuple(t.shape)}, strides {t.stride()}")
-    if masked is not None and (not masked.is_cuda or masked.element_size() != 1 or masked.shape != rows or not masked.is_contiguous()):
-        raise ValueError(f"masked: expected {rows[0]} bytes on the GPU, got {masked.dtype}, shape {tuple(masked.shape)} on {masked.device}")
+    if masked is not None and (masked.get_device() != device or masked.element_size() != 1 or masked.shape != rows or not masked.is_contiguous()):
+        raise ValueError(f"masked: expected {rows[0]} bytes on cuda:{device}, got {masked.dtype}, shape {tuple(masked.shape)} on {masked.device}")
     _check(lib().focus_sample_tokens(_ptr(logits), int(logits.dtype == torch.float32), stride, _ptr(masked), _ptr(uniform), _ptr(temperature),
                                      _ptr(top_k), _ptr(top_p), _ptr(min_p), rows[0], vocab, _ptr(tokens), _ptr(conf), _ptr(prob),
-                                     _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_on(logits)))
+                                     _ptr(workspace), _space(workspace, device), _raw_stream(device)))
 
 
 def cache_update(k_cache, v_cache, shape: Shape, k_new, v_new, active_idx, counts, row_base: int) -> None:
@@ -418,9 +420,7 @@ def _check_shape(cache: QuantCache, s: Shape, device: int) -> None:
 
 def _quant_device(cache: QuantCache, s: Shape, t: torch.Tensor) -> int:
     """The current device, which a call's first tensor and its cache have to be on."""
-    device = torch.cuda.current_device()
-    if t.get_device() != device:
-        raise ValueError(f"tensors on {t.device}, but the current device is cuda:{device}")
+    device = _device_of(t)
     if getattr(cache, "fits", None) != (bytes(s), device):
         _check_shape(cache, s, device)
     return device

@@ -370,3 +370,41 @@ def test_one_workspace_for_every_batch_up_to_the_largest():
         assert torch.equal(out[0], want[0][:m]) and torch.equal(out[2], want[2][:m])
         assert torch.allclose(out[1], want[1][:m], rtol=2.0 ** -19, atol=0)
     assert (ws[size:] == 0xab).all()
+
+
+def test_tensors_of_more_than_one_device_are_refused(monkeypatch):
+    """Without a GPU: tensors that say that they are on one, and a library that notes its calls."""
+    class Claims(torch.Tensor):
+        is_cuda = True
+        where = 0
+
+        def get_device(self):
+            return self.where
+
+    def on(t, where=0):
+        t = t.as_subclass(Claims)
+        t.where = where
+        return t
+
+    calls = []
+
+    class Noted:
+        def __getattr__(self, name):
+            return lambda *a: calls.append(name) or fb.FOCUS_OK
+
+    monkeypatch.setattr(fb, "lib", Noted)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 0, raising=False)
+    n, V = 3, 16
+    f32, i32 = lambda: on(torch.zeros(n)), lambda: on(torch.zeros(n, dtype=torch.int32))
+    args = dict(logits=on(torch.zeros((n, V), dtype=torch.bfloat16)), masked=on(torch.ones(n, dtype=torch.uint8)), uniform=f32(), temperature=f32(), top_k=i32(),
+                top_p=f32(), min_p=f32(), tokens=i32(), conf=f32(), prob=f32(), workspace=on(torch.zeros(1 << 16, dtype=torch.uint8)))
+    for name, t in args.items():
+        with pytest.raises(ValueError):
+            fb.sample_tokens(**{**args, name: on(t.clone(), 1)})
+    with pytest.raises(ValueError):
+        fb.sample_tokens(**{**args, "workspace": on(torch.zeros(1 << 16, dtype=torch.uint8)[::2])})
+    assert calls == []
+    fb.sample_tokens(**args)
+    fb.sample_tokens(**{**args, "masked": None, "conf": None, "top_k": None})
+    assert calls == ["focus_sample_tokens"] * 2
