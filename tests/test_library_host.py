@@ -154,3 +154,26 @@ def test_missing_library_fails_loudly(monkeypatch, tmp_path):
         fb.lib()
     with pytest.raises(FileNotFoundError):
         fb.helper_k(4.0, 1)
+
+
+def test_the_current_stream_without_the_private_function(monkeypatch):
+    """torch's handle of the current stream comes from a function that is not part of its interface: one without it works as well."""
+    import types
+
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: types.SimpleNamespace(cuda_stream=100 + (3 if device is None else device)))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 200 + device, raising=False)
+    assert fb._stream() == 203
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    assert fb._stream() == 103
+
+
+@pytest.mark.gpu
+def test_the_stream_of_a_call_is_the_current_one():
+    import torch
+    assert fb._stream() == torch.cuda.current_stream().cuda_stream
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        assert fb._stream() == side.cuda_stream != torch.cuda.default_stream().cuda_stream
+    assert fb._stream() == torch.cuda.current_stream().cuda_stream
