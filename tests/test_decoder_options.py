@@ -6,6 +6,7 @@ import torch
 from oracle import step_oracle as so
 from paper_2602_02159_amd import binding as fb
 from paper_2602_02159_amd.step import FocusDecoder
+from tests.test_quant_cache import check_attention, key_set
 
 DEV = "cuda:0"
 LAYERS, L_DENSE, TAIL, H, D, M, N, GEN, BLOCK, K, WINDOW, KEEP, SINKS, VOCAB = 5, 1, 1, 4, 128, 900, 64, 32, 64, 4, 2, 5, 6, 5003
@@ -97,6 +98,42 @@ def test_replayed_graphs_give_what_eager_calls_give():
                 dec.run_step()
         for a, b in zip(_buffers(eager), _buffers(graph)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_a_steps_layers_are_the_single_calls_bit_for_bit():
+    """Over the caches that the step leaves behind, with its lists: no sink, block, query or row of them may be missing.  And against the fp64
+    attention over exactly those keys, whose bounds scale with what is attended."""
+    dec = _make()
+    _fill(dec, 5)
+    dec.run_entry()
+    dec.run_step()
+    n, focus = int(dec.counts[1]), int(dec.counts[0])
+    active, sinks = dec.active_idx[:n].cpu().numpy(), dec.sink_idx.tolist()
+    assert len(set(sinks)) == SINKS and n > 1 and focus > 0
+    for l in range(LAYERS):
+        out, lse = torch.full_like(dec.out[l], 7.0), torch.zeros((H, dec.max_active), device=DEV)
+        s = fb.make_shape(dec.q[l], dec.k_cache[l], dec.v_cache[l], M, BLOCK, out)
+        if dec.is_sparse(l):
+            scores, kept = torch.zeros_like(dec.scores[l]), torch.zeros_like(dec.kept[l])
+            ws = torch.empty(fb.workspace_bytes(fb.FN_QUANT_LAYER, s, dec.max_active, KEEP, SINKS), dtype=torch.uint8, device=DEV)
+            fb.quant_layer(dec.q[l], dec.focus_idx, dec.active_idx, dec.counts, dec.caches[l], dec.kbar[l], s, KEEP, dec.sink_idx, SINKS, scores, kept, out,
+                           lse, ws)
+            assert torch.equal(kept, dec.kept[l]) and torch.equal(scores, dec.scores[l])
+            keys = key_set(M, N, BLOCK, kept.tolist(), sinks)
+        elif dec.quantised[l]:
+            ws = torch.empty(fb.workspace_bytes(fb.FN_QUANT_ATTN, s, dec.max_active, dec.n_b, 0), dtype=torch.uint8, device=DEV)
+            fb.quant_attn(dec.q[l], dec.active_idx, dec.counts, dec.caches[l], s, dec.all_blocks, dec.n_b, None, 0, out, lse, ws)
+            keys = np.arange(M + N)
+        else:
+            mass, found = torch.zeros_like(dec.col_mass), torch.zeros_like(dec.sink_idx)
+            ws = torch.empty(fb.workspace_bytes(fb.FN_PROBE_LAYER, s, dec.max_active, 0, SINKS), dtype=torch.uint8, device=DEV)
+            fb.probe_layer(dec.q[l], dec.active_idx, dec.counts, dec.k_cache[l], dec.v_cache[l], s, SINKS, out, lse, mass, found, ws)
+            assert torch.equal(mass, dec.col_mass) and torch.equal(found, dec.sink_idx)
+            keys = np.arange(M + N)
+        assert torch.equal(out[:, :n], dec.out[l][:, :n]), l
+        k, v = dec.read_cache(l)
+        check_attention(dec.out[l], lse, dec.q[l], k, v, active, keys)
 
 
 def test_options_that_do_not_go_together():
