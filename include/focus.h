@@ -308,7 +308,7 @@ typedef enum focus_dtype { FOCUS_BF16 = 0, FOCUS_F32 = 1 } focus_dtype;
  *   prob     [dev] fp32[n_rows] out or NULL: probability with which it was drawn, among the kept tokens
  *   workspace  [dev] focus_sample_tokens_workspace(n_rows, vocab) bytes, 16-byte aligned; nothing is assumed about its contents
  * Results are the same from call to call, and a row's token and prob whatever rows are beside it; conf, whose sum is of floats, is good to 2^-20
- * and may differ in its last bits with n_rows.  1 <= n_rows <= 65535, 1 <= vocab <= 2097152.
+ * (0 for a token whose weight at temperature 1 is below 2^-126) and may differ in its last bits with n_rows.  1 <= n_rows <= 65535, 1 <= vocab <= 2097152.
  */
 int focus_sample_tokens(const void* logits, int32_t dtype, int64_t row_stride, const uint8_t* masked, const float* uniform,
                         const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, int32_t n_rows,

@@ -143,7 +143,7 @@ __device__ __forceinline__ float weight(float z, float top, const Scale& s) {
   }
   r += __builtin_fmaf(d, s.hi, -x);
   const float w = __builtin_amdgcn_exp2f(-x);
-  return x < 60.f ? __builtin_fmaf(w * -0.6931471805599453f, r, w) : 0.f;
+  return x < 126.f ? __builtin_fmaf(w * -0.6931471805599453f, r, w) : 0.f;  // (a mass is none from 43 on, a confidence counts as far as floats go)
 }
 // 0 <= w < 512 in units of 2^-42, to nearest: the doubles of [1024, 2048) are 2^-42 apart
 __device__ __forceinline__ uint64_t mass_of(float w) {

@@ -408,3 +408,18 @@ def test_tensors_of_more_than_one_device_are_refused(monkeypatch):
     fb.sample_tokens(**args)
     fb.sample_tokens(**{**args, "masked": None, "conf": None, "top_k": None})
     assert calls == ["focus_sample_tokens"] * 2
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("V", [3, 20000])  # (20000 logits of nearly the same share: ends that are searched for in the whole row)
+def test_the_confidence_of_a_token_far_below_the_largest(V, dtype):
+    """At a temperature of 100 a token 85 below the largest is drawn nearly as often: its confidence, at temperature 1, is exp(-85) of the sum, 2^-122.6."""
+    for down in (40.0, 42.0, 60.0, 85.0):
+        z = torch.full((2, V), -down, dtype=dtype)
+        z[:, 0] = 0.0
+        tokens, conf, prob = run(z, np.float32(0.75), 100.0, 0, np.array([1.0, 0.97], dtype=np.float32))
+        for i, p in enumerate((1.0, float(np.float32(0.97)))):
+            t, c, q = so.sample_token(z[i].double().numpy(), 0.75, 100.0, 0, p, 0.0)
+            assert t > 0 and tokens[i] == t
+            assert abs(conf[i] - c) <= 2.0 ** -20 * c and abs(prob[i] - q) <= 2.0 ** -20 * q
