@@ -103,8 +103,10 @@ SplitPlan plan_attention(const focus_shape& s, int max_active, int n_keep, int n
 // per compute unit, whose half as many partial results outweigh its fewer requests under way (256 and 512 workgroups: 16 queries, 32 heads,
 // 32 832 keys 52.0 and 52.4 us, 16 448 keys 32.6 and 33.5; 28 queries, 32 832 keys 53.5 and 57.3; 25 queries, half of 512 blocks 38.8 and 41.8;
 // 8 heads, 28 queries, 16 448 keys 17.8 and 20.8); d = 64, and query groups, two (d = 64, 32 832 keys 41.9 and 31.7; 175 queries as above 30.1 and 25.8).
-// Rows that are read once and are more than the memory-side cache holds pass the caches by (32 heads, 32 832 keys, 16 queries 56.0 -> 53.9 us, one
-// query 54.6 -> 50.5); fewer may still be there from another call (half of 512 blocks, 139 MB, three layers in turn 41.7 -> 47.3).
+// Rows of more than 200 MB pass the caches by: the memory-side cache does not hold them until the next call.  Through the caches and past them, 16 queries,
+// 32 heads: four layers in turn, 34 MB of keys a layer 13.4 and 14.3 us, 67 MB 19.1 and 19.9, 101 MB 26.4 and 24.8, 134 MB 32.5 and 30.1, 168 MB 38.4 and 35.6,
+// 201 MB 43.5 and 40.9, 235 MB 50.0 and 47.0, 268 MB 53.9 and 50.6, 403 MB 77.0 and 71.3; one layer over and over 134 MB 28.1 and 29.9, 201 MB 37.1 and 40.1,
+// 268 MB 47.7 and 49.8, 403 MB 78.2 and 71.0.  (Half of 512 blocks, 139 MB, three layers in turn 41.7 and 47.3.)
 constexpr int kQuantGroups = 512, kQuantGroupsLoop = 256;
 constexpr int64_t kQuantStreamBytes = 200000000;
 SplitPlan plan_quant_attention(const focus_shape& s, int max_active, int n_keep, int n_sink) {

@@ -102,7 +102,9 @@ __global__ __launch_bounds__(256) void quant_update_kernel(const CacheUpdate u, 
 }
 
 // The same of a long list, which is compared with itself once for several heads: every entry behind the workgroup's first slot is read by
-// one thread and compared with all its slots.
+// one thread and compared with all its slots.  By its bytes 4096 rows of 32 heads would take 20 us and 32 768 rows 158, at the rate of a copy, and not
+// 26.5 and 207: the copy waits for the comparison, quadratic in the length of the list (32 768 entries: 5e8 pairs, some 40 us by the
+// instructions).  (At d = 64 the slots' 32 positions are more scalars than fit; lanes of vector registers hold what is left over.)
 template <int D>
 __global__ __launch_bounds__(256) void quant_update_many_kernel(const CacheUpdate u, const QuantCache q, int heads) {
   constexpr int kChunks = D / 8, kSlots = 256 / kChunks, kAhead = 2;
@@ -136,7 +138,6 @@ __global__ __launch_bounds__(256) void quant_update_many_kernel(const CacheUpdat
   const bool live = a < n_act && i >= 0 && row >= 0 && row < u.n_rows && !((again_sh >> j) & 1u);
   const int64_t at = live ? row : 0;
   const int h0 = (int)blockIdx.y * heads, h1 = min(h0 + heads, u.n_heads);
-#pragma unroll 2
   for (int h = h0; h < h1; ++h) {
     const int64_t src = (int64_t)h * u.nsh + (int64_t)slot * u.nsn + c * 8, e = (int64_t)h * q.esh + at * q.esn;
     const uint4 k = *reinterpret_cast<const uint4*>(u.Kn + src);

@@ -243,9 +243,13 @@ __device__ __forceinline__ uint32_t min_p_key(float min_p, double down, float to
 }
 
 // The whole row by one workgroup that walks it as often as it takes: the order is searched bit by bit.  What is kept is
-// {key > cut} and of {key == cut} the ids up to `last_id`.  For the rows that the lists below do not hold: logits so
-// alike that thousands lie within 1/16 of T where an end is.  A pass is bound by what one compute unit computes, so passes are what counts: bf16,
-// 126 464 logits, top_p 550 us a row, as long for 64 (one bit of the order a pass, and of the ids: 1331).
+// {key > cut} and of {key == cut} the ids up to `last_id`.  For the rows that the lists below do not hold, which are more than
+// those of logits all alike.  Normal logits, top_p 0.7 to 0.9: more than 4096 tokens lie within 1/16 of T where the end is at a spread over T of 0.5 and
+// less for 126 464 (64 rows: in some of them at 0.75), of 1 for 200 000, 1.5 for 262 144, 2 for a million.  And where top_p is close to
+// 1 and ends among the many tokens of small weight, or nearer to the last than the bins' error: 126 464 at a spread of 3, from 0.999 on.
+// A pass is bound by what one compute unit computes, so passes are what counts: 126 464 logits, top_p: 517 us a row, as float32 962 (33 where the lists
+// hold the end); 64 rows 549 to 558; 32 003 170 and 301; 200 000 840; a million 3.7 ms (65 us).  (One bit of the order a pass, and of the ids, took
+// two and a half times as long.)
 constexpr int kRowThreads = 512;
 template <class T>
 __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t* sh2, uint64_t* wave_mass, int* found) {
@@ -453,18 +457,19 @@ __device__ void search_row(const SampleArgs& a, int row, uint64_t* sh, uint64_t*
 // below 2^-24 of its chunk's sum then got no share.)  Where the lists do not hold the tokens of a bin, or the bins do not resolve
 // the logits (2^18 and more, at T = 1), the last launch searches the row instead.
 //
-// What bounds it.  One row of 126 464: three launches of 4.5, 9.9 and 9.2 us, each a chain of round trips (3.5, 2.6 and 2.4 where the largest
-// logit is taken).  64 such rows (bf16, 16 MB, three
-// quarters of them drawn from) 13.6, 15.0 and 9.9 us, 511 rows of 32 003 (float32, 65 MB) 26.0, 29.0 and 15.4: the arithmetic on each logit,
-// 50 to 60 instructions in either of the first two where the bulk of a row carries the mass, at a quarter to a half of the rate at
-// which HBM would deliver.  One workgroup that keeps a whole row in registers through all three parts (up to 65 536 bf16 logits) saves two
+// What bounds it.  One row of 126 464: three launches of 3.9, 10.5 and 8.7 us, each a chain of round trips (3.3, 2.4 and 2.1 where the largest
+// logit is taken).  64 such rows (bf16, 16 MB, three quarters of them drawn from) 11.2, 16.6 and 9.7 us, 511 rows of 32 003 (float32,
+// 65 MB) 20.8, 38.9 and 14.8: the arithmetic on each logit, an exponential, a bin and an atomic in the first launch, a weight with
+// its rounding kept and its mass in the second where the bulk of a row carries the mass, at a quarter to a half of the rate at which
+// HBM would deliver (511 float32 rows without a filter 55.5 us a call, of which the largest are taken 30.4).  One workgroup that keeps a whole row in registers through all three parts (up to 65 536 bf16 logits) saves two
 // launches and the second read, and is slower: it holds 128 registers and 68 KB of LDS and computes the same, with fewer wavefronts to hide
 // the parts in which one waits (511 rows 72 -> 81 us).
 // =====================================================================================================
 constexpr int kBins = 512;
 constexpr int kScanThreads = 512;
 constexpr int kSlice = 32 * kScanThreads, kSliceSmall = 8 * kScanThreads;  // logits of a workgroup
-constexpr int kSliceList = 2048, kRowList = 4096;                          // entries of a slice, of a row
+// Entries of the list of a slice and of a row: what eight tokens a thread hold in the last launch, 32 KB of its LDS; 16 KB of workspace a slice.
+constexpr int kSliceList = 2048, kRowList = 4096;
 constexpr int kSegChunks = 64;
 constexpr int kMaxSlices = kSampleMaxVocab / kSlice;
 constexpr float kMostBin = 4194304.f;                       // beyond, floats would not hold bin numbers and their neighbours
@@ -940,7 +945,9 @@ __device__ __forceinline__ End find_end(const uint64_t (&order)[RUN], const uint
   }
 }
 
-constexpr int kRankMost = 512, kRankAhead = 8;  // tokens that are ranked each against every other; LDS reads under way
+// Tokens that are ranked each against every other, a thread's one at most; LDS reads under way.  (Lists of 65 to 512 narrowed instead: 511 float32
+// rows of 32 003, top_p 0.9 70.0 -> 75.6 us, 0.95 73.5 -> 76.9; 64 bf16 rows of 126 464, top_k 50 to 800 within 0.3 us.)
+constexpr int kRankMost = 512, kRankAhead = 8;
 // SEGS: the most segments of a row; fewer leave LDS for a second workgroup per compute unit.
 constexpr int kFewSegs = 1024, kMaxSegs = kSampleMaxVocab / (kSegChunks * 4);
 template <class T, int SEGS>
@@ -1166,7 +1173,11 @@ struct SamplePlan {
   int slice, slices, segs, rows;  // logits of a slice; rows of a pass
   size_t stat, bins, rest, listed, list, cut, seg, total;
 };
-constexpr int kSmallPlans = 64, kMostRows = 1024, kMostRowSlices = 4096;  // slices of kSlice of a call that takes quarters; rows and slices of a pass
+// Slices of kSlice of a call that takes quarters instead: a quarter of the work a workgroup, and four times the histograms to add up.  Top_k 50, top_p
+// 0.95, slices and quarters: 126 464 logits, 1 row (8 slices) 27.1 and 23.3 us, 8 rows 28.4 and 24.9, 12 28.4 and 28.2, 24 29.2 and 33.3, 64 37.3 and 57.2;
+// 32 003, 1 row (2 slices) 26.3 and 21.3, 32 rows 28.0 and 23.5, 64 28.7 and 27.1, 128 29.2 and 37.3.
+constexpr int kSmallPlans = 64;
+constexpr int kMostRows = 1024, kMostRowSlices = 4096;  // rows and slices of a pass
 // Where the parts of a workspace lie for so many rows, slices of all rows and segments of all rows.
 static void place_parts(SamplePlan& p, size_t rows, size_t n, size_t segs) {
   size_t off = 0;

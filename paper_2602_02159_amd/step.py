@@ -203,10 +203,11 @@ class FocusDecoder:
     `row_base` is the cache row of position 0 of the generation block.
 
     `quantised`: the caches of all layers but the probe layer, whose logits choose the sinks of the others, hold eight-bit rows
-    (uint8 k_cache[l] / v_cache[l] with k_exp[l] / v_exp[l]); the entry then is focus_refresh_attn and focus_quant_refresh, a step's layers are
-    focus_quant_update and focus_quant_attn (every block kept) or focus_quant_layer.  read_cache(l) gives such rows back as bf16.
-    `sample` (with vocab): the step draws its tokens, focus_sample_tokens in the place of focus_token_confidence, from uniform [n_gen] with
-    temperature, top_k, top_p, min_p [n_gen], which the caller fills (1, 0, 1, 0 at first) -> tokens, conf, prob.
+    (uint8 k_cache[l] / v_cache[l] with k_exp[l] / v_exp[l]); the entry then is focus_quant_refresh and focus_refresh_attn over the new states, a
+    step's layers are focus_quant_update and focus_quant_attn (every block kept) or focus_quant_layer, in calls of their own.  read_cache(l) gives
+    such rows back as bf16.  The buffers of the entry's states (q_all, k_all, v_all, out_all) are bf16 either way.
+    `sample` (with vocab): the step draws its tokens from the bf16 logits, focus_sample_tokens in the place of focus_token_confidence, from uniform
+    [n_gen] with temperature, top_k, top_p, min_p [n_gen], which the caller fills (1, 0, 1, 0 at first) -> tokens, conf, prob.
     """
 
     def __init__(self, n_layers: int, l_dense: int, dense_tail: int, n_heads: int, head_dim: int, n_ctx: int, n_resp: int,
