@@ -28,6 +28,11 @@
  * and for a KV cache of eight-bit values:
  *     focus_quant_update, focus_quant_refresh, focus_quant_read   write and read such a cache
  *     focus_quant_attn, focus_quant_layer                         focus_sparse_attn and focus_sparse_layer over it
+ * and for the steps of many requests, whose caches are lists of pages:
+ *     focus_rotary           rows turned by their positions: Q and K_new as every entry point takes them
+ *     focus_paged_append     new K/V states of every request -> its pages, K (and Q) turned on the way
+ *     focus_paged_attn       attention of the requests' new rows over their pages
+ *     focus_token_logprobs   vocabulary logits -> log probabilities of given tokens, entropies, likeliest tokens
  *
  * Conventions shared by every entry point
  *  - Pointers marked [dev] are device (HBM) addresses, [host] are host addresses.  The caller owns every
@@ -406,6 +411,120 @@ int focus_quant_layer(const void* Q, const int32_t* focus_idx, const int32_t* ac
                       int32_t n_focus_max, int32_t max_active, const focus_quant_cache* cache, const float* kbar,
                       const focus_shape* shape, int32_t n_keep, const int32_t* sink_idx, int32_t n_sink, float* scores,
                       int32_t* kept_blocks, void* out, float* lse, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Rotation of rows by their positions.  A pair (a, b) of a row at position p becomes (a c - b s, b c + a s), c = scale * cos(p freq[j]) and
+ * s = scale * sin(p freq[j]) worked out in 64 bits and rounded to 32, each product and each sum rounded to 32 bits, the result to bf16.
+ */
+typedef struct focus_rotation {
+  const double* freq;  /* [dev] fp64[rot_dim / 2]: radians a position (focus_helper_rotary); negative ones turn the other way */
+  int32_t rot_dim;     /* values of a row that are turned, its first ones: a multiple of 16, 16 <= rot_dim <= d; the others stay */
+  int32_t interleaved; /* 0: value j and value j + rot_dim / 2 are pair j; non-zero: values 2j and 2j + 1 */
+  double scale;        /* of the turned values (1: lengths stay); not 0, finite */
+} focus_rotation;
+
+/*
+ * Rows turned by their positions: the Q and K_new that the other entry points take.
+ *   X    [dev] bf16 [n_rows, n_heads, d], strides x_stride_* in elements, multiples of 8;  d = head_dim: 64 or 128
+ *   out  [dev] bf16 [n_rows, n_heads, d], strides o_stride_* (a head-major [H, n, d] is one of them); it may be X itself with the same strides
+ *   positions [dev] int32[n_rows] or NULL (= 0, 1, 2, ...): row i is at position pos_base + positions[i].  Rows with positions[i] < 0 are
+ *             left out (nothing is written), so that the active_idx of focus_select_queries may be handed over as it is, with pos_base =
+ *             the position of the generation block's first token
+ * n_rows >= 1, 1 <= n_heads <= 65535.
+ */
+int focus_rotary(const void* X, int64_t x_stride_h, int64_t x_stride_n, void* out, int64_t o_stride_h, int64_t o_stride_n, int32_t n_rows,
+                 int32_t n_heads, int32_t head_dim, const int32_t* positions, int32_t pos_base, const focus_rotation* rot, void* stream);
+
+/*
+ * Frequencies of focus_rotation, [host]: freq[j] = base^(-2j / rot_dim), of which those that turn fewer than turns_low times in orig_len positions are
+ * divided by `factor`, those that turn more than turns_high times stay, and those between are mixed in proportion (a context longer than
+ * the one that was trained on).  turns_low = turns_high: a step there; infinite ones: all are divided; factor = 1: none is changed.
+ */
+int focus_helper_rotary(double base, int32_t rot_dim, double factor, int32_t orig_len, double turns_low, double turns_high, double* freq);
+
+/*
+ * KV cache in pages that requests share out among themselves.  Cache row j of a request lies in page page_table[request][j / page], at place j mod page.
+ * Rows are bf16 (k_exp = v_exp = NULL), or codes of eight bits with an exponent byte a row, as in focus_quant_cache.
+ * Strides: of a page, of a head, of a row, in elements of the rows (bf16: multiples of 8, codes: of 16), those of the exponents in bytes; so
+ * [n_pages, H, page, d] and [n_pages, page, H, d] are both such caches.  Row strides are at least d and less than 2^24.
+ */
+typedef struct focus_paged_cache {
+  void* k;
+  void* v;
+  uint8_t* k_exp;
+  uint8_t* v_exp;
+  int64_t k_stride_p, k_stride_h, k_stride_n;
+  int64_t v_stride_p, v_stride_h, v_stride_n;
+  int64_t exp_stride_p, exp_stride_h, exp_stride_n; /* of k_exp and v_exp */
+  int32_t n_pages, page;      /* pages; rows a page, 1 .. 65536 */
+  int32_t n_heads, head_dim;  /* K/V heads, 1 .. 1024; 64 or 128 */
+} focus_paged_cache;
+
+/*
+ * The requests of a step.  The rows of request r, in the tensors of a call, are row_start[r] .. row_start[r + 1] - 1: its newest positions, the last
+ * ones of seq_len[r].  Rows behind row_start[n_req] belong to no request and are neither read nor written.
+ */
+typedef struct focus_paged_batch {
+  const int32_t* seq_len;    /* [dev] int32[n_req]: cache rows of the request, its new ones included (<= 0: none) */
+  const int32_t* page_table; /* [dev] int32[n_req, table_width]: pages; the rows of an entry outside [0, n_pages) do not exist */
+  const int32_t* row_start;  /* [dev] int32[n_req + 1], ascending from 0, or NULL: request r has row r and no other (max_rows = 1) */
+  const int32_t* positions;  /* [dev] int32[n_rows] or NULL: position of every row instead of the request's last ones; < 0: of none */
+  int64_t table_stride;      /* elements from one request's entries to the next one's, >= table_width */
+  int32_t table_width;       /* pages of a request at most: cache rows past table_width * page do not exist */
+  int32_t n_req;             /* 1 .. 65535 */
+  int32_t max_rows;          /* rows of a request at most; a request's rows past that are not read nor written */
+  int32_t n_rows;            /* rows of the tensors; row_start[n_req] <= n_rows */
+} focus_paged_batch;
+
+/*
+ * New states of every request into its pages, K turned by its position on the way, and the rows of Q beside it.
+ *   K_new, V_new [dev] bf16 [n_rows, H, d], strides new_stride_* (both)
+ *   rot          the rotation of K and Q, or NULL: none
+ *   Q, Q_out     [dev] bf16 [n_rows, n_q_heads, d], strides q_stride_* and qo_stride_*: Q_out = Q turned (Q itself with the same strides, or clear
+ *                of it); both NULL with n_q_heads = 0
+ * A row without a position (positions[i] < 0) is left out, Q included; of one whose cache row does not exist K and V are left out.  Of rows of
+ * one request with the same position the last one's K and V stay.  A page that several requests list must not be written by two of them.
+ */
+int focus_paged_append(const focus_paged_cache* cache, const focus_paged_batch* batch, const void* K_new, const void* V_new, int64_t new_stride_h,
+                       int64_t new_stride_n, const focus_rotation* rot, const void* Q, int64_t q_stride_h, int64_t q_stride_n, void* Q_out,
+                       int64_t qo_stride_h, int64_t qo_stride_n, int32_t n_q_heads, void* stream);
+
+/*
+ * Attention of the requests' rows over their pages, built for one or a few rows a request:
+ *   out[i, g, :] = softmax_j(Q[i, g] . K[j, h] / sqrt(d)) . V[j, h, :],  j over the existing cache rows below seq_len of the row's request,
+ *          h = g / (n_q_heads / H); with `causal` also j <= the row's position
+ *   Q    [dev] bf16 [n_rows, n_q_heads, d], strides q_stride_*; n_q_heads a multiple of H
+ *   out  [dev] bf16 [n_rows, n_q_heads, d], strides o_stride_*
+ *   lse  [dev] fp32 [n_rows, n_q_heads] natural-log sum of exp of the scaled logits, may be NULL
+ * A row without a key gets zeros and -inf.  Keys that a row does not attend to do not reach it, whatever they hold.  As K is turned when it is
+ * written, leaving pages out of page_table (entries of -1) is the attention over the others.  Queries as for focus_quant_cache over rows of eight bits.
+ *   workspace [dev] focus_paged_attn_workspace() bytes, 16-byte aligned; nothing is assumed about its contents
+ * The same arguments give the same bits; in which order a row's keys are added up depends on the lengths of all requests.
+ * ceil(n_q_heads / H * max_rows / 16) * ceil(table_width * page / 32) * max(n_req, n_q_heads) < 2^31, with table_width * page < 2^31.
+ */
+int focus_paged_attn(const void* Q, int64_t q_stride_h, int64_t q_stride_n, int32_t n_q_heads, const focus_paged_cache* cache,
+                     const focus_paged_batch* batch, int32_t causal, void* out, int64_t o_stride_h, int64_t o_stride_n, float* lse, void* workspace,
+                     size_t ws_bytes, void* stream);
+/* Bytes of workspace focus_paged_attn needs; of the batch only the numbers count.  0 on invalid arguments.  [host] only. */
+size_t focus_paged_attn_workspace(const focus_paged_cache* cache, const focus_paged_batch* batch, int32_t n_q_heads);
+
+/*
+ * Log probabilities over the vocabulary, softmax at temperature 1 (NaN counts as -inf, +inf as the largest number):
+ *   logits, dtype, row_stride, masked   as for focus_sample_tokens
+ *   targets  [dev] int32[n_rows], or NULL (then logprob is NULL, too)
+ *   logprob  [dev] fp32[n_rows] out: log of the probability of targets[i] (-inf where its logit is); 0 for a target outside [0, vocab)
+ *   entropy  [dev] fp32[n_rows] out or NULL: -sum p log p, in nats
+ *   top_ids  [dev] int32[n_rows, top_n] out: the top_n likeliest tokens in order, the lower id on a tie; -1 past those above -inf
+ *   top_logprobs [dev] fp32[n_rows, top_n] out: their log probabilities, -inf past them;  0 <= top_n <= 32, both NULL with 0
+ * Rows with masked[i] == 0, and rows without a logit above -inf: logprob 0 (the latter -inf), entropy 0, top_ids -1, top_logprobs -inf.
+ *   workspace [dev] focus_token_logprobs_workspace(n_rows, vocab, top_n) bytes, 16-byte aligned
+ * 1 <= n_rows <= 65535, 1 <= vocab <= 2097152.
+ */
+int focus_token_logprobs(const void* logits, int32_t dtype, int64_t row_stride, const int32_t* targets, const uint8_t* masked, int32_t n_rows,
+                         int32_t vocab, int32_t top_n, float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace,
+                         size_t ws_bytes, void* stream);
+/* Bytes of workspace focus_token_logprobs needs, at least what fewer rows need; 0 on invalid arguments.  [host] only. */
+size_t focus_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t top_n);
 
 /*
  * Bytes of workspace `fn` needs for this shape; 0 on invalid arguments.  [host] only.  With less a call is refused

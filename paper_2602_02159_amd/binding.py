@@ -24,6 +24,8 @@ EXPORTS = ("focus_select_queries", "focus_expand_groups", "focus_block_means", "
            "focus_token_confidence", "focus_token_confidence_workspace", "focus_cache_update", "focus_update_sparse_layer",
            "focus_quant_update", "focus_quant_refresh", "focus_quant_read", "focus_quant_attn", "focus_quant_layer",
            "focus_sample_tokens", "focus_sample_tokens_workspace",
+           "focus_rotary", "focus_helper_rotary", "focus_paged_append", "focus_paged_attn", "focus_paged_attn_workspace",
+           "focus_token_logprobs", "focus_token_logprobs_workspace",
            "focus_workspace_bytes", "focus_helper_k", "focus_helper_n_keep", "focus_helper_n_sink", "focus_last_error",
            "focus_version")
 
@@ -46,6 +48,26 @@ class QuantCache(C.Structure):
     """Mirror of `focus_quant_cache`."""
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
                 ("exp_stride_h", C.c_int64), ("exp_stride_n", C.c_int64)]
+
+
+class Rotation(C.Structure):
+    """Mirror of `focus_rotation`."""
+    _fields_ = [("freq", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_double)]
+
+
+class PagedCache(C.Structure):
+    """Mirror of `focus_paged_cache`."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
+                ("k_stride_p", C.c_int64), ("k_stride_h", C.c_int64), ("k_stride_n", C.c_int64),
+                ("v_stride_p", C.c_int64), ("v_stride_h", C.c_int64), ("v_stride_n", C.c_int64),
+                ("exp_stride_p", C.c_int64), ("exp_stride_h", C.c_int64), ("exp_stride_n", C.c_int64),
+                ("n_pages", C.c_int32), ("page", C.c_int32), ("n_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class PagedBatch(C.Structure):
+    """Mirror of `focus_paged_batch`."""
+    _fields_ = [("seq_len", C.c_void_p), ("page_table", C.c_void_p), ("row_start", C.c_void_p), ("positions", C.c_void_p),
+                ("table_stride", C.c_int64), ("table_width", C.c_int32), ("n_req", C.c_int32), ("max_rows", C.c_int32), ("n_rows", C.c_int32)]
 
 
 _lib = None
@@ -89,7 +111,18 @@ def lib() -> C.CDLL:
         L.focus_sample_tokens.argtypes = [p, i32, C.c_int64, p, p, p, p, p, p, i32, i32, p, p, p, p, sz, p]
         L.focus_sample_tokens_workspace.argtypes = [i32, i32]
         L.focus_sample_tokens_workspace.restype = sz
-        for name in ("focus_sample_tokens", "focus_quant_update", "focus_quant_refresh", "focus_quant_read", "focus_quant_attn", "focus_quant_layer",
+        i64, rp, cp, bp = C.c_int64, C.POINTER(Rotation), C.POINTER(PagedCache), C.POINTER(PagedBatch)
+        L.focus_rotary.argtypes = [p, i64, i64, p, i64, i64, i32, i32, i32, p, i32, rp, p]
+        L.focus_helper_rotary.argtypes = [C.c_double, i32, C.c_double, i32, C.c_double, C.c_double, C.POINTER(C.c_double)]
+        L.focus_paged_append.argtypes = [cp, bp, p, p, i64, i64, rp, p, i64, i64, p, i64, i64, i32, p]
+        L.focus_paged_attn.argtypes = [p, i64, i64, i32, cp, bp, i32, p, i64, i64, p, p, sz, p]
+        L.focus_paged_attn_workspace.argtypes = [cp, bp, i32]
+        L.focus_paged_attn_workspace.restype = sz
+        L.focus_token_logprobs.argtypes = [p, i32, i64, p, p, i32, i32, i32, p, p, p, p, p, sz, p]
+        L.focus_token_logprobs_workspace.argtypes = [i32, i32, i32]
+        L.focus_token_logprobs_workspace.restype = sz
+        for name in ("focus_rotary", "focus_helper_rotary", "focus_paged_append", "focus_paged_attn", "focus_token_logprobs",
+                     "focus_sample_tokens", "focus_quant_update", "focus_quant_refresh", "focus_quant_read", "focus_quant_attn", "focus_quant_layer",
                      "focus_select_queries", "focus_expand_groups", "focus_block_means", "focus_block_scores", "focus_find_sinks",
                      "focus_select_and_find_sinks", "focus_sparse_attn", "focus_sparse_layer", "focus_sparse_layer_static", "focus_block_partials", "focus_top_blocks",
                      "focus_probe_layer", "focus_refresh_attn", "focus_token_confidence", "focus_cache_update", "focus_update_sparse_layer", "focus_cache_refresh", "focus_block_entry"):
@@ -530,3 +563,172 @@ def quant_layer(q, focus_idx, active_idx, counts, cache: QuantCache, kbar, shape
     _check(lib().focus_quant_layer(_ptr(q), _ptr(focus_idx), _ptr(active_idx), _ptr(counts), focus_idx.numel(), slots, C.byref(cache),
                                    _ptr(kbar), C.byref(shape), n_keep, _ptr(sink_idx), n_sink, _ptr(scores), _ptr(kept_blocks), _ptr(out), _ptr(lse),
                                    _ptr(workspace), _space(workspace, device), _raw_stream(device)))
+
+
+# ---- requests over a paged cache
+def rotary_freqs(base: float, rot_dim: int, factor: float = 1.0, orig_len: int = 1, turns_low: float = 0.0, turns_high: float = 0.0) -> torch.Tensor:
+    """Frequencies for make_rotation, float64 on the host: see focus_helper_rotary."""
+    values = (C.c_double * max(rot_dim // 2, 1))()
+    _check(lib().focus_helper_rotary(base, rot_dim, factor, orig_len, turns_low, turns_high, values))
+    return torch.tensor(list(values)[:rot_dim // 2], dtype=torch.float64)
+
+
+def make_rotation(freq: torch.Tensor, interleaved: bool = False, scale: float = 1.0) -> Rotation:
+    """focus_rotation from its frequencies, float64 [rot_dim / 2] on the device (kept by the description)."""
+    _need(freq, torch.float64, "freq")
+    if freq.dim() != 1 or not freq.is_contiguous():
+        raise ValueError(f"freq: expected values next to each other, got shape {tuple(freq.shape)}, strides {freq.stride()}")
+    rotation = Rotation(_ptr(freq), 2 * freq.numel(), int(interleaved), scale)
+    rotation.tensors, rotation.device = (freq,), freq.get_device()
+    return rotation
+
+
+def _page_strides(t: torch.Tensor):
+    return [0 if n == 1 else s for n, s in zip(t.shape[:3], t.stride()[:3])]
+
+
+def make_paged_cache(k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor | None = None, v_exp: torch.Tensor | None = None) -> PagedCache:
+    """focus_paged_cache from [n_pages, H, page, d] tensors (of any strides but the innermost, 1): bf16, or uint8 codes with the exponent bytes
+    uint8 [n_pages, H, page].  The description keeps the tensors."""
+    dtype = torch.bfloat16 if k_exp is None else torch.uint8
+    if (k_exp is None) != (v_exp is None):
+        raise ValueError("k_exp and v_exp go together")
+    for t, name in ((k, "k"), (v, "v")):
+        _need(t, dtype, name)
+        if t.dim() != 4 or t.shape != k.shape or t.stride(3) != 1:
+            raise ValueError(f"{name}: expected [n_pages, H, page, d], innermost stride 1, got {list(t.shape)}, strides {t.stride()}")
+        if t.get_device() != k.get_device():
+            raise ValueError("k, v and their exponents must be on one device")
+    cache = PagedCache()
+    cache.k, cache.v = _ptr(k), _ptr(v)
+    cache.n_pages, cache.n_heads, cache.page, cache.head_dim = k.shape
+    for t, name in ((k, "k"), (v, "v")):
+        p, h, n = _page_strides(t)
+        for axis, stride in (("p", p), ("h", h), ("n", n if t.shape[2] > 1 else max(t.shape[3], 16))):
+            setattr(cache, f"{name}_stride_{axis}", stride)
+    if k_exp is not None:
+        for t, name in ((k_exp, "k_exp"), (v_exp, "v_exp")):
+            _need(t, torch.uint8, name)
+            if t.shape != k.shape[:3] or t.stride() != k_exp.stride() or t.get_device() != k.get_device():
+                raise ValueError(f"{name}: expected {list(k.shape[:3])} with common strides on {k.device}, got {list(t.shape)}, strides {t.stride()}")
+        cache.k_exp, cache.v_exp = _ptr(k_exp), _ptr(v_exp)
+        cache.exp_stride_p, cache.exp_stride_h, cache.exp_stride_n = k_exp.stride()
+    cache.tensors, cache.device = (k, v, k_exp, v_exp), k.get_device()
+    return cache
+
+
+def make_paged_batch(seq_len: torch.Tensor, page_table: torch.Tensor, row_start: torch.Tensor | None = None, max_rows: int = 1,
+                     n_rows: int | None = None, positions: torch.Tensor | None = None) -> PagedBatch:
+    """focus_paged_batch: seq_len int32 [n_req], page_table int32 [n_req, width], row_start int32 [n_req + 1] and positions int32 [n_rows] or None.
+    n_rows: rows of the tensors that the calls take (None: n_req).  The description keeps the tensors, whose values may change between calls."""
+    n_req = seq_len.numel()
+    n_rows = n_req if n_rows is None else n_rows
+    if page_table.dim() != 2 or page_table.shape[0] != n_req or page_table.shape[1] < 1 or (page_table.stride(1) != 1 and page_table.shape[1] > 1):
+        raise ValueError(f"page_table: expected [{n_req}, width], innermost stride 1, got {list(page_table.shape)}, strides {page_table.stride()}")
+    _need(page_table, torch.int32, "page_table")
+    device = page_table.get_device()
+    _check_values(device, (seq_len, "seq_len", torch.int32, 1), (row_start, "row_start", torch.int32, 0 if row_start is None else n_req + 1),
+                  (positions, "positions", torch.int32, 0 if positions is None else n_rows))
+    batch = PagedBatch(_ptr(seq_len), _ptr(page_table), _ptr(row_start), _ptr(positions),
+                       max(page_table.stride(0), page_table.shape[1]) if n_req > 1 else page_table.shape[1], page_table.shape[1], n_req, max_rows, n_rows)
+    if n_req > 1 and page_table.stride(0) < page_table.shape[1]:
+        raise ValueError(f"page_table: rows lie on one another, strides {page_table.stride()}")
+    batch.tensors, batch.device = (seq_len, page_table, row_start, positions), device
+    return batch
+
+
+def _on_device(device: int, *descriptions) -> None:
+    for t, name in descriptions:
+        if t is not None and getattr(t, "device", device) != device:
+            raise ValueError(f"{name} on cuda:{t.device}, but the current device is cuda:{device}")
+
+
+def _check_heads(device: int, rows: int, head_dim: int, *expected) -> None:
+    """bf16 [rows, heads, head_dim], innermost stride 1."""
+    for t, name, heads in expected:
+        if t.dtype != torch.bfloat16 or t.get_device() != device:
+            raise TypeError(f"{name}: expected a tensor of torch.bfloat16 on cuda:{device}, got {t.dtype} on {t.device}")
+        if t.shape != (rows, heads, head_dim) or t.stride(2) != 1:
+            raise ValueError(f"{name}: expected {[rows, heads, head_dim]}, innermost stride 1, got {list(t.shape)}, strides {t.stride()}")
+
+
+def _hn(t: torch.Tensor):
+    """Strides of a head and of a row of [rows, heads, d] (those of a single one mean nothing)."""
+    n, h, _ = t.stride()
+    return (h if t.shape[1] > 1 else 0), (n if t.shape[0] > 1 else 0)
+
+
+def rotary(x, out, positions, pos_base: int, rotation: Rotation) -> None:
+    """x, out bf16 [rows, heads, d] of any strides (a transposed view of head-major rows is one; out may be x); positions int32 [rows] or None."""
+    device = _device_of(x, "x")
+    if x.dim() != 3:
+        raise ValueError(f"x: expected [rows, heads, d], got {list(x.shape)}")
+    n, heads, d = x.shape
+    _check_heads(device, n, d, (x, "x", heads), (out, "out", heads))
+    _check_values(device, (positions, "positions", torch.int32, 0 if positions is None else n))
+    _on_device(device, (rotation, "rotation"))
+    _check(lib().focus_rotary(_ptr(x), *_hn(x), _ptr(out), *_hn(out), n, heads, d, _ptr(positions), pos_base, C.byref(rotation), _raw_stream(device)))
+
+
+def paged_append(cache: PagedCache, batch: PagedBatch, k_new, v_new, rotation: Rotation | None = None, q=None, q_out=None) -> None:
+    """k_new, v_new bf16 [n_rows, H, d] (common strides) into the requests' pages; with q, q_out bf16 [n_rows, heads, d] those turned as well."""
+    device, n, d = _device_of(k_new, "k_new"), batch.n_rows, cache.head_dim
+    _check_heads(device, n, d, (k_new, "k_new", cache.n_heads), (v_new, "v_new", cache.n_heads))
+    strides = _hn(k_new)
+    if strides != _hn(v_new):
+        raise ValueError("k_new and v_new must share their strides")
+    heads, q_strides, out_strides = 0, (0, 0), (0, 0)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out go together")
+    if q is not None:
+        heads = q.shape[1] if q.dim() == 3 else -1
+        _check_heads(device, n, d, (q, "q", heads), (q_out, "q_out", heads))
+        q_strides, out_strides = _hn(q), _hn(q_out)
+    _on_device(device, (cache, "cache"), (batch, "batch"), (rotation, "rotation"))
+    _check(lib().focus_paged_append(C.byref(cache), C.byref(batch), _ptr(k_new), _ptr(v_new), *strides, None if rotation is None else C.byref(rotation),
+                                    _ptr(q), *q_strides, _ptr(q_out), *out_strides, heads, _raw_stream(device)))
+
+
+def paged_attn_workspace(cache: PagedCache, batch: PagedBatch, n_q_heads: int) -> int:
+    return int(lib().focus_paged_attn_workspace(C.byref(cache), C.byref(batch), n_q_heads))
+
+
+def paged_attn(q, cache: PagedCache, batch: PagedBatch, causal: bool, out, lse, workspace) -> None:
+    """q, out bf16 [n_rows, n_q_heads, d], lse fp32 [n_rows, n_q_heads] or None; workspace of paged_attn_workspace() bytes."""
+    device, n, d = _device_of(q, "q"), batch.n_rows, cache.head_dim
+    heads = q.shape[1] if q.dim() == 3 else -1
+    _check_heads(device, n, d, (q, "q", heads), (out, "out", heads))
+    _check_values(device, (lse, "lse", torch.float32, 0 if lse is None else n * heads))
+    _on_device(device, (cache, "cache"), (batch, "batch"))
+    _check(lib().focus_paged_attn(_ptr(q), *_hn(q), heads, C.byref(cache), C.byref(batch), int(causal), _ptr(out), *_hn(out), _ptr(lse), _ptr(workspace),
+                                  _space(workspace, device), _raw_stream(device)))
+
+
+def token_logprobs_workspace(n_rows: int, vocab: int, top_n: int) -> int:
+    return int(lib().focus_token_logprobs_workspace(n_rows, vocab, top_n))
+
+
+def token_logprobs(logits, targets, masked, logprob, entropy, top_ids, top_logprobs, workspace) -> None:
+    """logits bf16 or fp32 [n_rows, vocab] (rows 16-byte aligned); targets int32 and logprob fp32 [n_rows] (both or neither), entropy fp32 [n_rows] or
+    None, top_ids int32 and top_logprobs fp32 [n_rows, top_n] (both or neither); workspace of token_logprobs_workspace() bytes."""
+    if not logits.is_cuda or logits.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"logits: expected a CUDA tensor of bfloat16 or float32, got {logits.dtype} on {logits.device}")
+    if logits.dim() != 2 or logits.stride(1) != 1:
+        raise ValueError("logits: expected [n_rows, vocab], innermost stride 1")
+    device = _device_of(logits, "logits")
+    rows, vocab = logits.shape
+    stride = logits.stride(0) if rows > 1 else (vocab + 7) // 8 * 8  # (of one row any will do)
+    if (top_ids is None) != (top_logprobs is None) or (targets is None) != (logprob is None):
+        raise ValueError("targets and logprob, top_ids and top_logprobs go together")
+    top_n = 0 if top_ids is None else top_ids.shape[1] if top_ids.dim() == 2 else -1
+    for t, dtype, shape, name in ((targets, torch.int32, (rows,), "targets"), (logprob, torch.float32, (rows,), "logprob"), (entropy, torch.float32, (rows,), "entropy"),
+                                  (top_ids, torch.int32, (rows, top_n), "top_ids"), (top_logprobs, torch.float32, (rows, top_n), "top_logprobs")):
+        if t is not None and not (t.dtype == dtype and t.get_device() == device and t.shape == shape and t.is_contiguous()):
+            _need(t, dtype, name)
+            _device_of(t, name)
+            raise ValueError(f"{name}: expected {list(shape)} next to each other, got {list(t.shape)}, strides {t.stride()}")
+    if masked is not None and (masked.get_device() != device or masked.element_size() != 1 or masked.shape != (rows,) or not masked.is_contiguous()):
+        raise ValueError(f"masked: expected {rows} bytes on cuda:{device}, got {masked.dtype}, shape {tuple(masked.shape)} on {masked.device}")
+    _check(lib().focus_token_logprobs(_ptr(logits), int(logits.dtype == torch.float32), stride, _ptr(targets), _ptr(masked), rows, vocab, top_n,
+                                      _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs), _ptr(workspace), _space(workspace, device),
+                                      _raw_stream(device)))

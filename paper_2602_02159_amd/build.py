@@ -13,7 +13,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfocus_hip.so")
-SOURCES = ["focus_api.hip", "focus_small.hip", "focus_mfma.hip", "focus_quant.hip", "focus_sample.hip"]
+SOURCES = ["focus_api.hip", "focus_small.hip", "focus_mfma.hip", "focus_quant.hip", "focus_sample.hip", "focus_rotary.hip",
+           "focus_paged.hip", "focus_logprob.hip"]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fno-gpu-rdc", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # the first 14 dwords of a kernel's scalar arguments arrive in registers: most launches of a step are two or three

@@ -528,6 +528,81 @@ static int check_attention(const char* who, const focus_shape* shape, const void
   return FOCUS_OK;
 }
 
+// ---- requests over a paged cache
+static int check_rotation(const char* who, const focus_rotation* rot, int32_t head_dim) {
+  if (!rot->freq) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
+  if (reinterpret_cast<uintptr_t>(rot->freq) & 7u) return fail(FOCUS_EINVAL, "%s: freq must be 8-byte aligned", who);
+  if (rot->rot_dim < 16 || rot->rot_dim > head_dim || (rot->rot_dim & 15))
+    return fail(FOCUS_EUNSUPPORTED, "%s: rot_dim=%d (a multiple of 16 up to head_dim)", who, rot->rot_dim);
+  if (!(std::fabs(rot->scale) > 0.0) || std::isinf(rot->scale)) return fail(FOCUS_EINVAL, "%s: scale is 0 or not finite", who);
+  return FOCUS_OK;
+}
+
+static int check_head_dim(const char* who, int32_t head_dim) {
+  if (head_dim != 64 && head_dim != 128) return fail(FOCUS_EUNSUPPORTED, "%s: head_dim=%d (64 or 128)", who, head_dim);
+  return FOCUS_OK;
+}
+
+// bf16 rows [n_rows, heads, d] in any order
+static int check_rows(const char* who, const char* name, const void* t, int64_t stride_h, int64_t stride_n, int32_t heads = 1, int32_t n_rows = 1) {
+  if ((heads > 1 && stride_h == 0) || (n_rows > 1 && stride_n == 0)) return fail(FOCUS_EINVAL, "%s: rows of %s lie on one another", who, name);
+  if (!t) return fail(FOCUS_EINVAL, "%s: %s is NULL", who, name);
+  if ((stride_h & 7) || (stride_n & 7) || stride_h < 0 || stride_n < 0) return fail(FOCUS_EINVAL, "%s: strides of %s invalid or not multiples of 8", who, name);
+  if (!aligned16(t)) return fail(FOCUS_EINVAL, "%s: pointers must be 16-byte aligned", who);
+  return FOCUS_OK;
+}
+
+static int check_paged_sizes(const char* who, const focus_paged_cache* c, const focus_paged_batch* b) {
+  if (!c || !b) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
+  if (int rc = check_head_dim(who, c->head_dim)) return rc;
+  if (c->n_heads < 1 || c->n_heads > 1024) return fail(FOCUS_EINVAL, "%s: n_heads=%d not in [1, 1024]", who, c->n_heads);
+  if (c->n_pages < 1 || c->page < 1 || c->page > 65536) return fail(FOCUS_EINVAL, "%s: n_pages=%d or page=%d (1 .. 65536) out of range", who, c->n_pages, c->page);
+  if (b->n_req < 1 || b->n_req > 65535) return fail(FOCUS_EINVAL, "%s: n_req=%d not in [1, 65535]", who, b->n_req);
+  if (b->max_rows < 1 || b->n_rows < 1) return fail(FOCUS_EINVAL, "%s: max_rows=%d or n_rows=%d less than 1", who, b->max_rows, b->n_rows);
+  if (b->table_width < 1 || (int64_t)b->table_width * c->page > INT32_MAX)
+    return fail(FOCUS_EINVAL, "%s: table_width=%d pages of %d rows out of range", who, b->table_width, c->page);
+  return FOCUS_OK;
+}
+
+static int check_paged(const char* who, const focus_paged_cache* c, const focus_paged_batch* b) {
+  if (int rc = check_paged_sizes(who, c, b)) return rc;
+  if (!c->k || !c->v || !b->seq_len || !b->page_table) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
+  if (!c->k_exp != !c->v_exp) return fail(FOCUS_EINVAL, "%s: k_exp and v_exp are both NULL or neither", who);
+  const int64_t step = c->k_exp ? 16 : 8;
+  const int64_t rows[2] = {c->k_stride_n, c->v_stride_n}, others[4] = {c->k_stride_p, c->k_stride_h, c->v_stride_p, c->v_stride_h};
+  for (int64_t s : rows)
+    if (s < c->head_dim || s % step || s >= (int64_t(1) << 24)) return fail(FOCUS_EINVAL, "%s: row stride %lld (a multiple of %lld in [head_dim, 2^24))", who, (long long)s, (long long)step);
+  for (int64_t s : others)
+    if (s < 0 || s % step) return fail(FOCUS_EINVAL, "%s: strides of pages and heads are multiples of %lld", who, (long long)step);
+  if (c->k_exp && (c->exp_stride_p < 0 || c->exp_stride_h < 0 || c->exp_stride_n < 1)) return fail(FOCUS_EINVAL, "%s: strides of the exponents out of range", who);
+  if (!aligned16(c->k) || !aligned16(c->v)) return fail(FOCUS_EINVAL, "%s: pointers must be 16-byte aligned", who);
+  if (b->table_stride < b->table_width) return fail(FOCUS_EINVAL, "%s: table_stride less than table_width", who);
+  if (!b->row_start && (b->max_rows != 1 || b->n_rows < b->n_req)) return fail(FOCUS_EINVAL, "%s: without row_start every request has one row", who);
+  return FOCUS_OK;
+}
+
+static PagedBatch paged_batch(const focus_paged_batch& b) {
+  PagedBatch x;
+  x.seq_len = b.seq_len;
+  x.page_table = b.page_table;
+  x.row_start = b.row_start;
+  x.positions = b.positions;
+  x.table_stride = b.table_stride;
+  x.table_width = b.table_width;
+  x.n_req = b.n_req;
+  x.max_rows = std::min(b.max_rows, b.n_rows);
+  x.n_rows = b.n_rows;
+  return x;
+}
+
+static int check_paged_queries(const char* who, const focus_paged_cache* c, const focus_paged_batch* b, int32_t n_q_heads) {
+  if (n_q_heads < 1 || n_q_heads > 65535 || n_q_heads % c->n_heads) return fail(FOCUS_EINVAL, "%s: n_q_heads=%d not a multiple of n_heads=%d up to 65535", who, n_q_heads, c->n_heads);
+  const int64_t tiles = ceil_div64((int64_t)b->table_width * c->page, 32), groups = ceil_div64((int64_t)n_q_heads / c->n_heads * std::min(b->max_rows, b->n_rows), 16);
+  if (groups > INT32_MAX / tiles || groups * tiles > INT32_MAX / std::max(b->n_req, n_q_heads))
+    return fail(FOCUS_EUNSUPPORTED, "%s: %lld groups of 16 rows, %lld tiles of 32 keys, %d requests, %d heads are too many", who, (long long)groups, (long long)tiles, b->n_req, n_q_heads);
+  return FOCUS_OK;
+}
+
 }  // namespace focus
 
 using namespace focus;
@@ -1004,6 +1079,168 @@ int focus_quant_layer(const void* Q, const int32_t* focus_idx, const int32_t* ac
   e = launch_quant_attn(Q, active_idx, counts, max_active, quant_cache(*cache), *shape, fused ? nullptr : kept_blocks, n_keep, sink_idx, n_sink, p, out,
                         lse, part_o, part_ml, fused ? &f : nullptr, st);
   if (e != hipSuccess) return launch_fail("focus_quant_layer(attention)", e);
+  return FOCUS_OK;
+}
+
+int focus_rotary(const void* X, int64_t x_stride_h, int64_t x_stride_n, void* out, int64_t o_stride_h, int64_t o_stride_n, int32_t n_rows,
+                 int32_t n_heads, int32_t head_dim, const int32_t* positions, int32_t pos_base, const focus_rotation* rot, void* stream) {
+  const char* who = "focus_rotary";
+  if (!rot) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
+  if (int rc = check_head_dim(who, head_dim)) return rc;
+  if (int rc = check_rotation(who, rot, head_dim)) return rc;
+  if (n_rows < 1) return fail(FOCUS_EINVAL, "%s: n_rows=%d less than 1", who, n_rows);
+  if (n_heads < 1 || n_heads > 65535) return fail(FOCUS_EINVAL, "%s: n_heads=%d not in [1, 65535]", who, n_heads);
+  if (int rc = check_rows(who, "X", X, x_stride_h, x_stride_n)) return rc;
+  if (int rc = check_rows(who, "out", out, o_stride_h, o_stride_n, n_heads, n_rows)) return rc;
+  if (X == out && (x_stride_h != o_stride_h || x_stride_n != o_stride_n)) return fail(FOCUS_EINVAL, "%s: in place, but with other strides", who);
+  TurnRows p = {};
+  p.Q = static_cast<const uint16_t*>(X);
+  p.Qo = static_cast<uint16_t*>(out);
+  p.qsh = x_stride_h; p.qsn = x_stride_n;
+  p.qosh = o_stride_h; p.qosn = o_stride_n;
+  p.freq = rot->freq;
+  p.scale = rot->scale;
+  p.rot_dim = rot->rot_dim;
+  p.interleaved = rot->interleaved != 0;
+  p.n_q_heads = n_heads;
+  p.b.positions = positions;
+  p.b.n_rows = n_rows;
+  p.pos_base = pos_base;
+  hipError_t e = launch_turn_rows(p, head_dim, false, false, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return launch_fail(who, e);
+  return FOCUS_OK;
+}
+
+int focus_helper_rotary(double base, int32_t rot_dim, double factor, int32_t orig_len, double turns_low, double turns_high, double* freq) {
+  const char* who = "focus_helper_rotary";
+  if (!freq) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
+  if (rot_dim < 2 || (rot_dim & 1)) return fail(FOCUS_EINVAL, "%s: rot_dim=%d", who, rot_dim);
+  if (!(base > 0.0) || !(factor > 0.0) || std::isinf(base) || std::isinf(factor) || orig_len < 1 || !(turns_low <= turns_high))
+    return fail(FOCUS_EINVAL, "%s: base and factor are positive numbers, orig_len at least 1, turns_low <= turns_high", who);
+  for (int32_t j = 0; j < rot_dim / 2; ++j) {
+    const double f = std::pow(base, -2.0 * j / rot_dim), turns = orig_len * f / (2.0 * 3.14159265358979323846);
+    const double whole = turns >= turns_high ? 1.0 : (turns <= turns_low ? 0.0 : (turns - turns_low) / (turns_high - turns_low));  // share that stays
+    freq[j] = f * (whole + (1.0 - whole) / factor);
+  }
+  return FOCUS_OK;
+}
+
+int focus_paged_append(const focus_paged_cache* cache, const focus_paged_batch* batch, const void* K_new, const void* V_new, int64_t new_stride_h,
+                       int64_t new_stride_n, const focus_rotation* rot, const void* Q, int64_t q_stride_h, int64_t q_stride_n, void* Q_out,
+                       int64_t qo_stride_h, int64_t qo_stride_n, int32_t n_q_heads, void* stream) {
+  const char* who = "focus_paged_append";
+  if (int rc = check_paged(who, cache, batch)) return rc;
+  if (int rc = check_rows(who, "K_new", K_new, new_stride_h, new_stride_n)) return rc;
+  if (int rc = check_rows(who, "V_new", V_new, new_stride_h, new_stride_n)) return rc;
+  if (rot)
+    if (int rc = check_rotation(who, rot, cache->head_dim)) return rc;
+  if (!Q != !Q_out || (!Q && n_q_heads != 0)) return fail(FOCUS_EINVAL, "%s: Q and Q_out are both NULL, with n_q_heads = 0, or neither", who);
+  if (Q) {
+    if (n_q_heads < 1 || n_q_heads > 65535) return fail(FOCUS_EINVAL, "%s: n_q_heads=%d not in [1, 65535]", who, n_q_heads);
+    if (int rc = check_rows(who, "Q", Q, q_stride_h, q_stride_n)) return rc;
+    if (int rc = check_rows(who, "Q_out", Q_out, qo_stride_h, qo_stride_n, n_q_heads, batch->n_rows)) return rc;
+    if (Q == Q_out && (q_stride_h != qo_stride_h || q_stride_n != qo_stride_n)) return fail(FOCUS_EINVAL, "%s: in place, but with other strides", who);
+  }
+  TurnRows p = {};
+  p.Q = static_cast<const uint16_t*>(Q);
+  p.Qo = static_cast<uint16_t*>(Q_out);
+  p.qsh = q_stride_h; p.qsn = q_stride_n;
+  p.qosh = qo_stride_h; p.qosn = qo_stride_n;
+  p.Kn = static_cast<const uint16_t*>(K_new);
+  p.Vn = static_cast<const uint16_t*>(V_new);
+  p.nsh = new_stride_h; p.nsn = new_stride_n;
+  p.K = cache->k;
+  p.V = cache->v;
+  p.k_exp = cache->k_exp;
+  p.v_exp = cache->v_exp;
+  p.ksp = cache->k_stride_p; p.ksh = cache->k_stride_h; p.ksn = cache->k_stride_n;
+  p.vsp = cache->v_stride_p; p.vsh = cache->v_stride_h; p.vsn = cache->v_stride_n;
+  p.esp = cache->exp_stride_p; p.esh = cache->exp_stride_h; p.esn = cache->exp_stride_n;
+  if (rot) {
+    p.freq = rot->freq;
+    p.scale = rot->scale;
+    p.rot_dim = rot->rot_dim;
+    p.interleaved = rot->interleaved != 0;
+  }
+  p.n_q_heads = n_q_heads;
+  p.n_heads = cache->n_heads;
+  p.page = cache->page;
+  p.n_pages = cache->n_pages;
+  p.b = paged_batch(*batch);
+  hipError_t e = launch_turn_rows(p, cache->head_dim, true, cache->k_exp != nullptr, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return launch_fail(who, e);
+  return FOCUS_OK;
+}
+
+size_t focus_paged_attn_workspace(const focus_paged_cache* cache, const focus_paged_batch* batch, int32_t n_q_heads) {
+  if (check_paged_sizes("focus_paged_attn_workspace", cache, batch) || check_paged_queries("focus_paged_attn_workspace", cache, batch, n_q_heads)) return 0;
+  return plan_paged_attn(cache->n_heads, n_q_heads / cache->n_heads, cache->head_dim, paged_batch(*batch), cache->page).total;
+}
+
+int focus_paged_attn(const void* Q, int64_t q_stride_h, int64_t q_stride_n, int32_t n_q_heads, const focus_paged_cache* cache,
+                     const focus_paged_batch* batch, int32_t causal, void* out, int64_t o_stride_h, int64_t o_stride_n, float* lse, void* workspace,
+                     size_t ws_bytes, void* stream) {
+  const char* who = "focus_paged_attn";
+  if (int rc = check_paged(who, cache, batch)) return rc;
+  if (int rc = check_paged_queries(who, cache, batch, n_q_heads)) return rc;
+  if (int rc = check_rows(who, "Q", Q, q_stride_h, q_stride_n)) return rc;
+  if (int rc = check_rows(who, "out", out, o_stride_h, o_stride_n, n_q_heads, batch->n_rows)) return rc;
+  const PagedBatch b = paged_batch(*batch);
+  const PagedPlan plan = plan_paged_attn(cache->n_heads, n_q_heads / cache->n_heads, cache->head_dim, b, cache->page);
+  if (!workspace || ws_bytes < plan.total || !aligned16(workspace))
+    return fail(FOCUS_EWORKSPACE, "%s: workspace needs %zu bytes, 16-byte aligned", who, plan.total);
+  const int64_t size = cache->k_exp ? 1 : 2;
+  PagedAttn p = {};
+  p.Q = static_cast<const uint16_t*>(Q);
+  p.out = static_cast<uint16_t*>(out);
+  p.lse = lse;
+  p.qsh = q_stride_h; p.qsn = q_stride_n;
+  p.osh = o_stride_h; p.osn = o_stride_n;
+  p.K = static_cast<const uint8_t*>(cache->k);
+  p.V = static_cast<const uint8_t*>(cache->v);
+  p.k_exp = cache->k_exp;
+  p.v_exp = cache->v_exp;
+  p.ksp = cache->k_stride_p * size; p.ksh = cache->k_stride_h * size; p.ksn = cache->k_stride_n * size;
+  p.vsp = cache->v_stride_p * size; p.vsh = cache->v_stride_h * size; p.vsn = cache->v_stride_n * size;
+  p.esp = cache->exp_stride_p; p.esh = cache->exp_stride_h; p.esn = cache->exp_stride_n;
+  p.b = b;
+  p.H = cache->n_heads;
+  p.group = n_q_heads / cache->n_heads;
+  p.page = cache->page;
+  p.n_pages = cache->n_pages;
+  p.causal = causal != 0;
+  p.workers = plan.workers;
+  p.unit_rows = plan.unit_rows;
+  p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cache->head_dim));
+  p.part_o = static_cast<float*>(workspace);
+  p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + plan.part_ml);
+  hipError_t e = launch_paged_attn(p, plan, cache->head_dim, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return launch_fail(who, e);
+  return FOCUS_OK;
+}
+
+size_t focus_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t top_n) {
+  if (n_rows < 1 || n_rows > 65535 || vocab < 1 || vocab > kSampleMaxVocab || top_n < 0 || top_n > kLogprobTop) return 0;
+  return token_logprobs_workspace(n_rows, vocab, top_n);
+}
+
+int focus_token_logprobs(const void* logits, int32_t dtype, int64_t row_stride, const int32_t* targets, const uint8_t* masked, int32_t n_rows,
+                         int32_t vocab, int32_t top_n, float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace,
+                         size_t ws_bytes, void* stream) {
+  const char* who = "focus_token_logprobs";
+  if (!logits || !targets != !logprob) return fail(FOCUS_EINVAL, "%s: NULL pointer (targets and logprob go together)", who);
+  if (dtype != FOCUS_BF16 && dtype != FOCUS_F32) return fail(FOCUS_EUNSUPPORTED, "%s: dtype=%d", who, dtype);
+  if (n_rows < 1 || n_rows > 65535) return fail(FOCUS_EINVAL, "%s: n_rows=%d not in [1, 65535]", who, n_rows);
+  if (vocab < 1 || vocab > kSampleMaxVocab) return fail(FOCUS_EINVAL, "%s: vocab=%d not in [1, %d]", who, vocab, kSampleMaxVocab);
+  if (top_n < 0 || top_n > kLogprobTop) return fail(FOCUS_EINVAL, "%s: top_n=%d not in [0, %d]", who, top_n, kLogprobTop);
+  if (top_n > 0 && (!top_ids || !top_logprobs)) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
+  if (row_stride < vocab || (row_stride & (dtype == FOCUS_F32 ? 3 : 7)) || !aligned16(logits))
+    return fail(FOCUS_EINVAL, "%s: rows must be 16-byte aligned, row_stride >= vocab", who);
+  const size_t need = token_logprobs_workspace(n_rows, vocab, top_n);
+  if (!workspace || ws_bytes < need || !aligned16(workspace)) return fail(FOCUS_EWORKSPACE, "%s: workspace needs %zu bytes, 16-byte aligned", who, need);
+  hipError_t e = launch_token_logprobs(logits, dtype, row_stride, targets, masked, n_rows, vocab, top_n, logprob, entropy, top_ids, top_logprobs,
+                                       workspace, static_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return launch_fail(who, e);
   return FOCUS_OK;
 }
 

@@ -173,6 +173,63 @@ hipError_t launch_quant_attn(const void* Q, const int32_t* active_idx, const int
                              const int32_t* kept_blocks, int n_keep, const int32_t* sink_idx, int n_sink, const SplitPlan& p, void* out, float* lse,
                              float* part_o, float* part_ml, const FusedTopC* fused, hipStream_t st);
 
+// ---- requests over a paged cache (focus_rotary.hip, focus_paged.hip).  As focus_paged_batch.
+struct PagedBatch {
+  const int32_t* seq_len;
+  const int32_t* page_table;
+  const int32_t* row_start;
+  const int32_t* positions;
+  int64_t table_stride;
+  int table_width, n_req, max_rows, n_rows;
+};
+// focus_rotary (of `b` only positions and n_rows count) and focus_paged_append.  Strides of the cache in its elements.
+struct TurnRows {
+  const uint16_t* Q;
+  uint16_t* Qo;
+  const uint16_t* Kn;
+  const uint16_t* Vn;
+  void* K;
+  void* V;
+  uint8_t* k_exp;
+  uint8_t* v_exp;
+  const double* freq;
+  double scale;
+  int64_t qsh, qsn, qosh, qosn, nsh, nsn, ksp, ksh, ksn, vsp, vsh, vsn, esp, esh, esn;
+  PagedBatch b;
+  int pos_base, rot_dim, interleaved, n_q_heads, n_heads, page, n_pages;
+};
+hipError_t launch_turn_rows(const TurnRows& p, int head_dim, bool pages, bool quant, hipStream_t st);
+struct PagedAttn {
+  const uint16_t* Q;
+  const uint8_t* K;
+  const uint8_t* V;
+  const uint8_t* k_exp;
+  const uint8_t* v_exp;
+  uint16_t* out;
+  float* lse;
+  float* part_o;
+  float2* part_ml;
+  int64_t qsh, qsn, osh, osn;
+  int64_t ksp, ksh, ksn, vsp, vsh, vsn, esp, esh, esn;  // of the cache, in bytes
+  PagedBatch b;
+  int H, group, page, n_pages, causal;
+  int workers;      // wavefronts among which the tiles of all requests are divided
+  int unit_rows;    // rows of a partial result
+  float scale_log2;
+};
+struct PagedPlan {
+  int q_tiles;      // 16-query tiles of a unit: 1 or 2
+  int unit_rows, workers;
+  size_t part_ml, total;
+};
+PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch& b, int page);
+hipError_t launch_paged_attn(const PagedAttn& a, const PagedPlan& p, int head_dim, hipStream_t st);
+// Log probabilities (focus_logprob.hip)
+constexpr int kLogprobTop = 32;
+size_t token_logprobs_workspace(int n_rows, int vocab, int top_n);
+hipError_t launch_token_logprobs(const void* logits, int dtype, int64_t row_stride, const int32_t* targets, const uint8_t* masked, int n_rows, int vocab,
+                                 int top_n, float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace, hipStream_t st);
+
 // ---- MFMA kernels (focus_mfma.hip)
 // mode 0: logits [H, ceil(L / 4), 16, 4] + part_ml out (at most 16 queries); mode 1: part_ml out only; mode 2: lse2 in, or part_ml of
 // mode 1 (not null; lse_in_logits), colpart [q_groups * H, L] out

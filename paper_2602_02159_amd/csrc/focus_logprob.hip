@@ -1,0 +1,321 @@
+// Log probabilities of given tokens, entropies and the likeliest tokens.
+//
+// With m the largest logit of a row and y_v = z_v - m, what has to be known is r = sum of exp(y_v) over all tokens but one of the largest, and
+// A = sum of exp(y_v) y_v:
+//   log sum exp(z) = m + log1p(r)        log p_t = z_t - m - log1p(r)        entropy = log1p(r) - A / (1 + r)
+// Leaving the largest out of the sum keeps the digits of rows that are all but certain: 1 + r would round them away.
+//
+//   logprob_part_kernel  a workgroup has 8192 logits of a row, 32 a thread, in registers: their largest, r and A, and their likeliest tokens
+//   logprob_join_kernel  a workgroup a row: the parts together
+#include <type_traits>
+
+#include "focus_common.h"
+#include "focus_kernels.h"
+#include "focus_topk.h"
+
+namespace focus {
+
+constexpr int kLogitsThread = 32, kLogitsPart = 256 * kLogitsThread;
+constexpr int kTopCandidates = 512;
+
+// NaN as -inf, +inf as the largest number
+__device__ __forceinline__ float tame(float x) { return fminf(fmaxf(x, -INFINITY), 3.4028234663852886e38f); }
+// place in the order of the logits, 0 for those that are no candidate
+__device__ __forceinline__ uint32_t top_key(float z) { return z == -INFINITY ? 0u : order_key(z); }
+
+struct LogprobArgs {
+  const void* logits;
+  const int32_t* targets;
+  const uint8_t* masked;
+  float* logprob;
+  float* entropy;
+  int32_t* top_ids;
+  float* top_logprobs;
+  float4* part;     // [n_rows, n_parts] (m, r, A in units of log 2, -)
+  uint2* part_top;  // [n_rows, n_parts, top_n] (key, id), key 0: none
+  int64_t row_stride;
+  int vocab, n_parts, top_n;
+};
+
+struct TopShared256 {
+  uint32_t best[256];
+  uint2 list[kTopCandidates];
+  uint32_t count, threshold;
+  unsigned long long wave_best[4];
+};
+
+// The top_n first, in order, of what 256 threads hold, N entries each: key_at(i) (0: none) and id_at(i), `best` = the largest key of the
+// thread.  emit(rank, key, id) is called once for each of them.  The top_n-th largest of the threads' best, to sixteen bits, is a bound that at least top_n
+// entries reach; those that do are listed and rank themselves by comparison.  Where too many do (equal logits), one is found after
+// the other.  Every thread of the workgroup has to call it.
+// `UNROLL` turns at once: all of them where the entries are registers.
+template <int N, int UNROLL, class Key, class Id, class Emit>
+__device__ __forceinline__ void block_top(TopShared256& sm, uint32_t best, int top_n, const Key key_at, const Id id_at, const Emit emit) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  sm.best[tid] = best;
+  if (tid == 0) sm.count = 0u;
+  __syncthreads();
+  if (wave == 0) {
+    uint32_t k[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) k[u] = sm.best[u * kWave + lane] >> 16;
+    uint32_t t = 0u;
+    for (int bit = 15; bit >= 0; --bit) {
+      const uint32_t with = t | (1u << bit);
+      int n = 0;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) n += __popcll(__ballot(k[u] >= with));
+      if (n >= top_n) t = with;
+    }
+    if (lane == 0) sm.threshold = max(t << 16, 1u);
+  }
+  __syncthreads();
+  const uint32_t threshold = sm.threshold;
+  if (best >= threshold) {
+#pragma unroll UNROLL
+    for (int i = 0; i < N; ++i) {
+      const uint32_t key = key_at(i);
+      if (key >= threshold) {
+        const uint32_t at = atomicAdd(&sm.count, 1u);  // (the list's order does not matter)
+        if (at < (uint32_t)kTopCandidates) sm.list[at] = make_uint2(key, (uint32_t)id_at(i));
+      }
+    }
+  }
+  __syncthreads();
+  const int n = (int)sm.count;
+  if (n <= kTopCandidates) {
+    for (int i = tid; i < n; i += 256) {
+      const uint2 mine = sm.list[i];
+      int rank = 0;
+      for (int j = 0; j < n; ++j) {
+        const uint2 other = sm.list[j];
+        rank += other.x > mine.x || (other.x == mine.x && other.y < mine.y);
+      }
+      if (rank < top_n) emit(rank, mine.x, (int)mine.y);
+    }
+    for (int i = n + tid; i < top_n; i += 256) emit(i, 0u, -1);
+    return;
+  }
+  // larger = earlier in the order; the lower id first
+  unsigned long long last = ~0ull;
+  for (int k = 0; k < top_n; ++k) {
+    unsigned long long mine = 0ull;
+#pragma unroll UNROLL
+    for (int i = 0; i < N; ++i) {
+      const uint32_t key = key_at(i);
+      const unsigned long long x = key == 0u ? 0ull : ((unsigned long long)key << 32) | (uint32_t)~id_at(i);
+      if (x < last && x > mine) mine = x;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const unsigned long long y = __shfl_xor(mine, o, kWave);
+      mine = y > mine ? y : mine;
+    }
+    __syncthreads();  // (wave_best is read in the turn before)
+    if (lane == 0) sm.wave_best[wave] = mine;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) mine = sm.wave_best[w] > mine ? sm.wave_best[w] : mine;
+    last = mine;
+    if (tid == 0) emit(k, (uint32_t)(mine >> 32), mine == 0ull ? -1 : (int)~(uint32_t)mine);
+  }
+}
+
+// max / sum over the workgroup of four wavefronts, in a fixed order; `sh` of four entries
+__device__ __forceinline__ float block_max4(float x, float* sh) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, kWave));
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
+}
+
+constexpr float kLog2eF = 1.4426950408889634f, kLn2F = 0.6931471805599453f;
+constexpr float kNothing = -200.f;  // 2^-200 is zero: exponents below are taken as this one, so that no 0 times infinity comes up
+
+template <class T>
+__global__ __launch_bounds__(256) void logprob_part_kernel(const LogprobArgs p) {
+  constexpr int E = 16 / sizeof(T), V = kLogitsThread / E;  // logits a load, loads
+  __shared__ float max_sh[4];
+  __shared__ float4 sum_sh[4];
+  __shared__ TopShared256 top_sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.y, part = blockIdx.x;
+  if (p.masked && p.masked[row] == 0) return;
+  const T* z_row = static_cast<const T*>(p.logits) + (int64_t)row * p.row_stride;
+  const int first = part * kLogitsPart + tid * E;
+  auto id_at = [&](int i) __attribute__((always_inline)) { return first + (i / E) * (256 * E) + i % E; };
+  float z[kLogitsThread];
+  uint4 w[V];
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    const int id = first + k * 256 * E;
+    if (id + E <= p.vocab) w[k] = *reinterpret_cast<const uint4*>(z_row + id);
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    const int id = first + k * 256 * E;
+    if (id + E <= p.vocab) {
+      const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        z[k * E + e] = tame(sizeof(T) == 4 ? __uint_as_float(u[e & 3]) : ((e & 1) ? bf16_hi(u[(e >> 1) & 3]) : bf16_lo(u[(e >> 1) & 3])));
+    } else {  // a row's last, shorter piece, logit by logit
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        z[k * E + e] = -INFINITY;
+        if (id + e < p.vocab) {
+          if constexpr (sizeof(T) == 4)
+            z[k * E + e] = tame(*reinterpret_cast<const float*>(z_row + id + e));
+          else
+            z[k * E + e] = tame(bf16_lo(*reinterpret_cast<const uint16_t*>(z_row + id + e)));
+        }
+      }
+    }
+  }
+  float mine = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kLogitsThread; ++i) mine = fmaxf(mine, z[i]);
+  const float m = block_max4(mine, max_sh), m_use = m == -INFINITY ? 0.f : m;
+
+  float rest = 0.f, A = 0.f, equal = 0.f;  // of the logits below m; how many equal it
+  auto add = [&](auto careful) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kLogitsThread; ++i) {
+      const float y = fmaxf((z[i] - m_use) * kLog2eF, kNothing), e = __builtin_amdgcn_exp2f(y);
+      A = __builtin_fmaf(e, y, A);
+      if constexpr (decltype(careful)::value) {
+        rest += z[i] == m ? 0.f : e;
+        equal += z[i] == m ? 1.f : 0.f;
+      } else {
+        rest += e;
+      }
+    }
+  };
+  if (__ballot(mine == m) != 0ull)
+    add(std::true_type{});
+  else
+    add(std::false_type{});
+  rest = wave_sum(rest);
+  A = wave_sum(A);
+  equal = wave_sum(equal);
+  if (lane == 0) sum_sh[wave] = make_float4(rest, A, equal, 0.f);
+  __syncthreads();
+  if (tid == 0) {
+    float r = 0.f, a = 0.f, n = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      r += sum_sh[k].x;
+      a += sum_sh[k].y;
+      n += sum_sh[k].z;
+    }
+    p.part[(int64_t)row * p.n_parts + part] = m == -INFINITY ? make_float4(-INFINITY, 0.f, 0.f, 0.f) : make_float4(m, r + (n - 1.f), a, 0.f);
+  }
+  if (p.top_n > 0) {
+    uint2* list = p.part_top + ((int64_t)row * p.n_parts + part) * p.top_n;
+    block_top<kLogitsThread, kLogitsThread>(
+        top_sh, top_key(mine), p.top_n,
+        [&](int i) __attribute__((always_inline)) { return top_key(z[i]); }, id_at, [&](int rank, uint32_t key, int id) { list[rank] = make_uint2(key, (uint32_t)id); });
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) {
+  constexpr int kEach = 32;  // entries of the parts' lists a thread
+  __shared__ float max_sh[4];
+  __shared__ float2 sum_sh[4];
+  __shared__ TopShared256 top_sh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x;
+  const bool live = !p.masked || p.masked[row] != 0;
+  int target = -1;
+  float z_t = -INFINITY;
+  if (p.targets && live) {
+    target = p.targets[row];
+    if (target >= 0 && target < p.vocab) {
+      const T* z = static_cast<const T*>(p.logits) + (int64_t)row * p.row_stride + target;
+      if constexpr (sizeof(T) == 4)
+        z_t = tame(*reinterpret_cast<const float*>(z));
+      else
+        z_t = tame(bf16_lo(*reinterpret_cast<const uint16_t*>(z)));
+    }
+  }
+  if (!live) {  // whole workgroup
+    if (tid == 0) {
+      if (p.logprob) p.logprob[row] = 0.f;
+      if (p.entropy) p.entropy[row] = 0.f;
+    }
+    for (int i = tid; i < p.top_n; i += 256) {
+      p.top_ids[(int64_t)row * p.top_n + i] = -1;
+      p.top_logprobs[(int64_t)row * p.top_n + i] = -INFINITY;
+    }
+    return;
+  }
+  float4 s = make_float4(-INFINITY, 0.f, 0.f, 0.f);  // at most 256 parts: one a thread
+  if (tid < p.n_parts) s = p.part[(int64_t)row * p.n_parts + tid];
+  const float m = block_max4(s.x, max_sh), m_use = m == -INFINITY ? 0.f : m;
+  // Of the parts whose largest logit is the row's the first one's is left out of r
+  const unsigned long long top = __ballot(s.x == m && m != -INFINITY);
+  int before = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) before += w < wave && max_sh[w] == m ? 1 : 0;
+  const bool first = before == 0 && top != 0ull && lane == __builtin_ctzll(top | (1ull << 63));
+  const float d = fmaxf((s.x - m_use) * kLog2eF, kNothing), f = __builtin_amdgcn_exp2f(d);
+  const float whole = s.x == -INFINITY ? 0.f : 1.f + s.y;
+  const float r_mine = wave_sum(first ? s.y : f * whole), a_mine = wave_sum(f * (s.z + whole * d));
+  if (lane == 0) sum_sh[wave] = make_float2(r_mine, a_mine);
+  __syncthreads();
+  float r = 0.f, a = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    r += sum_sh[w].x;
+    a += sum_sh[w].y;
+  }
+  const float log_sum = log1pf(r);
+  if (tid == 0) {
+    if (p.logprob) p.logprob[row] = target < 0 || target >= p.vocab ? 0.f : (m == -INFINITY ? -INFINITY : (z_t - m) - log_sum);
+    if (p.entropy) p.entropy[row] = m == -INFINITY ? 0.f : log_sum - kLn2F * a / (1.f + r);
+  }
+  if (p.top_n == 0) return;
+  const uint2* list = p.part_top + (int64_t)row * p.n_parts * p.top_n;
+  const int n = p.n_parts * p.top_n;  // <= 256 * kEach
+  uint32_t best = 0u;
+  for (int i = tid; i < n; i += 256) best = max(best, list[i].x);
+  block_top<kEach, 4>(
+      top_sh, best, p.top_n, [&](int i) { return tid + 256 * i < n ? list[tid + 256 * i].x : 0u; }, [&](int i) { return (int)list[tid + 256 * i].y; },
+      [&](int rank, uint32_t key, int id) {
+        p.top_ids[(int64_t)row * p.top_n + rank] = id;
+        p.top_logprobs[(int64_t)row * p.top_n + rank] = id < 0 ? -INFINITY : (order_value(key) - m) - log_sum;
+      });
+}
+
+static size_t logprob_parts_bytes(int n_rows, int n_parts) { return (size_t)n_rows * n_parts * sizeof(float4); }
+size_t token_logprobs_workspace(int n_rows, int vocab, int top_n) {
+  const int n_parts = ceil_div(vocab, kLogitsPart);
+  return logprob_parts_bytes(n_rows, n_parts) + (size_t)n_rows * n_parts * top_n * sizeof(uint2);
+}
+
+template <class T>
+static hipError_t launch_logprobs_t(const LogprobArgs& p, int n_rows, hipStream_t st) {
+  hipLaunchKernelGGL(logprob_part_kernel<T>, dim3(p.n_parts, n_rows), dim3(256), 0, st, p);
+  hipLaunchKernelGGL(logprob_join_kernel<T>, dim3(n_rows), dim3(256), 0, st, p);
+  return hipGetLastError();
+}
+hipError_t launch_token_logprobs(const void* logits, int dtype, int64_t row_stride, const int32_t* targets, const uint8_t* masked, int n_rows, int vocab,
+                                 int top_n, float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace, hipStream_t st) {
+  LogprobArgs p;
+  p.logits = logits;
+  p.targets = targets;
+  p.masked = masked;
+  p.logprob = logprob;
+  p.entropy = entropy;
+  p.top_ids = top_ids;
+  p.top_logprobs = top_logprobs;
+  p.row_stride = row_stride;
+  p.vocab = vocab;
+  p.n_parts = ceil_div(vocab, kLogitsPart);
+  p.top_n = top_n;
+  p.part = static_cast<float4*>(workspace);
+  p.part_top = reinterpret_cast<uint2*>(static_cast<char*>(workspace) + logprob_parts_bytes(n_rows, p.n_parts));
+  return dtype == FOCUS_F32 ? launch_logprobs_t<float>(p, n_rows, st) : launch_logprobs_t<uint16_t>(p, n_rows, st);
+}
+
+}  // namespace focus

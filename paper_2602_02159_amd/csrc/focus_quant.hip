@@ -15,14 +15,11 @@
 
 #include "focus_attn.h"
 #include "focus_cache.h"
+#include "focus_codes.h"
 #include "focus_common.h"
 #include "focus_kernels.h"
 
 namespace focus {
-
-constexpr int kExpMin = 127 - 110, kExpMax = 127 + 119;  // as stored
-
-__device__ __forceinline__ float exp_value(uint32_t byte) { return __uint_as_float(byte << 23); }  // 2^(byte - 127), 0 for 0
 
 // The rows of a wavefront's lanes, eight values a lane: N = D / 8 neighbouring lanes hold one row.  Its power of two, as stored.
 template <int N>
@@ -40,22 +37,12 @@ __device__ __forceinline__ uint32_t row_exponent(const uint4& x) {
 
 // eight values as codes; `inv` = 2^-E
 __device__ __forceinline__ uint2 encode8(const uint4& x, float inv) {
-  auto scaled = [&](float v) {  // the limit matters for rows whose E is at its upper end only; infinities and NaN take the NaN code
-    const float y = fminf(fmaxf(v * inv, -448.f), 448.f);
-    return fabsf(v) < INFINITY ? y : __builtin_nanf("");
-  };
+  auto scaled = [&](float v) { return scaled_for_code(v, inv); };
   auto four = [&](uint32_t a, uint32_t b) {
     int w = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(bf16_lo(a)), scaled(bf16_hi(a)), 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(scaled(bf16_lo(b)), scaled(bf16_hi(b)), w, true);
   };
   return make_uint2(four(x.x, x.y), four(x.z, x.w));
-}
-__device__ __forceinline__ uint32_t decode2(uint32_t codes, bool high, float scale) {  // two of the four codes as a bf16 pair, times 2^E
-  return high ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true))
-              : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false));
-}
-__device__ __forceinline__ uint4 decode8(const uint2& c, float scale) {
-  return make_uint4(decode2(c.x, false, scale), decode2(c.x, true, scale), decode2(c.y, false, scale), decode2(c.y, true, scale));
 }
 
 // ---------------------------------------------------------------------------------------- writing and reading
@@ -290,26 +277,6 @@ struct QuantTile {
   uint32_t v[8][D / 64];
   uint32_t e;  // exponent of row lane % 32, of K in the lower half of the wavefront, of V in the upper
 };
-
-// STREAM: rows that one workgroup alone reads pass the caches by (load_stream16)
-template <bool STREAM, class V>
-__device__ __forceinline__ V load_row_piece(const uint8_t* p) {
-  return STREAM ? __builtin_nontemporal_load(reinterpret_cast<const V*>(p)) : *reinterpret_cast<const V*>(p);
-}
-template <int D, bool STREAM>
-__device__ __forceinline__ void load_codes(uint32_t (&v)[D / 64], const uint8_t* p) {
-  if constexpr (D == 128) {
-    const uintx2 w = load_row_piece<STREAM, uintx2>(p);
-    v[0] = w.x;
-    v[1] = w.y;
-  } else {
-    v[0] = load_row_piece<STREAM, uint32_t>(p);
-  }
-}
-template <bool STREAM>
-__device__ __forceinline__ uint4 load_codes16(const uint8_t* p) {
-  return __builtin_bit_cast(uint4, load_row_piece<STREAM, uintx4>(p));
-}
 
 // `exps`: the exponents of the head, of K or V by the half of the wavefront.  Requires t.vmask != 0; slots without a key read another
 // row of the key set, as in issue_subtile_part.
