@@ -1209,7 +1209,9 @@ int focus_paged_attn(const void* Q, int64_t q_stride_h, int64_t q_stride_n, int3
   p.page = cache->page;
   p.n_pages = cache->n_pages;
   p.causal = causal != 0;
+  p.page_shift = (cache->page & (cache->page - 1)) == 0 ? __builtin_ctz(cache->page) : -1;
   p.workers = plan.workers;
+  p.log_bundle = plan.log_bundle;
   p.unit_rows = plan.unit_rows;
   p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cache->head_dim));
   p.part_o = static_cast<float*>(workspace);

@@ -213,13 +213,15 @@ struct PagedAttn {
   int64_t ksp, ksh, ksn, vsp, vsh, vsn, esp, esh, esn;  // of the cache, in bytes
   PagedBatch b;
   int H, group, page, n_pages, causal;
-  int workers;      // wavefronts among which the tiles of all requests are divided
+  int page_shift;   // log2 of page, or -1
+  int log_bundle;   // K/V heads of a bundle, which as many wavefronts of a workgroup take together
+  int workers;      // bundles of wavefronts, among which the tiles of all requests are divided
   int unit_rows;    // rows of a partial result
   float scale_log2;
 };
 struct PagedPlan {
   int q_tiles;      // 16-query tiles of a unit: 1 or 2
-  int unit_rows, workers;
+  int unit_rows, log_bundle, workers, groups;
   size_t part_ml, total;
 };
 PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch& b, int page);

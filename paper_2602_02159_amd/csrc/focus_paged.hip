@@ -1,10 +1,11 @@
 // Attention of the requests' few new rows over their pages.
 //
 // The keys of a request are cut into tiles of 32, and a unit is what shares them: the rows of a request times the query heads of one K/V head, sixteen
-// (or 32) of those at a time.  All tiles of all units, in the order request, head, group of rows, tile, are divided evenly among the wavefronts
+// (or 32) of those at a time.  All tiles of all units, in the order request, heads, group of rows, tile, are divided evenly among the wavefronts
 // of one launch, by the lengths that they find in memory: a batch of one long and many short requests keeps the whole chip busy, and a captured graph
 // does so for lengths that nobody knew when it was captured.  A wavefront keeps the running softmax of the unit that it is in; a unit that
-// lies within one wavefront is written out by it, the pieces of the others go to the workspace, and a second launch joins them.
+// lies within one wavefront is written out by it, the pieces of the others go to the workspace, and a second launch joins them.  The wavefronts of
+// a workgroup take neighbouring heads of the same tiles: where the heads of a row lie side by side their rows are then fetched at about the same time.
 //
 // The products are those of the attention over the quantised cache: rows go from memory straight into the registers in which
 // v_mfma_f32_16x16x32_bf16 takes them.
@@ -58,7 +59,11 @@ __device__ __forceinline__ uint32_t head_tiles(const PagedAttn& p, int r) {
 }
 
 __device__ __forceinline__ uint32_t wave_total(uint32_t x) {
-  return wave_reduce_u32(x, [](uint32_t a, uint32_t b) { return a + b; });
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)wave_reduce_u32(x, [](uint32_t a, uint32_t b) { return a + b; }));
+}
+// a number that is the same in all lanes, in scalar registers: what follows from it is worked out once a wavefront
+__device__ __forceinline__ int64_t same(int64_t x) {
+  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
 }
 
 // The requests' tiles as one wavefront adds them up, 64 requests a turn; those of the first kKept turns stay in registers.
@@ -112,120 +117,244 @@ struct Prefix {
   }
 };
 
-// The tiles of all requests, R of them, among W wavefronts: floor(i R / W) is the first one of wavefront i.
+// The tiles of all requests, R of them, among W wavefronts: floor(i R / W) is the first one of wavefront i.  Quotients in 64-bit floating
+// point, put right by one where they are next to a whole number (a division of 64-bit integers takes longer than a round trip to L2).
 struct Shares {
   int64_t base;  // R = base * W + rest
-  uint32_t rest, workers;
-  __device__ __forceinline__ Shares(int64_t R, int W) {
-    base = R / W;
-    rest = (uint32_t)(R - base * W);
-    workers = (uint32_t)W;
+  int rest, workers;
+  double per_worker;  // 1 / W
+  __device__ __forceinline__ Shares(int64_t R, int W) : workers(W) {
+    per_worker = 1.0 / (double)W;
+    base = (int64_t)((double)R * per_worker);
+    rest = (int)(R - base * W);
+    if (rest < 0) rest += W, --base;
+    if (rest >= W) rest -= W, ++base;
   }
-  __device__ __forceinline__ int64_t begin(int i) const { return base * i + rest * (uint32_t)i / workers; }  // W <= 2^16
+  // floor(rest i / W): rest i + 1/2 is at least 1 / (2 W) from the next multiple of W
+  __device__ __forceinline__ int64_t begin(int i) const { return base * i + (int)(((double)(rest * i) + 0.5) * per_worker); }
   // the last wavefront that begins with tile s or before it
   __device__ __forceinline__ int of(int64_t s) const {
-    const double per = (double)base + (double)rest / (double)workers;
-    int i = min(max((int)((double)s / per), 0), (int)workers - 1);
+    int i = (int)(((double)s + 0.5) / ((double)base + (double)rest * per_worker));
+    i = min(max(i, 0), workers - 1);
     while (i > 0 && begin(i) > s) --i;
-    while (i + 1 < (int)workers && begin(i + 1) <= s) ++i;
+    while (i + 1 < workers && begin(i + 1) <= s) ++i;
     return i;
   }
 };
 
-// A tile's place
-struct Tile {
+// A group of rows of a request and a bundle of K/V heads, one a wavefront
+struct Unit {
   Request q;
-  int r, h, qg, t;
-  bool first, last;  // of the piece of its unit that the wavefront has
+  int r, b, qg;
 };
 
+// The rows of a tile lie in LDS between memory and the products: every wavefront has a ring of its own, 32 KB of rows, whose loads go to LDS
+// directly and are waited for by their number.  (The same bytes under way in registers cost two more copies of the code, or wavefronts that wait
+// for one tile at a time: 32 heads, 32 832 keys 91.5 us.)
 template <int D, bool QUANT>
-struct TileRows {
-  static constexpr int kK = QUANT ? D / 64 : D / 32, kV = QUANT ? D / 64 : D / 32;  // 16-byte pieces of a K row, dwords of a V row's piece
-  uint4 k[2][kK];
-  uint32_t v[8][kV];
-  uint32_t e;     // QUANT: exponent of row lane % 32, of K in the lower half of the wavefront, of V in the upper
+struct Ring {
+  static constexpr int kRow = QUANT ? D : 2 * D, kRows = kTile * kRow;  // bytes of a row, of a tile's K (or V)
+  static constexpr int kChunks = kRow / 16, kPerLoad = 64 / kChunks, kLoads = kTile / kPerLoad;
+  static constexpr int kDepth = 8192 / kRows;  // tiles
+  static constexpr int kExps = QUANT ? 256 : 0;  // an exponent a row, in 32 bits: of K, of V
+  static constexpr int kStage = 2 * kRows + kExps, kTileLoads = 2 * kLoads + (QUANT ? 1 : 0);
+  static constexpr int kBytes = kDepth * kStage;
+  // chunk `x` of a row lies at place x ^ turn(row): reads of one chunk of several rows meet different banks
+  static __device__ __forceinline__ int turn(int row) { return kRow == 64 ? (row >> 1) & 3 : row & (kChunks - 1); }
+};
+typedef const __attribute__((address_space(1))) void* gptr_t;
+typedef __attribute__((address_space(3))) void* lptr_t;
+
+// Pages as a wavefront holds them: lane l has entry `first` + l of request r's table.
+struct Window {
+  int r, first, entry;
+};
+// Where the rows of a tile lie.  Slots without a key take another row of the tile, all of them row 0 of page 0 where it has none (what
+// is read there is not used, but zero times an infinity would be).
+struct TilePlace {
   uint32_t mask;  // bit s: slot s holds a key
+  bool plain;     // every slot does, and sixteen rows lie in one page: page0, at0 and page1, at1; else page and at of slot lane % 32
+  int page0, at0, page1, at1, page, at;
 };
-
-template <int N>
-__device__ __forceinline__ void load_piece(uint32_t (&v)[N], const uint8_t* p) {
-  if constexpr (N == 4) {
-    const uintx4 w = *reinterpret_cast<const uintx4*>(p);
-    v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
-  } else if constexpr (N == 2) {
-    const uintx2 w = *reinterpret_cast<const uintx2*>(p);
-    v[0] = w.x; v[1] = w.y;
-  } else {
-    v[0] = *reinterpret_cast<const uint32_t*>(p);
+__device__ __forceinline__ TilePlace locate(const PagedAttn& p, const Unit& u, int t, Window& win, int lane) {
+  TilePlace x;
+  x.page = x.at = x.page0 = x.page1 = x.at0 = x.at1 = 0;
+  x.mask = 0u;
+  x.plain = false;
+  const int row0 = t * kTile, n = min(u.q.len - row0, kTile);
+  if (n <= 0) return x;
+  auto entry_of = [&](int row) __attribute__((always_inline)) { return p.page_shift >= 0 ? row >> p.page_shift : row / p.page; };
+  const int e0 = entry_of(row0), e_last = entry_of(row0 + n - 1);
+  if (u.r != win.r || e0 < win.first || e_last >= win.first + kWave) {
+    win.r = u.r;
+    win.first = e0;
+    win.entry = p.b.page_table[(int64_t)u.r * p.b.table_stride + min(e0 + lane, p.b.table_width - 1)];
   }
-}
-
-// page of slot lane % 32 of a tile (any entry for slots past the keys)
-__device__ __forceinline__ int load_entry(const PagedAttn& p, const Tile& t, int lane) {
-  const int row = min(t.t * kTile + (lane & 31), max(t.q.len - 1, 0));
-  return p.b.page_table[(int64_t)t.r * p.b.table_stride + row / p.page];
-}
-
-// Rows of a tile; `entry` from load_entry.  Slots without a key read another row of the tile, all of them row 0 of page 0 where it has none
-// (what is read there is not used, but zero times an infinity would be).
-template <int D, bool QUANT>
-__device__ __forceinline__ void load_tile_rows(TileRows<D, QUANT>& x, const PagedAttn& p, const Tile& t, int entry, int lane) {
-  constexpr int kPiece = D / 16 * (QUANT ? 1 : 2);  // bytes of a V row that a lane takes
-  const int c = lane & 15, g = lane >> 4, row0 = t.t * kTile;
-  const int mine = min(row0 + (lane & 31), max(t.q.len - 1, 0));
-  const bool there = row0 + (lane & 31) < t.q.len && entry >= 0 && entry < p.n_pages;
+  if (n == kTile && (p.page & 15) == 0) {
+    const int e1 = entry_of(row0 + 16);
+    x.page0 = __builtin_amdgcn_readlane(win.entry, e0 - win.first);
+    x.page1 = __builtin_amdgcn_readlane(win.entry, e1 - win.first);
+    x.at0 = row0 - e0 * p.page;
+    x.at1 = row0 + 16 - e1 * p.page;
+    if ((uint32_t)x.page0 < (uint32_t)p.n_pages && (uint32_t)x.page1 < (uint32_t)p.n_pages) {
+      x.plain = true;
+      x.mask = 0xffffffffu;
+      return x;
+    }
+  }
+  const int row = row0 + min(lane & 31, n - 1), e = entry_of(row);
+  const int entry = __shfl(win.entry, e - win.first, kWave), at = row - e * p.page;
+  const bool there = (lane & 31) < n && entry >= 0 && entry < p.n_pages;
   x.mask = (uint32_t)__ballot(there);  // (the upper half of the wavefront repeats the lower one)
-  const uint8_t* Kh = p.K + (int64_t)t.h * p.ksh;
-  const uint8_t* Vh = p.V + (int64_t)t.h * p.vsh;
-  if (x.mask == 0xffffffffu && (p.page & 15) == 0) {  // sixteen rows lie in one page
-    const int page0 = __builtin_amdgcn_readlane(entry, 0), page1 = __builtin_amdgcn_readlane(entry, 16);
-    const int at0 = row0 % p.page, at1 = (row0 + 16) % p.page;
-    const uint8_t* kp[2] = {Kh + (int64_t)page0 * p.ksp + (int64_t)at0 * p.ksn, Kh + (int64_t)page1 * p.ksp + (int64_t)at1 * p.ksn};
-    const uint8_t* vp[2] = {Vh + (int64_t)page0 * p.vsp + (int64_t)at0 * p.vsn, Vh + (int64_t)page1 * p.vsp + (int64_t)at1 * p.vsn};
-    const uint32_t ko = (uint32_t)c * (uint32_t)p.ksn + (uint32_t)(g * 16), vo = (uint32_t)(4 * g) * (uint32_t)p.vsn + (uint32_t)(c * kPiece);
+  if (x.mask != 0u) {
+    const int from = there ? lane : __builtin_ctz(x.mask);
+    x.page = __shfl(entry, from, kWave);
+    x.at = __shfl(at, from, kWave);
+  }
+  return x;
+}
+__device__ __forceinline__ int64_t offset_of_slot(int64_t off, int slot) {
+  const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)off, slot, kWave), hi = (uint32_t)__shfl((int)(uint32_t)((uint64_t)off >> 32), slot, kWave);
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+// The rows of a tile to `stage`.  Lane l of load i supplies the 16 bytes that land at stage + 1024 i + 16 l: place l mod kChunks of row
+// i * kPerLoad + l / kChunks.
+template <int D, bool QUANT>
+__device__ __forceinline__ void request_rows(const uint8_t* base, int64_t stride_p, int64_t stride_n, TilePlace x, char* stage, int lane) {
+  using G = Ring<D, QUANT>;
+  const int sub = lane / G::kChunks, pos = lane % G::kChunks;
+  if (x.plain) {
+    const uint8_t* rows[2] = {base + (int64_t)x.page0 * stride_p + (int64_t)x.at0 * stride_n, base + (int64_t)x.page1 * stride_p + (int64_t)x.at1 * stride_n};
+    const uint32_t lane_row = (uint32_t)sub * (uint32_t)stride_n;  // (16 rows of the stride fit 32 bits)
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < x.kK; ++j) x.k[i][j] = *reinterpret_cast<const uint4*>(kp[i] + 64 * j + ko);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) load_piece(x.v[e], vp[e >> 2] + (e & 3) * p.vsn + vo);
-    if constexpr (QUANT) {
-      const int page = (lane & 16) ? page1 : page0, at = ((lane & 16) ? at1 : at0) + (lane & 15);
-      x.e = (lane < 32 ? p.k_exp : p.v_exp)[(int64_t)page * p.esp + (int64_t)t.h * p.esh + (int64_t)at * p.esn];
+    for (int i = 0; i < G::kLoads; ++i) {
+      const int slot = i * G::kPerLoad + sub, first = i * G::kPerLoad;
+      const uint8_t* src = rows[first >> 4] + (int64_t)(first & 15) * stride_n + (lane_row + (uint32_t)((pos ^ G::turn(slot)) << 4));
+      __builtin_amdgcn_global_load_lds((gptr_t)src, (lptr_t)(stage + i * 1024), 16, 0, kStreamPolicy);
     }
     return;
   }
-  int page = 0, at = 0;
-  if (x.mask != 0u) {
-    const int from = there ? lane : __builtin_ctz(x.mask);
-    page = __shfl(entry, from, kWave);
-    const int row = __shfl(mine, from, kWave);
-    at = row - row / p.page * p.page;
+  const int64_t mine = (int64_t)x.page * stride_p + (int64_t)x.at * stride_n;
+#pragma unroll
+  for (int i = 0; i < G::kLoads; ++i) {
+    const int slot = i * G::kPerLoad + sub;
+    const uint8_t* src = base + offset_of_slot(mine, slot) + ((pos ^ G::turn(slot)) << 4);
+    __builtin_amdgcn_global_load_lds((gptr_t)src, (lptr_t)(stage + i * 1024), 16, 0, kStreamPolicy);
   }
-  const int64_t k_off = (int64_t)page * p.ksp + (int64_t)at * p.ksn, v_off = (int64_t)page * p.vsp + (int64_t)at * p.vsn;
-  auto of_slot = [&](int64_t off, int slot) __attribute__((always_inline)) {
-    const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)off, slot, kWave), hi = (uint32_t)__shfl((int)(uint32_t)((uint64_t)off >> 32), slot, kWave);
-    return (int64_t)(((uint64_t)hi << 32) | lo);
-  };
+}
+// exponents of slot lane % 32, of K in the lower half of the wavefront, of V in the upper
+__device__ __forceinline__ void request_exponents(const PagedAttn& p, TilePlace x, int h, char* stage, int lane) {
+  const int page = x.plain ? ((lane & 16) ? x.page1 : x.page0) : x.page, at = x.plain ? ((lane & 16) ? x.at1 : x.at0) + (lane & 15) : x.at;
+  const uint8_t* src = (lane < 32 ? p.k_exp : p.v_exp) + (int64_t)page * p.esp + (int64_t)h * p.esh + (int64_t)at * p.esn;
+  __builtin_amdgcn_global_load_lds((gptr_t)src, (lptr_t)stage, 1, 0, 0);
+}
+
+// Operands from a stage, outside the compiler's sight and complete on return (read_k_operands16): it would wait for every load to LDS.
+// K codes: lane (c, g) has the chunks 4 j + g of the rows c and 16 + c
+template <int D>
+__device__ __forceinline__ void read_k_codes(uint4 (&k)[2][D / 64], const char* stage, int lane) {
+  using G = Ring<D, true>;
+  const int c = lane & 15, g = lane >> 4;
+  const uint32_t a = lds_address(stage) + c * G::kRow + ((g ^ G::turn(c)) << 4);
+  uintx4 x[2][D / 64];
+  if constexpr (D == 128)
+    asm volatile(
+        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %4 offset:2048\n\tds_read_b128 %3, %5 offset:2048\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0][0]), "=&v"(x[0][1]), "=&v"(x[1][0]), "=&v"(x[1][1])
+        : "v"(a), "v"(a ^ 64u)
+        : "memory");
+  else
+    asm volatile("ds_read_b128 %0, %2\n\tds_read_b128 %1, %2 offset:1024\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x[0][0]), "=&v"(x[1][0]) : "v"(a) : "memory");
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint8_t* k = Kh + of_slot(k_off, 16 * i + c) + 16 * g;
+  for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < x.kK; ++j) x.k[i][j] = *reinterpret_cast<const uint4*>(k + 64 * j);
+    for (int j = 0; j < D / 64; ++j) k[i][j] = __builtin_bit_cast(uint4, x[i][j]);
+}
+// V codes: lane (c, g) has D / 16 neighbouring codes, the c-th of a row, of the rows 4 g + e and 16 + 4 g + e
+template <int D>
+__device__ __forceinline__ void read_v_codes(uint32_t (&v)[8][D / 64], const char* stage, int lane) {
+  using G = Ring<D, true>;
+  const int c = lane & 15, g = lane >> 4;
+  if constexpr (D == 128) {  // turn(4 g + e) = 4 (g mod 2) ^ e
+    const uint32_t a = lds_address(stage) + 4 * g * G::kRow + (((c >> 1) ^ (4 * (g & 1))) << 4) + (c & 1) * 8;
+    uintx2 x[8];
+    asm volatile(
+        "ds_read_b64 %0, %8\n\tds_read_b64 %1, %9 offset:128\n\tds_read_b64 %2, %10 offset:256\n\tds_read_b64 %3, %11 offset:384\n\t"
+        "ds_read_b64 %4, %8 offset:2048\n\tds_read_b64 %5, %9 offset:2176\n\tds_read_b64 %6, %10 offset:2304\n\tds_read_b64 %7, %11 offset:2432\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+        : "v"(a), "v"(a ^ 16u), "v"(a ^ 32u), "v"(a ^ 48u)
+        : "memory");
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      v[e][0] = x[e].x;
+      v[e][1] = x[e].y;
+    }
+  } else {  // turn(4 g + e) = 2 (g mod 2) ^ e / 2
+    const uint32_t a = lds_address(stage) + 4 * g * G::kRow + (((c >> 2) ^ (2 * (g & 1))) << 4) + (c & 3) * 4;
+    asm volatile(
+        "ds_read_b32 %0, %8\n\tds_read_b32 %1, %8 offset:64\n\tds_read_b32 %2, %9 offset:128\n\tds_read_b32 %3, %9 offset:192\n\t"
+        "ds_read_b32 %4, %8 offset:1024\n\tds_read_b32 %5, %8 offset:1088\n\tds_read_b32 %6, %9 offset:1152\n\tds_read_b32 %7, %9 offset:1216\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(v[0][0]), "=&v"(v[1][0]), "=&v"(v[2][0]), "=&v"(v[3][0]), "=&v"(v[4][0]), "=&v"(v[5][0]), "=&v"(v[6][0]), "=&v"(v[7][0])
+        : "v"(a), "v"(a ^ 16u)
+        : "memory");
   }
+}
+// 2^E of the rows 4 g + i and 16 + 4 g + i, of K and of V
+__device__ __forceinline__ void read_exponents(floatx4 (&ek)[2], floatx4 (&ev)[2], const char* stage, int lane) {
+  const uint32_t a = lds_address(stage) + 16 * (lane >> 4);
+  uintx4 x[4];
+  asm volatile(
+      "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:64\n\tds_read_b128 %2, %4 offset:128\n\tds_read_b128 %3, %4 offset:192\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3])
+      : "v"(a)
+      : "memory");
 #pragma unroll
-  for (int e = 0; e < 8; ++e) load_piece(x.v[e], Vh + of_slot(v_off, 16 * (e >> 2) + 4 * g + (e & 3)) + c * kPiece);
-  if constexpr (QUANT) x.e = (lane < 32 ? p.k_exp : p.v_exp)[(int64_t)page * p.esp + (int64_t)t.h * p.esh + (int64_t)at * p.esn];
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      ek[i][e] = exp_value(x[i][e]);
+      ev[i][e] = exp_value(x[2 + i][e]);
+    }
+}
+
+// Sixteen bytes of a stage, as above; the reads and writes of a wavefront keep their order
+__device__ __forceinline__ uint4 read_chunk(const char* at) {
+  uintx4 x;
+  asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x) : "v"(lds_address(at)) : "memory");
+  return __builtin_bit_cast(uint4, x);
+}
+// Whether one of two bf16 numbers, or of four codes, is an infinity or a NaN
+template <bool QUANT>
+__device__ __forceinline__ bool beyond_finite(uint32_t w) {
+  if (QUANT) return ((~w & 0x7fu) == 0u) | ((~w & 0x7f00u) == 0u) | ((~w & 0x7f0000u) == 0u) | ((~w & 0x7f000000u) == 0u);
+  return ((~w & 0x7f80u) == 0u) | ((~w & 0x7f800000u) == 0u);
+}
+// Rewrites the numbers of a word of a stage: which = 0: zero in the place of infinities and NaN; 1: one where +inf or NaN is, zero elsewhere; 2: of
+// -inf or NaN
+template <bool QUANT>
+__device__ __forceinline__ void rewrite_word(const char* at, int which) {
+  constexpr int kBits = QUANT ? 8 : 16;
+  uint32_t w, y = 0u;
+  asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(w) : "v"(lds_address(at)) : "memory");
+#pragma unroll 1
+  for (int shift = 0; shift < 32; shift += kBits) {
+    const uint32_t z = (w >> shift) & ((1u << kBits) - 1u), size = z & ((1u << (kBits - 1)) - 1u), limit = QUANT ? 0x7fu : 0x7f80u;
+    const bool nan = QUANT ? size == limit : size > limit, mine = nan || (size == limit && (z != size) == (which == 2));
+    y |= (which == 0 ? (size < limit ? z : 0u) : (mine ? (QUANT ? 0x38u : 0x3f80u) : 0u)) << shift;
+  }
+  asm volatile("ds_write_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : : "v"(lds_address(at)), "v"(y) : "memory");
 }
 
 // Query rows of tile n of a unit: lane (c, g) has row 16 n + c in the order of the K rows' pieces, zeros past the unit's rows
 template <int D, bool QUANT>
-__device__ __forceinline__ void load_queries(bf16x8 (&q)[D / 32], const PagedAttn& p, const Tile& t, int at, int lane) {
+__device__ __forceinline__ void load_queries(bf16x8 (&q)[D / 32], const PagedAttn& p, const Unit& t, int h, int at, int lane) {
   const int g = lane >> 4, i = at / p.group;
   const bool there = i < t.q.n;
   const int64_t row = t.q.first + (there ? i : 0);
-  const uint16_t* src = p.Q + row * p.qsn + (int64_t)(t.h * p.group + (there ? at - i * p.group : 0)) * p.qsh + (QUANT ? 16 * g : 8 * g);
+  const uint16_t* src = p.Q + row * p.qsn + (int64_t)(h * p.group + (there ? at - i * p.group : 0)) * p.qsh + (QUANT ? 16 * g : 8 * g);
 #pragma unroll
   for (int kk = 0; kk < D / 32; ++kk) {
     const uint4 v = *reinterpret_cast<const uint4*>(src + (QUANT ? 64 * (kk >> 1) + 8 * (kk & 1) : 32 * kk));
@@ -233,72 +362,82 @@ __device__ __forceinline__ void load_queries(bf16x8 (&q)[D / 32], const PagedAtt
   }
 }
 
-// workgroups per compute unit, by the registers
-static constexpr int groups_per_cu(int head_dim, int q_tiles) { return head_dim == 64 && q_tiles == 1 ? 3 : 2; }
-template <int D, bool QUANT, int NT>
-__global__ __launch_bounds__(256, groups_per_cu(D, NT)) void paged_attn_kernel(const PagedAttn p) {
-  constexpr int kKS = D / 32, kCT = D / 16, kV = TileRows<D, QUANT>::kV, kVec = D / 64;
-  __shared__ __attribute__((aligned(16))) float exps_sh[QUANT ? 4 : 1][64];
+template <int D, bool QUANT, bool CAUSAL, int NT>
+__global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
+  using G = Ring<D, QUANT>;
+  constexpr int kKS = D / 32, kCT = D / 16, kDepth = G::kDepth;
+  __shared__ __attribute__((aligned(256))) char ring_sh[kWavesPerGroup * G::kBytes];
   const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int worker = (int)blockIdx.x * 4 + wave;
+  const int in_bundle = wave & ((1 << p.log_bundle) - 1), bundles = p.H >> p.log_bundle;
+  const int wave_id = (int)blockIdx.x * kWavesPerGroup + wave, worker = wave_id >> p.log_bundle;
+  char* ring = ring_sh + wave * G::kBytes;
 
   const Prefix<NT> prefix(p, lane);
-  const Shares shares((int64_t)prefix.total * p.H, p.workers);
-  const int64_t begin = shares.begin(worker);
-  const int n_tiles = (int)(shares.begin(worker + 1) - begin);
+  const Shares shares((int64_t)prefix.total * bundles, p.workers);
+  const int64_t begin = same(shares.begin(worker));
+  const int n_tiles = (int)(same(shares.begin(worker + 1)) - begin);
   if (n_tiles <= 0) return;
 
-  Tile here;
+  Unit u;  // of the tile that is worked on,
+  int t;
   {
     uint32_t before;
-    here.r = prefix.find(p, (uint32_t)((uint64_t)begin / (uint32_t)p.H), before, lane);
-    here.q = load_request<NT>(p, here.r);
-    const uint32_t local = (uint32_t)(begin - (int64_t)before * p.H), unit = local / (uint32_t)here.q.tiles;
-    here.t = (int)(local - unit * (uint32_t)here.q.tiles);
-    here.h = (int)(unit / (uint32_t)here.q.groups);
-    here.qg = (int)unit - here.h * here.q.groups;
-    here.first = true;
-    here.last = here.t == here.q.tiles - 1 || n_tiles == 1;
+    u.r = prefix.find(p, (uint32_t)((uint64_t)begin / (uint32_t)bundles), before, lane);
+    u.q = load_request<NT>(p, u.r);
+    const uint32_t local = (uint32_t)(begin - (int64_t)before * bundles), unit = local / (uint32_t)u.q.tiles;
+    t = (int)(local - unit * (uint32_t)u.q.tiles);
+    u.b = (int)(unit / (uint32_t)u.q.groups);
+    u.qg = (int)unit - u.b * u.q.groups;
   }
-  // the tile behind `t`, the i-th of the wavefront
-  auto advance = [&](Tile t, int i) __attribute__((always_inline)) {
-    ++t.t;
-    t.first = t.t >= t.q.tiles;
-    if (t.first) {
-      t.t = 0;
-      ++t.qg;
-      if (t.qg >= t.q.groups) {
-        t.qg = 0;
-        ++t.h;
-        if (t.h >= p.H) {
-          t.h = 0;
-          do {  // requests without a row have no tile
-            ++t.r;
-            t.q = load_request<NT>(p, t.r);
-          } while (t.q.n == 0);
-        }
-      }
-    }
-    t.last = t.t == t.q.tiles - 1 || i == n_tiles - 1;
-    return t;
+  Unit ahead = u;  // and of the one to be requested next
+  int t_ahead = t, asked = 0;
+  auto next_unit = [&](Unit& x) __attribute__((always_inline)) {
+    if (++x.qg < x.q.groups) return;
+    x.qg = 0;
+    if (++x.b < bundles) return;
+    x.b = 0;
+    do {  // requests without a row have no tile
+      ++x.r;
+      x.q = load_request<NT>(p, x.r);
+    } while (x.q.n == 0);
   };
-
+  Window window{-1, 0, 0};
+  TilePlace place;
+  int masks = 0;  // lane l: the mask of the tile in stage l
+  auto stage_of = [&](int i) __attribute__((always_inline)) { return ring + (i & (kDepth - 1)) * G::kStage; };
+  auto head_of = [&](const Unit& x) __attribute__((always_inline)) { return (x.b << p.log_bundle) + in_bundle; };
+  auto request_k = [&]() __attribute__((always_inline)) {
+    place = locate(p, ahead, t_ahead, window, lane);
+    char* stage = stage_of(asked);
+    if constexpr (QUANT) request_exponents(p, place, head_of(ahead), stage + 2 * G::kRows, lane);
+    request_rows<D, QUANT>(p.K + (int64_t)head_of(ahead) * p.ksh, p.ksp, p.ksn, place, stage, lane);
+    masks = lane == (asked & (kDepth - 1)) ? (int)place.mask : masks;
+  };
+  auto request_v = [&]() __attribute__((always_inline)) {
+    request_rows<D, QUANT>(p.V + (int64_t)head_of(ahead) * p.vsh, p.vsp, p.vsn, place, stage_of(asked) + G::kRows, lane);
+    ++asked;
+    if (++t_ahead >= ahead.q.tiles && asked < n_tiles) {
+      t_ahead = 0;
+      next_unit(ahead);
+    }
+  };
   bf16x8 q[NT][kKS];
   int limit[NT];  // keys that the lane's row may attend to
   float m_run[NT], l_run[NT];
   floatx4 o[NT][kCT];
-
-  auto begin_unit = [&](const Tile& t) __attribute__((always_inline)) {
+  // Column tile ct of O^T: bf16 rows, the columns 16 ct + c; codes, the columns c * D / 16 + ct.  Rows of a tile are in lane (c, g) the columns ...
+  // ... of query row c.
+  auto begin_unit = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int at = (t.qg * NT + n) * 16 + c;
-      load_queries<D, QUANT>(q[n], p, t, at, lane);
-      limit[n] = t.q.len;
-      if (p.causal) {
-        const int i = min(at / p.group, max(t.q.n - 1, 0));
-        const int position = p.b.positions ? p.b.positions[t.q.first + i] : max(p.b.seq_len[t.r], 0) - t.q.count + i;
-        limit[n] = min(position, t.q.len - 1) + 1;
+      const int at = (u.qg * NT + n) * 16 + c;
+      load_queries<D, QUANT>(q[n], p, u, head_of(u), at, lane);
+      limit[n] = u.q.len;
+      if constexpr (CAUSAL) {
+        const int i = min(at / p.group, max(u.q.n - 1, 0));
+        const int position = p.b.positions ? p.b.positions[u.q.first + i] : max(p.b.seq_len[u.r], 0) - u.q.count + i;
+        limit[n] = min(position, u.q.len - 1) + 1;
       }
       m_run[n] = -INFINITY;
       l_run[n] = 0.f;
@@ -307,216 +446,223 @@ __global__ __launch_bounds__(256, groups_per_cu(D, NT)) void paged_attn_kernel(c
     }
   };
 
-  // operands of the second product for the columns 2 w and 2 w + 1 (codes: 4 w + i) of a lane's piece
-  auto v_operand = [&](const uint32_t (&v)[8][kV], int w, int i) __attribute__((always_inline)) {
-    uint32_t s[4];
-    if constexpr (QUANT) {
+  // S of a tile: lane (c, g) has the logits of row c and the keys 4 g + i, 16 + 4 g + i
+  auto multiply_k = [&](floatx4 (&acc)[NT][2], const char* stage) __attribute__((always_inline)) {
 #pragma unroll
-      for (int m = 0; m < 4; ++m) s[m] = decode2(__builtin_amdgcn_perm(v[2 * m + 1][w], v[2 * m][w], i < 2 ? 0x05010400u : 0x07030602u), i & 1, 1.f);
-    } else {
-#pragma unroll
-      for (int m = 0; m < 4; ++m) s[m] = __builtin_amdgcn_perm(v[2 * m + 1][w], v[2 * m][w], i == 0 ? 0x05040100u : 0x07060302u);
-    }
-    return make_uint4(s[0], s[1], s[2], s[3]);
-  };
-  constexpr int kPer = QUANT ? 4 : 2;  // columns a dword
-
-  auto consume = [&](const TileRows<D, QUANT>& x, const Tile& t) __attribute__((always_inline)) {
-    floatx4 acc[NT][2];
-    floatx4 ek[2], ev[2];
-    if constexpr (QUANT) exps_sh[wave][lane] = exp_value(x.e);
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
+    for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
       for (int n = 0; n < NT; ++n) acc[n][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if constexpr (QUANT) {
+      uint4 k[2][D / 64];
+      read_k_codes<D>(k, stage, lane);
 #pragma unroll
-      for (int j = 0; j < TileRows<D, QUANT>::kK; ++j) {
-        const uint4 w = x.k[kt][j];
-        if constexpr (QUANT) {
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+          const uint4 w = k[kt][j];
           const bf16x8 k0 = as_bf16x8(decode8(make_uint2(w.x, w.y), 1.f)), k1 = as_bf16x8(decode8(make_uint2(w.z, w.w), 1.f));
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             acc[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[n][2 * j], acc[n][kt], 0, 0, 0);
             acc[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[n][2 * j + 1], acc[n][kt], 0, 0, 0);
           }
-        } else {
-#pragma unroll
-          for (int n = 0; n < NT; ++n) acc[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(w), q[n][j], acc[n][kt], 0, 0, 0);
         }
-      }
-    }
-    if constexpr (QUANT) {
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      const float* es = exps_sh[wave];
+    } else {
+      bf16x8 k[2][kKS];
+      read_k_operands16<D>(k, stage, lane);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        ek[i] = *reinterpret_cast<const floatx4*>(es + 16 * i + 4 * g);
-        ev[i] = *reinterpret_cast<const floatx4*>(es + 32 + 16 * i + 4 * g);
-      }
+      for (int j = 0; j < kKS; ++j)
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) acc[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kt][j], q[n][j], acc[n][kt], 0, 0, 0);
     }
-    bf16x8 hi[NT], lo[NT];
-    uint32_t seen[NT];
-    bool apart = false;  // rows of the unit that see different keys
+  };
+
+  // The running softmax.  P as two bf16 numbers, see above
+  auto softmax = [&](floatx4 (&acc)[NT][2], uint32_t mask, const floatx4 (&ek)[2], const floatx4 (&ev)[2], bf16x8 (&hi)[NT], bf16x8 (&lo)[NT],
+                     uint32_t (&seen)[NT]) __attribute__((always_inline)) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       if constexpr (QUANT) {
         acc[n][0] *= ek[0];
         acc[n][1] *= ek[1];
       }
-      seen[n] = x.mask;
-      if (p.causal) {
-        seen[n] &= low_mask(limit[n] - t.t * kTile);
-        apart |= seen[n] != x.mask;
-      }
+      seen[n] = mask;
+      if constexpr (CAUSAL) seen[n] &= low_mask(limit[n] - t * kTile);
       float ps[8];
       const float alpha = softmax_step(acc[n], seen[n], g, p.scale_log2, m_run[n], l_run[n], ps);
       if (__ballot(alpha != 1.f) != 0ull) {
 #pragma unroll
         for (int ct = 0; ct < kCT; ++ct) o[n][ct] *= alpha;
       }
-      float rest[8];
+      if constexpr (QUANT) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (QUANT) ps[e] *= ev[e >> 2][e & 3];
+        for (int e = 0; e < 8; ++e) ps[e] *= ev[e >> 2][e & 3];
       }
       hi[n] = pack_bf16x8(ps);
       const uint4 w = __builtin_bit_cast(uint4, hi[n]);
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+      const uint32_t h[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) rest[e] = ps[e] - ((e & 1) ? bf16_hi(u[e >> 1]) : bf16_lo(u[e >> 1]));
-      lo[n] = pack_bf16x8(rest);
+      for (int e = 0; e < 8; ++e) ps[e] -= (e & 1) ? bf16_hi(h[e >> 1]) : bf16_lo(h[e >> 1]);
+      lo[n] = pack_bf16x8(ps);
     }
-    // A key that some rows of the unit may not see has probability zero there, and zero times an infinity or a NaN of its V would still reach
-    // them.  Where that can be, the products are those of the finite values, and what infinities and NaN do to the rows that see them is added.
-    bool beyond = false;
-    if (p.causal && __ballot(apart) != 0ull) {
-      bool any = false;
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-#pragma unroll
-        for (int w = 0; w < kV; ++w) {
-          const uint32_t y = x.v[e][w];
-          if constexpr (QUANT)
-            any |= ((~y & 0x7fu) == 0u) | ((~y & 0x7f00u) == 0u) | ((~y & 0x7f0000u) == 0u) | ((~y & 0x7f000000u) == 0u);
-          else
-            any |= ((~y & 0x7f80u) == 0u) | ((~y & 0x7f800000u) == 0u);
-        }
-      beyond = __ballot(any) != 0ull;
-    }
-    if (!beyond) {
-#pragma unroll
-      for (int w = 0; w < kV; ++w)
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const bf16x8 v = as_bf16x8(v_operand(x.v, w, i));
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            o[n][kPer * w + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, hi[n], o[n][kPer * w + i], 0, 0, 0);
-            o[n][kPer * w + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, lo[n], o[n][kPer * w + i], 0, 0, 0);
-          }
-        }
-    } else {
-      bf16x8 sees[NT];  // one where the row may attend to the key
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        uint32_t u[4];
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          const uint32_t two = seen[n] >> (16 * (m >> 1) + 4 * g + 2 * (m & 1));
-          u[m] = ((two & 1u) ? 0x3f80u : 0u) | ((two & 2u) ? 0x3f800000u : 0u);
-        }
-        sees[n] = as_bf16x8(make_uint4(u[0], u[1], u[2], u[3]));
-      }
-#pragma unroll
-      for (int w = 0; w < kV; ++w)
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const uint4 v = v_operand(x.v, w, i);
-          const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-          uint32_t finite[4], above[4], below[4];  // the value or 0; one where it is +inf or NaN; one where it is -inf or NaN
-#pragma unroll
-          for (int m = 0; m < 4; ++m) {
-            finite[m] = above[m] = below[m] = 0u;
-#pragma unroll
-            for (int half = 0; half < 32; half += 16) {
-              const uint32_t y = (u[m] >> half) & 0xffffu, size = y & 0x7fffu;
-              finite[m] |= size < 0x7f80u ? y << half : 0u;
-              above[m] |= size > 0x7f80u || y == 0x7f80u ? 0x3f80u << half : 0u;
-              below[m] |= size > 0x7f80u || y == 0xff80u ? 0x3f80u << half : 0u;
-            }
-          }
-          const bf16x8 f = as_bf16x8(make_uint4(finite[0], finite[1], finite[2], finite[3]));
-          const bf16x8 up = as_bf16x8(make_uint4(above[0], above[1], above[2], above[3]));
-          const bf16x8 down = as_bf16x8(make_uint4(below[0], below[1], below[2], below[3]));
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            floatx4& y = o[n][kPer * w + i];
-            y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, hi[n], y, 0, 0, 0);
-            y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, lo[n], y, 0, 0, 0);
-            const floatx4 none = {0.f, 0.f, 0.f, 0.f};
-            const floatx4 more = __builtin_amdgcn_mfma_f32_16x16x32_bf16(up, sees[n], none, 0, 0, 0);
-            const floatx4 less = __builtin_amdgcn_mfma_f32_16x16x32_bf16(down, sees[n], none, 0, 0, 0);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] += (more[k] > 0.f ? INFINITY : 0.f) + (less[k] > 0.f ? -INFINITY : 0.f);
-          }
-        }
-    }
-    if constexpr (QUANT) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next tile's exponents follow these reads
   };
 
-  // `t`: the last tile of the piece, which began with tile `start` of the unit.  Lane (c, g) has the columns (4 g + i) * D / 16 + ct of row c.
-  auto end_piece = [&](const Tile& t, int start) __attribute__((always_inline)) {
-    const bool whole = start == 0 && t.t == t.q.tiles - 1;
+  auto read_v = [&](bf16x8 (&v)[kCT], const char* stage) __attribute__((always_inline)) {
+    if constexpr (QUANT) {
+      uint32_t codes[8][D / 64];
+      read_v_codes<D>(codes, stage, lane);
+#pragma unroll
+      for (int ct = 0; ct < kCT; ++ct) {  // the codes of two rows next to each other, widened in pairs
+        uint32_t s[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          s[m] = decode2(__builtin_amdgcn_perm(codes[2 * m + 1][ct >> 2], codes[2 * m][ct >> 2], (ct & 2) == 0 ? 0x05010400u : 0x07030602u), ct & 1, 1.f);
+        v[ct] = as_bf16x8(make_uint4(s[0], s[1], s[2], s[3]));
+      }
+    } else {
+      read_v_operands16<D>(v, stage, lane);
+    }
+  };
+  auto multiply_v = [&](char* stage, uint32_t mask, const bf16x8 (&hi)[NT], const bf16x8 (&lo)[NT], const uint32_t (&seen)[NT]) __attribute__((always_inline)) {
+    // A key that some rows of the unit may not see has probability zero there, and zero times an infinity or a NaN of its V would still reach
+    // them.  Where a tile holds such values its stage is rewritten, with ones for those that lead up, then down, whose products with ones for the
+    // keys that a row sees say where an infinity or a NaN has to come, and at last with zeros in their place.
+    bool apart = false;
+    if constexpr (CAUSAL) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) apart |= seen[n] != mask;
+    }
+    if (CAUSAL && __ballot(apart) != 0ull) {
+      bool any = false;
+#pragma unroll 1
+      for (int i = 0; i < G::kLoads; ++i) {
+        const uint4 w = read_chunk(stage + i * 1024 + lane * 16);
+        any |= beyond_finite<QUANT>(w.x) | beyond_finite<QUANT>(w.y) | beyond_finite<QUANT>(w.z) | beyond_finite<QUANT>(w.w);
+      }
+      if (__ballot(any) != 0ull) {
+        Window win{-1, 0, 0};
+        const TilePlace here = locate(p, u, t, win, lane);
+#pragma unroll 1
+        for (int which = 2; which >= 0; --which) {
+          request_rows<D, QUANT>(p.V + (int64_t)head_of(u) * p.vsh, p.vsp, p.vsn, here, stage, lane);
+          wait_loads();
+#pragma unroll 1
+          for (int i = 0; i < 4 * G::kLoads; ++i) rewrite_word<QUANT>(stage + i * 256 + lane * 4, which);
+          if (which == 0) break;
+          bf16x8 v[kCT];
+          read_v(v, stage);
+          const float add = which == 1 ? INFINITY : -INFINITY;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            uint32_t y[4];  // one for the keys that the row sees
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+              const uint32_t two = seen[n] >> (16 * (m >> 1) + 4 * g + 2 * (m & 1));
+              y[m] = (two & 1u) * 0x3f80u | ((two >> 1) & 1u) * 0x3f800000u;
+            }
+            const bf16x8 sees = as_bf16x8(make_uint4(y[0], y[1], y[2], y[3]));
+#pragma unroll
+            for (int ct = 0; ct < kCT; ++ct) {
+              const floatx4 found = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[ct], sees, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[n][ct][i] += found[i] > 0.f ? add : 0.f;
+            }
+          }
+        }
+      }
+    }
+    bf16x8 v[kCT];
+    read_v(v, stage);
+#pragma unroll
+    for (int ct = 0; ct < kCT; ++ct)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        o[n][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[ct], hi[n], o[n][ct], 0, 0, 0);
+        o[n][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[ct], lo[n], o[n][ct], 0, 0, 0);
+      }
+  };
+
+  // Writes out what the wavefront has of unit u.  Lane (c, g) has of row c the columns 16 ct + 4 g + i of bf16 rows, (4 g + i) * D / 16 + ct of codes.
+  auto end_piece = [&](int start, int end) __attribute__((always_inline)) {
+    const bool whole = start == 0 && end == u.q.tiles;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const int at = (t.qg * NT + n) * 16 + c, i = at / p.group, head = t.h * p.group + at - i * p.group;
-      if (i >= t.q.n) continue;
-      if (whole) {
-        const float inv = l_run[n] == 0.f ? 0.f : 1.f / l_run[n];
-        uint16_t* dst = p.out + (int64_t)(t.q.first + i) * p.osn + (int64_t)head * p.osh;
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-          uint32_t w[kCT / 2];
-#pragma unroll
-          for (int ct = 0; ct < kCT; ct += 2) w[ct / 2] = cvt_pk_bf16(o[n][ct][m] * inv, o[n][ct + 1][m] * inv);
-          if constexpr (D == 128)
-            *reinterpret_cast<uint4*>(dst + (4 * g + m) * kCT) = make_uint4(w[0], w[1], w[2], w[3]);
-          else
-            *reinterpret_cast<uint2*>(dst + (4 * g + m) * kCT) = make_uint2(w[0], w[1]);
-        }
-        if (p.lse && g == 0)
-          p.lse[(int64_t)(t.q.first + i) * (p.H * p.group) + head] = l_run[n] == 0.f ? -INFINITY : (m_run[n] + __builtin_amdgcn_logf(l_run[n])) * kLn2;
-      } else {
-        const int64_t row = (int64_t)(2 * worker + (start == 0)) * p.unit_rows + 16 * n + c;
-        float* dst = p.part_o + row * D;
+      const int at = (u.qg * NT + n) * 16 + c, i = at / p.group, head = head_of(u) * p.group + at - i * p.group;
+      if (i >= u.q.n) continue;
+      const float inv = !whole ? 1.f : (l_run[n] == 0.f ? 0.f : 1.f / l_run[n]);
+      uint16_t* out = p.out + (int64_t)(u.q.first + i) * p.osn + (int64_t)head * p.osh;
+      const int64_t row = (int64_t)(2 * wave_id + (start == 0)) * p.unit_rows + 16 * n + c;
+      float* part = p.part_o + row * D;
+      auto put = [&](int column, const floatx4& x) __attribute__((always_inline)) {  // four columns
+        if (whole)
+          *reinterpret_cast<uint2*>(out + column) = make_uint2(cvt_pk_bf16(x[0] * inv, x[1] * inv), cvt_pk_bf16(x[2] * inv, x[3] * inv));
+        else
+          *reinterpret_cast<floatx4*>(part + column) = x;
+      };
+      if constexpr (QUANT) {
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
-          for (int v = 0; v < kVec; ++v)
-            *reinterpret_cast<floatx4*>(dst + (4 * g + m) * kCT + 4 * v) = floatx4{o[n][4 * v][m], o[n][4 * v + 1][m], o[n][4 * v + 2][m], o[n][4 * v + 3][m]};
-        if (g == 0) p.part_ml[row] = make_float2(m_run[n], l_run[n]);
+          for (int ct = 0; ct < kCT; ct += 4) put((4 * g + m) * kCT + ct, floatx4{o[n][ct][m], o[n][ct + 1][m], o[n][ct + 2][m], o[n][ct + 3][m]});
+      } else {
+#pragma unroll
+        for (int ct = 0; ct < kCT; ++ct) put(16 * ct + 4 * g, o[n][ct]);
+      }
+      if (g == 0) {
+        if (!whole)
+          p.part_ml[row] = make_float2(m_run[n], l_run[n]);
+        else if (p.lse)
+          p.lse[(int64_t)(u.q.first + i) * (p.H * p.group) + head] = l_run[n] == 0.f ? -INFINITY : (m_run[n] + __builtin_amdgcn_logf(l_run[n])) * kLn2;
       }
     }
   };
 
-  int start = 0, entry = load_entry(p, here, lane);
+  // A stage's K is requested again as soon as it is in registers, its V likewise.  Loads return in order: a wait leaves those under way that were
+  // requested behind what is waited for.  Where no more are requested it leaves none.
+  int start = t;
 #pragma unroll 1
-  for (int i = 0; i < n_tiles; ++i) {
-    if (here.first) {
-      start = here.t;
-      begin_unit(here);
-    }
-    TileRows<D, QUANT> x;
-    load_tile_rows<D, QUANT>(x, p, here, entry, lane);
-    Tile next = here;
-    if (i + 1 < n_tiles) {
-      next = advance(here, i + 1);
-      entry = load_entry(p, next, lane);  // travels with the rows
+  for (int i = -kDepth; i < n_tiles; ++i) {
+    const bool more = asked < n_tiles, work = i >= 0;
+    char* stage = stage_of(i);
+    uint32_t mask = 0u;
+    floatx4 acc[NT][2], ek[2], ev[2];
+    if (work) {
+      mask = (uint32_t)__builtin_amdgcn_readlane(masks, i & (kDepth - 1));
+      if (t == start) begin_unit();
+      if (i + kDepth <= n_tiles)
+        wait_loads_but<G::kLoads + (kDepth - 1) * G::kTileLoads>();
+      else
+        wait_loads();
+      if (mask != 0u) {
+        multiply_k(acc, stage);
+        if constexpr (QUANT) read_exponents(ek, ev, stage + 2 * G::kRows, lane);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
-    if (x.mask != 0u) consume(x, here);
-    if (here.last) end_piece(here, start);
-    here = next;
+    if (more) request_k();
+    __builtin_amdgcn_sched_barrier(0);
+    if (work) {
+      bf16x8 hi[NT], lo[NT];
+      uint32_t seen[NT];
+      if (mask != 0u) softmax(acc, mask, ek, ev, hi, lo, seen);
+      if (more)
+        wait_loads_but<(kDepth - 1) * G::kTileLoads + G::kTileLoads - G::kLoads>();
+      else
+        wait_loads();
+      if (mask != 0u) multiply_v(stage + G::kRows, mask, hi, lo, seen);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) request_v();
+    if (work) {
+      ++t;
+      if (t >= u.q.tiles || i == n_tiles - 1) {
+        end_piece(start, t);
+        start = t = 0;
+        if (i < n_tiles - 1) next_unit(u);
+      }
+    }
   }
 }
 
@@ -524,7 +670,7 @@ __global__ __launch_bounds__(256, groups_per_cu(D, NT)) void paged_attn_kernel(c
 // tiles follows from s alone, and with it where the pieces lie.
 template <int D, int NT, int NW>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
-  constexpr int kVec = D / 64, kAhead = 8;
+  constexpr int kVec = D / 64, kAhead = 20;
   __shared__ float2 ml_sh[NW];
   __shared__ float o_sh[NW][D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -538,55 +684,53 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
   const Request q = load_request<NT>(p, r);
   if (i >= q.n) return;
   const int h = head / p.group, unit_row = i * p.group + head - h * p.group, qg = unit_row / (16 * NT), in_unit = unit_row - qg * 16 * NT;
-  const Shares shares((int64_t)prefix.total * p.H, p.workers);
-  const int64_t s = (int64_t)prefix.before(p, r, lane) * p.H + ((int64_t)h * q.groups + qg) * q.tiles;
-  const int w0 = shares.of(s), w1 = shares.of(s + q.tiles - 1);
+  const int bundles = p.H >> p.log_bundle, bundle = h >> p.log_bundle, in_bundle = h - (bundle << p.log_bundle);
+  const Shares shares((int64_t)prefix.total * bundles, p.workers);
+  const int64_t s = (int64_t)prefix.before(p, r, lane) * bundles + ((int64_t)bundle * q.groups + qg) * q.tiles;
+  const int w0 = (int)same(shares.of(s)), w1 = (int)same(shares.of(s + q.tiles - 1));
   if (w0 == w1) return;
   const int n = w1 - w0 + 1;  // (some of them may have no tile)
+  // Wavefront w takes the pieces w, w + NW, ..., kAhead of them at a time: their statistics, lane by lane, and their rows, all requested at once.
   float m_run = -INFINITY, l_run = 0.f, o[kVec];
 #pragma unroll
   for (int v = 0; v < kVec; ++v) o[v] = 0.f;
-  for (int j0 = NW == 1 ? 0 : wave * kWave; j0 < n; j0 += NW * kWave) {
-    const int j = j0 + lane, w = w0 + j;
-    float2 ml = make_float2(-INFINITY, 0.f);
-    const int64_t row = (int64_t)(2 * w + (j == 0)) * p.unit_rows + in_unit;
-    if (j < n && shares.begin(w) < shares.begin(w + 1)) ml = p.part_ml[row];
+  const int mine = NW == 1 ? n : (n - wave + NW - 1) / NW, first = NW == 1 ? 0 : wave;
+#pragma unroll 1
+  for (int k0 = 0; k0 < mine; k0 += kAhead) {
+    auto slot_row = [&](int j) __attribute__((always_inline)) { return (int64_t)(2 * (((w0 + j) << p.log_bundle) + in_bundle) + (j == 0)) * p.unit_rows + in_unit; };
+    const int j = first + (k0 + min(lane, kAhead - 1)) * NW;
+    const int j_there = min(j, n - 1);
+    float2 ml = p.part_ml[slot_row(j_there)];
+    float y[kAhead][kVec];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const float* src = p.part_o + slot_row(min(first + (k0 + k) * NW, n - 1)) * D + lane * kVec;
+      if constexpr (kVec == 2) {
+        const float2 x = *reinterpret_cast<const float2*>(src);
+        y[k][0] = x.x;
+        y[k][1] = x.y;
+      } else {
+        y[k][0] = *src;
+      }
+    }
+    // (nothing was written for a wavefront without a tile)
+    if (j >= n || lane >= kAhead || shares.begin(w0 + j_there) == shares.begin(w0 + j_there + 1)) ml = make_float2(-INFINITY, 0.f);
     float top = ml.x;
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k, kWave));
     const float m_new = fmaxf(m_run, top), m_use = m_new == -INFINITY ? 0.f : m_new;
     const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - m_use), old = __builtin_amdgcn_exp2f(m_run - m_use);
     l_run = l_run * old + wave_sum(f * ml.y);
-#pragma unroll
-    for (int v = 0; v < kVec; ++v) o[v] *= old;
     m_run = m_new;
     const unsigned long long some = __ballot(ml.y != 0.f);
-    const int n_here = min(n - j0, kWave);
-    for (int k0 = 0; k0 < n_here; k0 += kAhead) {
-      float y[kAhead][kVec];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
+    for (int v = 0; v < kVec; ++v) o[v] *= old;
 #pragma unroll
-        for (int v = 0; v < kVec; ++v) y[k][v] = 0.f;
-        if (k0 + k < n_here && ((some >> (k0 + k)) & 1ull)) {
-          const float* src = p.part_o + ((int64_t)(2 * (w0 + j0 + k0 + k) + (j0 + k0 + k == 0)) * p.unit_rows + in_unit) * D + lane * kVec;
-          if constexpr (kVec == 2) {
-            const float2 t = *reinterpret_cast<const float2*>(src);
-            y[k][0] = t.x;
-            y[k][1] = t.y;
-          } else {
-            y[k][0] = *src;
-          }
-        }
-      }
+    for (int k = 0; k < kAhead; ++k) {
+      const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), k));
+      const bool take = ((some >> k) & 1ull) != 0ull;
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, f), (k0 + k) & 63));
-        if (k0 + k < n_here && ((some >> (k0 + k)) & 1ull)) {
-#pragma unroll
-          for (int v = 0; v < kVec; ++v) o[v] += w * y[k][v];
-        }
-      }
+      for (int v = 0; v < kVec; ++v) o[v] = take ? __builtin_fmaf(w, y[k][v], o[v]) : o[v];
     }
   }
   if constexpr (NW > 1) {
@@ -621,17 +765,20 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
   if (p.lse && lane == 0) p.lse[(int64_t)(q.first + i) * Hq + head] = l_run == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_run)) * kLn2;
 }
 
-// Wavefronts: as many as are resident at once, and no more than the batch may have tiles.
-constexpr int kPagedGroups = 256;  // compute units
+// Wavefronts: a workgroup's rings take most of a compute unit's LDS.  No more than the batch may have tiles.
+constexpr int kPagedGroups = 512;
 PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch& b, int page) {
   PagedPlan p;
   const int64_t rows = (int64_t)b.max_rows * group;
   p.q_tiles = rows <= 16 ? 1 : 2;
   p.unit_rows = (int)std::min<int64_t>(rows, 16 * p.q_tiles);
   const int64_t tiles = ceil_div64((int64_t)b.table_width * page, kTile), units = ceil_div64(rows, 16 * p.q_tiles) * n_heads;
-  const int64_t most = tiles * units >= (int64_t(1) << 31) ? int64_t(1) << 31 : tiles * units * b.n_req;
-  p.workers = (int)std::min<int64_t>((int64_t)kPagedGroups * kWavesPerGroup * groups_per_cu(head_dim, p.q_tiles), ceil_div64(most, kWavesPerGroup) * kWavesPerGroup);
-  const size_t slots = (size_t)2 * p.workers;
+  p.log_bundle = (n_heads & 3) == 0 ? 2 : ((n_heads & 1) == 0 ? 1 : 0);
+  const int per_group = kWavesPerGroup >> p.log_bundle;  // wavefronts that take different tiles
+  const int64_t bundled = (tiles * units >= (int64_t(1) << 31) ? int64_t(1) << 31 : tiles * units * b.n_req) >> p.log_bundle;
+  p.groups = (int)std::min<int64_t>(kPagedGroups, ceil_div64(bundled, per_group));
+  p.workers = p.groups * per_group;
+  const size_t slots = (size_t)2 * p.groups * kWavesPerGroup;
   p.part_ml = (slots * p.unit_rows * head_dim * sizeof(float) + 255) & ~(size_t)255;
   p.total = p.part_ml + slots * p.unit_rows * sizeof(float2);
   return p;
@@ -641,11 +788,12 @@ PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch
 constexpr int kJoinGroups = 1024;
 template <int D, int NT>
 static hipError_t launch_paged_t(const PagedAttn& a, const PagedPlan& p, hipStream_t st) {
-  const int groups = p.workers / kWavesPerGroup;
+  const bool causal = a.causal && (a.b.max_rows > 1 || a.b.positions != nullptr);  // (the last row sees every key)
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.groups), dim3(256), 0, st, a); };
   if (a.k_exp != nullptr)
-    hipLaunchKernelGGL((paged_attn_kernel<D, true, NT>), dim3(groups), dim3(256), 0, st, a);
+    causal ? launch(paged_attn_kernel<D, true, true, NT>) : launch(paged_attn_kernel<D, true, false, NT>);
   else
-    hipLaunchKernelGGL((paged_attn_kernel<D, false, NT>), dim3(groups), dim3(256), 0, st, a);
+    causal ? launch(paged_attn_kernel<D, false, true, NT>) : launch(paged_attn_kernel<D, false, false, NT>);
   if ((int64_t)a.b.table_width * a.page <= kTile) return hipGetLastError();  // no unit has two tiles
   const int64_t rows = (int64_t)a.b.n_req * a.b.max_rows * a.H * a.group;
   if (rows <= kJoinGroups)
@@ -654,9 +802,12 @@ static hipError_t launch_paged_t(const PagedAttn& a, const PagedPlan& p, hipStre
     hipLaunchKernelGGL((paged_join_kernel<D, NT, 1>), grid_list(ceil_div64(rows, 4)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
+template <int D>
+static hipError_t launch_paged_d(const PagedAttn& a, const PagedPlan& p, hipStream_t st) {
+  return p.q_tiles == 1 ? launch_paged_t<D, 1>(a, p, st) : launch_paged_t<D, 2>(a, p, st);
+}
 hipError_t launch_paged_attn(const PagedAttn& a, const PagedPlan& p, int head_dim, hipStream_t st) {
-  if (head_dim == 128) return p.q_tiles == 1 ? launch_paged_t<128, 1>(a, p, st) : launch_paged_t<128, 2>(a, p, st);
-  return p.q_tiles == 1 ? launch_paged_t<64, 1>(a, p, st) : launch_paged_t<64, 2>(a, p, st);
+  return head_dim == 128 ? launch_paged_d<128>(a, p, st) : launch_paged_d<64>(a, p, st);
 }
 
 }  // namespace focus
