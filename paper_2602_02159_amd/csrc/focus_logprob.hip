@@ -37,6 +37,29 @@ struct LogprobArgs {
   int vocab, n_parts, top_n;
 };
 
+// one logit of a row
+template <class T>
+__device__ __forceinline__ float logit(const T* row, int id) {
+  return tame(sizeof(T) == 4 ? *reinterpret_cast<const float*>(row + id) : bf16_lo(*reinterpret_cast<const uint16_t*>(row + id)));
+}
+
+// over the wavefront, in a fixed order; every lane receives the result
+__device__ __forceinline__ float wave_sum_fast(float x) { return group_sum(row_sum16(x)); }
+__device__ __forceinline__ float wave_max_fast(float x) {
+  x = fmaxf(x, lane_dpp<0xB1>(x));
+  x = fmaxf(x, lane_dpp<0x4E>(x));
+  x = fmaxf(x, lane_dpp<0x141>(x));
+  x = fmaxf(x, lane_dpp<0x140>(x));
+  return group_max(x);
+}
+// over the workgroup of four wavefronts; `sh` of four entries
+__device__ __forceinline__ float block_max4(float x, float* sh) {
+  x = wave_max_fast(x);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
+}
+
 struct TopShared256 {
   uint32_t best[256];
   uint2 list[kTopCandidates];
@@ -44,49 +67,46 @@ struct TopShared256 {
   unsigned long long wave_best[4];
 };
 
-// The top_n first, in order, of what 256 threads hold, N entries each: key_at(i) (0: none) and id_at(i), `best` = the largest key of the
-// thread.  emit(rank, key, id) is called once for each of them.  The top_n-th largest of the threads' best, to sixteen bits, is a bound that at least top_n
-// entries reach; those that do are listed and rank themselves by comparison.  Where too many do (equal logits), one is found after
-// the other.  Every thread of the workgroup has to call it.
-// `UNROLL` turns at once: all of them where the entries are registers.
-template <int N, int UNROLL, class Key, class Id, class Emit>
-__device__ __forceinline__ void block_top(TopShared256& sm, uint32_t best, int top_n, const Key key_at, const Id id_at, const Emit emit) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// The largest number, to sixteen bits, that at least top_n of the threads' best reach (1 where fewer have one)
+__device__ __forceinline__ uint32_t top_threshold(TopShared256& sm, uint32_t best, int top_n) {
+  const int tid = threadIdx.x, lane = tid & 63;
   sm.best[tid] = best;
   if (tid == 0) sm.count = 0u;
   __syncthreads();
-  if (wave == 0) {
+  if (tid < kWave) {
     uint32_t k[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) k[u] = sm.best[u * kWave + lane] >> 16;
     uint32_t t = 0u;
+#pragma unroll 1
     for (int bit = 15; bit >= 0; --bit) {
       const uint32_t with = t | (1u << bit);
       int n = 0;
 #pragma unroll
       for (int u = 0; u < 4; ++u) n += __popcll(__ballot(k[u] >= with));
-      if (n >= top_n) t = with;
+      t = n >= top_n ? with : t;
     }
     if (lane == 0) sm.threshold = max(t << 16, 1u);
   }
   __syncthreads();
-  const uint32_t threshold = sm.threshold;
-  if (best >= threshold) {
-#pragma unroll UNROLL
-    for (int i = 0; i < N; ++i) {
-      const uint32_t key = key_at(i);
-      if (key >= threshold) {
-        const uint32_t at = atomicAdd(&sm.count, 1u);  // (the list's order does not matter)
-        if (at < (uint32_t)kTopCandidates) sm.list[at] = make_uint2(key, (uint32_t)id_at(i));
-      }
-    }
-  }
+  return sm.threshold;
+}
+__device__ __forceinline__ void list_candidate(TopShared256& sm, uint32_t key, int id) {
+  const uint32_t at = atomicAdd(&sm.count, 1u);  // (the list's order does not matter)
+  if (at < (uint32_t)kTopCandidates) sm.list[at] = make_uint2(key, (uint32_t)id);
+}
+// The top_n first of the listed candidates, in order, found by comparing each with all; emit(rank, key, id) is called once for every rank.  Where more than
+// the list holds came (equal logits), one is found after the other among the n_each entries that every thread has: key_at(i) (0: none), id_at(i).
+template <class Key, class Id, class Emit>
+__device__ __forceinline__ void emit_top(TopShared256& sm, int top_n, int n_each, const Key key_at, const Id id_at, const Emit emit) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   __syncthreads();
   const int n = (int)sm.count;
   if (n <= kTopCandidates) {
     for (int i = tid; i < n; i += 256) {
       const uint2 mine = sm.list[i];
       int rank = 0;
+#pragma unroll 4
       for (int j = 0; j < n; ++j) {
         const uint2 other = sm.list[j];
         rank += other.x > mine.x || (other.x == mine.x && other.y < mine.y);
@@ -96,12 +116,12 @@ __device__ __forceinline__ void block_top(TopShared256& sm, uint32_t best, int t
     for (int i = n + tid; i < top_n; i += 256) emit(i, 0u, -1);
     return;
   }
-  // larger = earlier in the order; the lower id first
-  unsigned long long last = ~0ull;
+  unsigned long long last = ~0ull;  // larger = earlier in the order; the lower id first
+#pragma unroll 1
   for (int k = 0; k < top_n; ++k) {
     unsigned long long mine = 0ull;
-#pragma unroll UNROLL
-    for (int i = 0; i < N; ++i) {
+#pragma unroll 1
+    for (int i = 0; i < n_each; ++i) {
       const uint32_t key = key_at(i);
       const unsigned long long x = key == 0u ? 0ull : ((unsigned long long)key << 32) | (uint32_t)~id_at(i);
       if (x < last && x > mine) mine = x;
@@ -121,53 +141,46 @@ __device__ __forceinline__ void block_top(TopShared256& sm, uint32_t best, int t
   }
 }
 
-// max / sum over the workgroup of four wavefronts, in a fixed order; `sh` of four entries
-__device__ __forceinline__ float block_max4(float x, float* sh) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, kWave));
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
-  __syncthreads();
-  return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
-}
-
 constexpr float kLog2eF = 1.4426950408889634f, kLn2F = 0.6931471805599453f;
 constexpr float kNothing = -200.f;  // 2^-200 is zero: exponents below are taken as this one, so that no 0 times infinity comes up
 
 template <class T>
-__global__ __launch_bounds__(256) void logprob_part_kernel(const LogprobArgs p) {
+__global__ __launch_bounds__(256, 6) void logprob_part_kernel(const LogprobArgs p) {
   constexpr int E = 16 / sizeof(T), V = kLogitsThread / E;  // logits a load, loads
   __shared__ float max_sh[4];
   __shared__ float4 sum_sh[4];
   __shared__ TopShared256 top_sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.y, part = blockIdx.x;
-  if (p.masked && p.masked[row] == 0) return;
   const T* z_row = static_cast<const T*>(p.logits) + (int64_t)row * p.row_stride;
   const int first = part * kLogitsPart + tid * E;
   auto id_at = [&](int i) __attribute__((always_inline)) { return first + (i / E) * (256 * E) + i % E; };
   float z[kLogitsThread];
-  uint4 w[V];
+  {
+    uint4 w[V];
+    const int whole = p.vocab / E * E - E;  // the last id from which sixteen bytes can be read, if any
+    if (whole >= 0) {
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-    const int id = first + k * 256 * E;
-    if (id + E <= p.vocab) w[k] = *reinterpret_cast<const uint4*>(z_row + id);
-  }
+      for (int k = 0; k < V; ++k) w[k] = *reinterpret_cast<const uint4*>(z_row + min(first + k * 256 * E, whole));
+    }
+    if (p.masked && p.masked[row] == 0) return;  // whole workgroup
 #pragma unroll
-  for (int k = 0; k < V; ++k) {
-    const int id = first + k * 256 * E;
-    if (id + E <= p.vocab) {
+    for (int k = 0; k < V; ++k) {
       const uint32_t u[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        z[k * E + e] = tame(sizeof(T) == 4 ? __uint_as_float(u[e & 3]) : ((e & 1) ? bf16_hi(u[(e >> 1) & 3]) : bf16_lo(u[(e >> 1) & 3])));
-    } else {  // a row's last, shorter piece, logit by logit
+      const bool in = first + k * 256 * E <= whole;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        z[k * E + e] = -INFINITY;
-        if (id + e < p.vocab) {
-          if constexpr (sizeof(T) == 4)
-            z[k * E + e] = tame(*reinterpret_cast<const float*>(z_row + id + e));
-          else
-            z[k * E + e] = tame(bf16_lo(*reinterpret_cast<const uint16_t*>(z_row + id + e)));
+        const float x = sizeof(T) == 4 ? __uint_as_float(u[e & 3]) : ((e & 1) ? bf16_hi(u[(e >> 1) & 3]) : bf16_lo(u[(e >> 1) & 3]));
+        z[k * E + e] = in ? tame(x) : -INFINITY;
+      }
+    }
+    if (part == (int)gridDim.x - 1) {  // a row's last, shorter piece, logit by logit
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const int id = first + k * 256 * E;
+        if (id > whole && id < p.vocab) {
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (id + e < p.vocab) z[k * E + e] = logit(z_row, id + e);
         }
       }
     }
@@ -177,29 +190,41 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(const LogprobArgs p) 
   for (int i = 0; i < kLogitsThread; ++i) mine = fmaxf(mine, z[i]);
   const float m = block_max4(mine, max_sh), m_use = m == -INFINITY ? 0.f : m;
 
-  float rest = 0.f, A = 0.f, equal = 0.f;  // of the logits below m; how many equal it
-  auto add = [&](auto careful) __attribute__((always_inline)) {
+  float rest = 0.f, A = 0.f;  // of the logits below m;
+  int equal = 0;              // how many equal it
 #pragma unroll
-    for (int i = 0; i < kLogitsThread; ++i) {
-      const float y = fmaxf((z[i] - m_use) * kLog2eF, kNothing), e = __builtin_amdgcn_exp2f(y);
-      A = __builtin_fmaf(e, y, A);
-      if constexpr (decltype(careful)::value) {
-        rest += z[i] == m ? 0.f : e;
-        equal += z[i] == m ? 1.f : 0.f;
-      } else {
-        rest += e;
+  for (int i = 0; i < kLogitsThread; ++i) {
+    const float y = fmaxf((z[i] - m_use) * kLog2eF, kNothing), e = __builtin_amdgcn_exp2f(y);
+    A = __builtin_fmaf(e, y, A);
+    const bool top = z[i] == m;
+    rest += top ? 0.f : e;
+    equal += top ? 1 : 0;
+  }
+  rest = wave_sum_fast(rest);
+  A = wave_sum_fast(A);
+  const float n_equal = wave_sum_fast((float)equal);
+  if (lane == 0) sum_sh[wave] = make_float4(rest, A, n_equal, 0.f);
+  if (p.top_n > 0) {
+    const uint32_t best = top_key(mine), threshold = top_threshold(top_sh, best, p.top_n);
+    uint32_t some = 0u;
+    if (__ballot(best >= threshold) != 0ull) {  // few wavefronts
+      const float least = threshold < 0x00800000u ? -3.4028234663852886e38f : order_value(threshold);  // (0x00800000: the lowest number's key)
+#pragma unroll
+      for (int i = 0; i < kLogitsThread; ++i) some |= z[i] >= least && z[i] > -INFINITY ? 1u << i : 0u;
+      if (best < threshold) some = 0u;
+      while (some != 0u) {  // one or two, which come from the cache
+        const int id = id_at(__builtin_ctz(some));
+        some &= some - 1u;
+        list_candidate(top_sh, top_key(logit(z_row, id)), id);
       }
     }
-  };
-  if (__ballot(mine == m) != 0ull)
-    add(std::true_type{});
-  else
-    add(std::false_type{});
-  rest = wave_sum(rest);
-  A = wave_sum(A);
-  equal = wave_sum(equal);
-  if (lane == 0) sum_sh[wave] = make_float4(rest, A, equal, 0.f);
-  __syncthreads();
+    uint2* list = p.part_top + ((int64_t)row * p.n_parts + part) * p.top_n;
+    emit_top(
+        top_sh, p.top_n, kLogitsThread, [&](int i) { return id_at(i) < p.vocab ? top_key(logit(z_row, id_at(i))) : 0u; }, id_at,
+        [&](int rank, uint32_t key, int id) { list[rank] = make_uint2(key, (uint32_t)id); });
+  } else {
+    __syncthreads();
+  }
   if (tid == 0) {
     float r = 0.f, a = 0.f, n = 0.f;
 #pragma unroll
@@ -210,17 +235,10 @@ __global__ __launch_bounds__(256) void logprob_part_kernel(const LogprobArgs p) 
     }
     p.part[(int64_t)row * p.n_parts + part] = m == -INFINITY ? make_float4(-INFINITY, 0.f, 0.f, 0.f) : make_float4(m, r + (n - 1.f), a, 0.f);
   }
-  if (p.top_n > 0) {
-    uint2* list = p.part_top + ((int64_t)row * p.n_parts + part) * p.top_n;
-    block_top<kLogitsThread, kLogitsThread>(
-        top_sh, top_key(mine), p.top_n,
-        [&](int i) __attribute__((always_inline)) { return top_key(z[i]); }, id_at, [&](int rank, uint32_t key, int id) { list[rank] = make_uint2(key, (uint32_t)id); });
-  }
 }
 
 template <class T>
 __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) {
-  constexpr int kEach = 32;  // entries of the parts' lists a thread
   __shared__ float max_sh[4];
   __shared__ float2 sum_sh[4];
   __shared__ TopShared256 top_sh;
@@ -231,11 +249,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
   if (p.targets && live) {
     target = p.targets[row];
     if (target >= 0 && target < p.vocab) {
-      const T* z = static_cast<const T*>(p.logits) + (int64_t)row * p.row_stride + target;
-      if constexpr (sizeof(T) == 4)
-        z_t = tame(*reinterpret_cast<const float*>(z));
-      else
-        z_t = tame(bf16_lo(*reinterpret_cast<const uint16_t*>(z)));
+      z_t = logit(static_cast<const T*>(p.logits) + (int64_t)row * p.row_stride, target);
     }
   }
   if (!live) {  // whole workgroup
@@ -251,6 +265,11 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
   }
   float4 s = make_float4(-INFINITY, 0.f, 0.f, 0.f);  // at most 256 parts: one a thread
   if (tid < p.n_parts) s = p.part[(int64_t)row * p.n_parts + tid];
+  const uint2* list = p.part_top + (int64_t)row * p.n_parts * p.top_n;
+  const int n = p.n_parts * p.top_n;  // at most 256 * 32
+  uint2 mine[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) mine[i] = tid + 256 * i < n ? list[tid + 256 * i] : make_uint2(0u, 0u);
   const float m = block_max4(s.x, max_sh), m_use = m == -INFINITY ? 0.f : m;
   // Of the parts whose largest logit is the row's the first one's is left out of r
   const unsigned long long top = __ballot(s.x == m && m != -INFINITY);
@@ -260,7 +279,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
   const bool first = before == 0 && top != 0ull && lane == __builtin_ctzll(top | (1ull << 63));
   const float d = fmaxf((s.x - m_use) * kLog2eF, kNothing), f = __builtin_amdgcn_exp2f(d);
   const float whole = s.x == -INFINITY ? 0.f : 1.f + s.y;
-  const float r_mine = wave_sum(first ? s.y : f * whole), a_mine = wave_sum(f * (s.z + whole * d));
+  const float r_mine = wave_sum_fast(first ? s.y : f * whole), a_mine = wave_sum_fast(f * (s.z + whole * d));
   if (lane == 0) sum_sh[wave] = make_float2(r_mine, a_mine);
   __syncthreads();
   float r = 0.f, a = 0.f;
@@ -275,12 +294,19 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
     if (p.entropy) p.entropy[row] = m == -INFINITY ? 0.f : log_sum - kLn2F * a / (1.f + r);
   }
   if (p.top_n == 0) return;
-  const uint2* list = p.part_top + (int64_t)row * p.n_parts * p.top_n;
-  const int n = p.n_parts * p.top_n;  // <= 256 * kEach
-  uint32_t best = 0u;
-  for (int i = tid; i < n; i += 256) best = max(best, list[i].x);
-  block_top<kEach, 4>(
-      top_sh, best, p.top_n, [&](int i) { return tid + 256 * i < n ? list[tid + 256 * i].x : 0u; }, [&](int i) { return (int)list[tid + 256 * i].y; },
+  // (the first two entries of a thread are here since before the statistics)
+  const int n_each = (n + 255) / 256;
+  uint32_t best = max(mine[0].x, mine[1].x);
+  for (int i = tid + 512; i < n; i += 256) best = max(best, list[i].x);
+  const uint32_t threshold = top_threshold(top_sh, best, p.top_n);
+  if (best >= threshold) {
+    for (int i = 0; i < n_each; ++i) {
+      const uint2 x = i < 2 ? mine[i] : (tid + 256 * i < n ? list[tid + 256 * i] : make_uint2(0u, 0u));
+      if (x.x >= threshold) list_candidate(top_sh, x.x, (int)x.y);
+    }
+  }
+  emit_top(
+      top_sh, p.top_n, n_each, [&](int i) { return tid + 256 * i < n ? list[tid + 256 * i].x : 0u; }, [&](int i) { return (int)list[tid + 256 * i].y; },
       [&](int rank, uint32_t key, int id) {
         p.top_ids[(int64_t)row * p.top_n + rank] = id;
         p.top_logprobs[(int64_t)row * p.top_n + rank] = id < 0 ? -INFINITY : (order_value(key) - m) - log_sum;
