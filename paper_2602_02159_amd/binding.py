@@ -52,11 +52,13 @@ class QuantCache(C.Structure):
 
 class Rotation(C.Structure):
     """Mirror of `focus_rotation`."""
+    device = None  # set by make_rotation; one that a caller filled in by hand is taken as it is, and so the next two
     _fields_ = [("freq", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_double)]
 
 
 class PagedCache(C.Structure):
     """Mirror of `focus_paged_cache`."""
+    device = None
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p),
                 ("k_stride_p", C.c_int64), ("k_stride_h", C.c_int64), ("k_stride_n", C.c_int64),
                 ("v_stride_p", C.c_int64), ("v_stride_h", C.c_int64), ("v_stride_n", C.c_int64),
@@ -66,6 +68,7 @@ class PagedCache(C.Structure):
 
 class PagedBatch(C.Structure):
     """Mirror of `focus_paged_batch`."""
+    device = None
     _fields_ = [("seq_len", C.c_void_p), ("page_table", C.c_void_p), ("row_start", C.c_void_p), ("positions", C.c_void_p),
                 ("table_stride", C.c_int64), ("table_width", C.c_int32), ("n_req", C.c_int32), ("max_rows", C.c_int32), ("n_rows", C.c_int32)]
 
@@ -637,56 +640,84 @@ def make_paged_batch(seq_len: torch.Tensor, page_table: torch.Tensor, row_start:
     return batch
 
 
-def _on_device(device: int, *descriptions) -> None:
-    for t, name in descriptions:
-        if t is not None and getattr(t, "device", device) != device:
-            raise ValueError(f"{name} on cuda:{t.device}, but the current device is cuda:{device}")
+# The checks of these calls: one condition where everything is as it should be (they are a few microseconds long), and functions that tell what is not.
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
 
 
-def _check_heads(device: int, rows: int, head_dim: int, *expected) -> None:
+def _current_device() -> int:
+    # the number without the initialisation that torch.cuda.current_device looks for: a CUDA tensor is there already
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:  # (not part of torch's interface)
+        return torch.cuda.current_device()
+
+
+def _explain_devices(device: int, *things) -> None:
+    for t, name in things:
+        there = device if t is None else t.get_device() if isinstance(t, torch.Tensor) else t.device
+        if there is not None and there != device:
+            raise ValueError(f"{name} on device {there}, but the current device is cuda:{device}")
+
+
+def _explain_heads(device: int, rows: int, head_dim: int, *expected) -> None:
     """bf16 [rows, heads, head_dim], innermost stride 1."""
     for t, name, heads in expected:
-        if t.dtype != torch.bfloat16 or t.get_device() != device:
+        if t.dtype != _BF16 or t.get_device() != device:
             raise TypeError(f"{name}: expected a tensor of torch.bfloat16 on cuda:{device}, got {t.dtype} on {t.device}")
         if t.shape != (rows, heads, head_dim) or t.stride(2) != 1:
             raise ValueError(f"{name}: expected {[rows, heads, head_dim]}, innermost stride 1, got {list(t.shape)}, strides {t.stride()}")
 
 
-def _hn(t: torch.Tensor):
+def _strides(shape, strides):
     """Strides of a head and of a row of [rows, heads, d] (those of a single one mean nothing)."""
-    n, h, _ = t.stride()
-    return (h if t.shape[1] > 1 else 0), (n if t.shape[0] > 1 else 0)
+    return (strides[1] if shape[1] > 1 else 0), (strides[0] if shape[0] > 1 else 0)
+
+
+def _fits(t, dtype, device: int, shape) -> bool:
+    return t is None or (t.dtype is dtype and t.get_device() == device and t.shape == shape and t.is_contiguous())
 
 
 def rotary(x, out, positions, pos_base: int, rotation: Rotation) -> None:
     """x, out bf16 [rows, heads, d] of any strides (a transposed view of head-major rows is one; out may be x); positions int32 [rows] or None."""
-    device = _device_of(x, "x")
-    if x.dim() != 3:
-        raise ValueError(f"x: expected [rows, heads, d], got {list(x.shape)}")
-    n, heads, d = x.shape
-    _check_heads(device, n, d, (x, "x", heads), (out, "out", heads))
-    _check_values(device, (positions, "positions", torch.int32, 0 if positions is None else n))
-    _on_device(device, (rotation, "rotation"))
-    _check(lib().focus_rotary(_ptr(x), *_hn(x), _ptr(out), *_hn(out), n, heads, d, _ptr(positions), pos_base, C.byref(rotation), _raw_stream(device)))
+    device, shape, xs, outs = _current_device(), x.shape, x.stride(), out.stride()
+    if not (x.dtype is out.dtype is _BF16 and x.get_device() == out.get_device() == device and out.shape == shape and len(shape) == 3 and xs[2] == 1 == outs[2]
+            and rotation.device in (device, None) and _fits(positions, _I32, device, shape[:1])):
+        _explain_devices(device, (x, "x"), (rotation, "rotation"))
+        if len(shape) != 3:
+            raise ValueError(f"x: expected [rows, heads, d], got {list(shape)}")
+        _explain_heads(device, shape[0], shape[2], (x, "x", shape[1]), (out, "out", shape[1]))
+        _check_values(device, (positions, "positions", _I32, 0 if positions is None else shape[0]))
+    n, heads, d = shape
+    status = lib().focus_rotary(x.data_ptr(), *_strides(shape, xs), out.data_ptr(), *_strides(shape, outs), n, heads, d, _ptr(positions), pos_base,
+                                C.byref(rotation), _raw_stream(device))
+    if status:
+        _check(status)
 
 
 def paged_append(cache: PagedCache, batch: PagedBatch, k_new, v_new, rotation: Rotation | None = None, q=None, q_out=None) -> None:
     """k_new, v_new bf16 [n_rows, H, d] (common strides) into the requests' pages; with q, q_out bf16 [n_rows, heads, d] those turned as well."""
-    device, n, d = _device_of(k_new, "k_new"), batch.n_rows, cache.head_dim
-    _check_heads(device, n, d, (k_new, "k_new", cache.n_heads), (v_new, "v_new", cache.n_heads))
-    strides = _hn(k_new)
-    if strides != _hn(v_new):
-        raise ValueError("k_new and v_new must share their strides")
+    device, shape, strides = _current_device(), k_new.shape, k_new.stride()
+    n, d = batch.n_rows, cache.head_dim
+    if not (shape == (n, cache.n_heads, d) == v_new.shape and strides == v_new.stride() and strides[2] == 1 and k_new.dtype is v_new.dtype is _BF16
+            and k_new.get_device() == v_new.get_device() == device and cache.device in (device, None) and batch.device in (device, None)
+            and (rotation is None or rotation.device in (device, None))):
+        _explain_devices(device, (k_new, "k_new"), (cache, "cache"), (batch, "batch"), (rotation, "rotation"))
+        _explain_heads(device, n, d, (k_new, "k_new", cache.n_heads), (v_new, "v_new", cache.n_heads))
+        if _strides(shape, strides) != _strides(shape, v_new.stride()):
+            raise ValueError("k_new and v_new must share their strides")
     heads, q_strides, out_strides = 0, (0, 0), (0, 0)
-    if (q is None) != (q_out is None):
+    if q is not None and q_out is not None:
+        q_shape, qs, outs = q.shape, q.stride(), q_out.stride()
+        heads = q_shape[1] if len(q_shape) == 3 else -1
+        if not (q_shape == (n, heads, d) == q_out.shape and qs[2] == 1 == outs[2] and q.dtype is q_out.dtype is _BF16 and q.get_device() == q_out.get_device() == device):
+            _explain_heads(device, n, d, (q, "q", heads), (q_out, "q_out", heads))
+        q_strides, out_strides = _strides(q_shape, qs), _strides(q_shape, outs)
+    elif q is not None or q_out is not None:
         raise ValueError("q and q_out go together")
-    if q is not None:
-        heads = q.shape[1] if q.dim() == 3 else -1
-        _check_heads(device, n, d, (q, "q", heads), (q_out, "q_out", heads))
-        q_strides, out_strides = _hn(q), _hn(q_out)
-    _on_device(device, (cache, "cache"), (batch, "batch"), (rotation, "rotation"))
-    _check(lib().focus_paged_append(C.byref(cache), C.byref(batch), _ptr(k_new), _ptr(v_new), *strides, None if rotation is None else C.byref(rotation),
-                                    _ptr(q), *q_strides, _ptr(q_out), *out_strides, heads, _raw_stream(device)))
+    status = lib().focus_paged_append(C.byref(cache), C.byref(batch), k_new.data_ptr(), v_new.data_ptr(), *_strides(shape, strides),
+                                      None if rotation is None else C.byref(rotation), _ptr(q), *q_strides, _ptr(q_out), *out_strides, heads, _raw_stream(device))
+    if status:
+        _check(status)
 
 
 def paged_attn_workspace(cache: PagedCache, batch: PagedBatch, n_q_heads: int) -> int:
@@ -695,13 +726,18 @@ def paged_attn_workspace(cache: PagedCache, batch: PagedBatch, n_q_heads: int) -
 
 def paged_attn(q, cache: PagedCache, batch: PagedBatch, causal: bool, out, lse, workspace) -> None:
     """q, out bf16 [n_rows, n_q_heads, d], lse fp32 [n_rows, n_q_heads] or None; workspace of paged_attn_workspace() bytes."""
-    device, n, d = _device_of(q, "q"), batch.n_rows, cache.head_dim
-    heads = q.shape[1] if q.dim() == 3 else -1
-    _check_heads(device, n, d, (q, "q", heads), (out, "out", heads))
-    _check_values(device, (lse, "lse", torch.float32, 0 if lse is None else n * heads))
-    _on_device(device, (cache, "cache"), (batch, "batch"))
-    _check(lib().focus_paged_attn(_ptr(q), *_hn(q), heads, C.byref(cache), C.byref(batch), int(causal), _ptr(out), *_hn(out), _ptr(lse), _ptr(workspace),
-                                  _space(workspace, device), _raw_stream(device)))
+    device, shape, qs, outs = _current_device(), q.shape, q.stride(), out.stride()
+    heads = shape[1] if len(shape) == 3 else -1
+    if not (shape == (batch.n_rows, heads, cache.head_dim) == out.shape and qs[2] == 1 == outs[2] and q.dtype is out.dtype is _BF16
+            and q.get_device() == out.get_device() == device and cache.device in (device, None) and batch.device in (device, None)
+            and _fits(lse, _F32, device, shape[:2])):
+        _explain_devices(device, (q, "q"), (cache, "cache"), (batch, "batch"))
+        _explain_heads(device, batch.n_rows, cache.head_dim, (q, "q", heads), (out, "out", heads))
+        _check_values(device, (lse, "lse", _F32, 0 if lse is None else shape[0] * heads))
+    status = lib().focus_paged_attn(q.data_ptr(), *_strides(shape, qs), heads, C.byref(cache), C.byref(batch), causal, out.data_ptr(), *_strides(shape, outs),
+                                    _ptr(lse), _ptr(workspace), _space(workspace, device), _raw_stream(device))
+    if status:
+        _check(status)
 
 
 def token_logprobs_workspace(n_rows: int, vocab: int, top_n: int) -> int:
@@ -711,24 +747,33 @@ def token_logprobs_workspace(n_rows: int, vocab: int, top_n: int) -> int:
 def token_logprobs(logits, targets, masked, logprob, entropy, top_ids, top_logprobs, workspace) -> None:
     """logits bf16 or fp32 [n_rows, vocab] (rows 16-byte aligned); targets int32 and logprob fp32 [n_rows] (both or neither), entropy fp32 [n_rows] or
     None, top_ids int32 and top_logprobs fp32 [n_rows, top_n] (both or neither); workspace of token_logprobs_workspace() bytes."""
-    if not logits.is_cuda or logits.dtype not in (torch.bfloat16, torch.float32):
-        raise TypeError(f"logits: expected a CUDA tensor of bfloat16 or float32, got {logits.dtype} on {logits.device}")
-    if logits.dim() != 2 or logits.stride(1) != 1:
+    dtype = logits.dtype
+    if not logits.is_cuda or (dtype is not _BF16 and dtype is not _F32):
+        raise TypeError(f"logits: expected a CUDA tensor of bfloat16 or float32, got {dtype} on {logits.device}")
+    shape, device = logits.shape, _current_device()
+    if len(shape) != 2 or logits.stride(1) != 1 or logits.get_device() != device:
+        _explain_devices(device, (logits, "logits"))
         raise ValueError("logits: expected [n_rows, vocab], innermost stride 1")
-    device = _device_of(logits, "logits")
-    rows, vocab = logits.shape
+    rows, vocab = shape
     stride = logits.stride(0) if rows > 1 else (vocab + 7) // 8 * 8  # (of one row any will do)
     if (top_ids is None) != (top_logprobs is None) or (targets is None) != (logprob is None):
         raise ValueError("targets and logprob, top_ids and top_logprobs go together")
-    top_n = 0 if top_ids is None else top_ids.shape[1] if top_ids.dim() == 2 else -1
-    for t, dtype, shape, name in ((targets, torch.int32, (rows,), "targets"), (logprob, torch.float32, (rows,), "logprob"), (entropy, torch.float32, (rows,), "entropy"),
-                                  (top_ids, torch.int32, (rows, top_n), "top_ids"), (top_logprobs, torch.float32, (rows, top_n), "top_logprobs")):
-        if t is not None and not (t.dtype == dtype and t.get_device() == device and t.shape == shape and t.is_contiguous()):
-            _need(t, dtype, name)
-            _device_of(t, name)
-            raise ValueError(f"{name}: expected {list(shape)} next to each other, got {list(t.shape)}, strides {t.stride()}")
-    if masked is not None and (masked.get_device() != device or masked.element_size() != 1 or masked.shape != (rows,) or not masked.is_contiguous()):
+    one = shape[:1]
+    top_n, many = 0, one
+    if top_ids is not None:
+        many = top_ids.shape
+        top_n = many[1] if len(many) == 2 else -1
+    if not (_fits(targets, _I32, device, one) and _fits(logprob, _F32, device, one) and _fits(entropy, _F32, device, one) and _fits(top_ids, _I32, device, (rows, top_n))
+            and _fits(top_logprobs, _F32, device, many)):
+        for t, kind, sizes, name in ((targets, _I32, one, "targets"), (logprob, _F32, one, "logprob"), (entropy, _F32, one, "entropy"),
+                                     (top_ids, _I32, (rows, top_n), "top_ids"), (top_logprobs, _F32, (rows, top_n), "top_logprobs")):
+            if not _fits(t, kind, device, sizes):
+                _need(t, kind, name)
+                _explain_devices(device, (t, name))
+                raise ValueError(f"{name}: expected {list(sizes)} next to each other, got {list(t.shape)}, strides {t.stride()}")
+    if masked is not None and (masked.get_device() != device or masked.element_size() != 1 or masked.shape != one or not masked.is_contiguous()):
         raise ValueError(f"masked: expected {rows} bytes on cuda:{device}, got {masked.dtype}, shape {tuple(masked.shape)} on {masked.device}")
-    _check(lib().focus_token_logprobs(_ptr(logits), int(logits.dtype == torch.float32), stride, _ptr(targets), _ptr(masked), rows, vocab, top_n,
-                                      _ptr(logprob), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs), _ptr(workspace), _space(workspace, device),
-                                      _raw_stream(device)))
+    status = lib().focus_token_logprobs(logits.data_ptr(), dtype is _F32, stride, _ptr(targets), _ptr(masked), rows, vocab, top_n, _ptr(logprob), _ptr(entropy),
+                                        _ptr(top_ids), _ptr(top_logprobs), _ptr(workspace), _space(workspace, device), _raw_stream(device))
+    if status:
+        _check(status)
