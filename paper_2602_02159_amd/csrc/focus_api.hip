@@ -1213,6 +1213,8 @@ int focus_paged_attn(const void* Q, int64_t q_stride_h, int64_t q_stride_n, int3
   p.workers = plan.workers;
   p.log_bundle = plan.log_bundle;
   p.unit_rows = plan.unit_rows;
+  p.most_groups = plan.most_groups;
+  p.whose = reinterpret_cast<int2*>(static_cast<char*>(workspace) + plan.whose);
   p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cache->head_dim));
   p.part_o = static_cast<float*>(workspace);
   p.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + plan.part_ml);

@@ -209,6 +209,7 @@ struct PagedAttn {
   float* lse;
   float* part_o;
   float2* part_ml;
+  int2* whose;      // [n_req, H, most_groups]
   int64_t qsh, qsn, osh, osn;
   int64_t ksp, ksh, ksn, vsp, vsh, vsn, esp, esh, esn;  // of the cache, in bytes
   PagedBatch b;
@@ -217,12 +218,14 @@ struct PagedAttn {
   int log_bundle;   // K/V heads of a bundle, which as many wavefronts of a workgroup take together
   int workers;      // bundles of wavefronts, among which the tiles of all requests are divided
   int unit_rows;    // rows of a partial result
+  int most_groups;  // groups of rows that a request may have
   float scale_log2;
 };
 struct PagedPlan {
   int q_tiles;      // 16-query tiles of a unit: 1 or 2
   int unit_rows, log_bundle, workers, groups;
-  size_t part_ml, total;
+  int most_groups;
+  size_t part_ml, whose, total;
 };
 PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch& b, int page);
 hipError_t launch_paged_attn(const PagedAttn& a, const PagedPlan& p, int head_dim, hipStream_t st);

@@ -83,14 +83,6 @@ struct Prefix {
     for (int r0 = kKept * kWave; r0 < p.b.n_req; r0 += kWave) sum += head_tiles<NT>(p, r0 + lane);
     total = wave_total(sum);
   }
-  // the tiles of a head before those of request r
-  __device__ __forceinline__ uint32_t before(const PagedAttn& p, int r, int lane) const {
-    uint32_t sum = 0u;
-#pragma unroll
-    for (int u = 0; u < kKept; ++u) sum += u * kWave + lane < r ? x[u] : 0u;
-    for (int r0 = kKept * kWave; r0 < r; r0 += kWave) sum += r0 + lane < r ? head_tiles<NT>(p, r0 + lane) : 0u;
-    return wave_total(sum);
-  }
   // the request in which tile t < total of a head lies
   __device__ __forceinline__ int find(const PagedAttn& p, uint32_t t, uint32_t& before, int lane) const {
     uint32_t mine = 0u, done = 0u;
@@ -377,7 +369,10 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
   const Shares shares((int64_t)prefix.total * bundles, p.workers);
   const int64_t begin = same(shares.begin(worker));
   const int n_tiles = (int)(same(shares.begin(worker + 1)) - begin);
-  if (n_tiles <= 0) return;
+  if (n_tiles <= 0) {  // (its pieces count for nothing where the units of its neighbours are joined)
+    for (int i = lane; i < p.unit_rows; i += kWave) p.part_ml[(int64_t)2 * wave_id * p.unit_rows + i] = make_float2(-INFINITY, 0.f);
+    return;
+  }
 
   Unit u;  // of the tile that is worked on,
   int t;
@@ -658,6 +653,14 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
     if (work) {
       ++t;
       if (t >= u.q.tiles || i == n_tiles - 1) {
+        if (t >= u.q.tiles && lane == 0) {  // of whom the pieces are
+          int2 whose = make_int2(0, 0);
+          if (start > 0) {
+            whose.x = shares.of(begin + i - (u.q.tiles - 1));
+            whose.y = worker - whose.x + 1;
+          }
+          p.whose[((int64_t)u.r * p.H + head_of(u)) * p.most_groups + u.qg] = whose;
+        }
         end_piece(start, t);
         start = t = 0;
         if (i < n_tiles - 1) next_unit(u);
@@ -666,8 +669,8 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
   }
 }
 
-// Joins the pieces of the units that several wavefronts worked on: NW wavefronts for one row of one query head.  The wavefront that had tile s of all
-// tiles follows from s alone, and with it where the pieces lie.
+// Joins the pieces of the units that several wavefronts worked on: NW wavefronts for one row of one query head.  Whose pieces they are the wavefront with
+// the last one has left (`whose`: the first of them, how many follow on one another; none: the unit is written).
 template <int D, int NT, int NW>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
   constexpr int kVec = D / 64, kAhead = 20;
@@ -676,20 +679,16 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hq = p.H * p.group;
   const int64_t at = NW == 1 ? (int64_t)list_index() * 4 + wave : (int64_t)list_index();
-  const int64_t row_at = at / Hq;
-  const int head = (int)(at - row_at * Hq);
-  const int r = (int)(row_at / p.b.max_rows), i = (int)(row_at - (int64_t)r * p.b.max_rows);
+  const int row_at = (int)(at / Hq), head = (int)(at - (int64_t)row_at * Hq);
+  const int r = row_at / p.b.max_rows, i = row_at - r * p.b.max_rows;
   if (r >= p.b.n_req) return;  // (the same in the whole workgroup where it has a barrier)
-  const Prefix<NT> prefix(p, lane);
-  const Request q = load_request<NT>(p, r);
-  if (i >= q.n) return;
   const int h = head / p.group, unit_row = i * p.group + head - h * p.group, qg = unit_row / (16 * NT), in_unit = unit_row - qg * 16 * NT;
-  const int bundles = p.H >> p.log_bundle, bundle = h >> p.log_bundle, in_bundle = h - (bundle << p.log_bundle);
-  const Shares shares((int64_t)prefix.total * bundles, p.workers);
-  const int64_t s = (int64_t)prefix.before(p, r, lane) * bundles + ((int64_t)bundle * q.groups + qg) * q.tiles;
-  const int w0 = (int)same(shares.of(s)), w1 = (int)same(shares.of(s + q.tiles - 1));
-  if (w0 == w1) return;
-  const int n = w1 - w0 + 1;  // (some of them may have no tile)
+  const int2 whose = p.whose[((int64_t)r * p.H + h) * p.most_groups + qg];
+  const RequestRows q = request_rows(p.b, r);
+  if (i >= q.n) return;  // (nor has anybody written `whose`)
+  const int w0 = __builtin_amdgcn_readfirstlane(whose.x), n = __builtin_amdgcn_readfirstlane(whose.y);
+  if (n == 0) return;
+  const int in_bundle = h & ((1 << p.log_bundle) - 1);
   // Wavefront w takes the pieces w, w + NW, ..., kAhead of them at a time: their statistics, lane by lane, and their rows, all requested at once.
   float m_run = -INFINITY, l_run = 0.f, o[kVec];
 #pragma unroll
@@ -704,7 +703,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
     float y[kAhead][kVec];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const float* src = p.part_o + slot_row(min(first + (k0 + k) * NW, n - 1)) * D + lane * kVec;
+#pragma unroll
+      for (int v = 0; v < kVec; ++v) y[k][v] = 0.f;
+      if (k0 + k >= mine) continue;  // (the same in all lanes)
+      const float* src = p.part_o + slot_row(first + (k0 + k) * NW) * D + lane * kVec;
       if constexpr (kVec == 2) {
         const float2 x = *reinterpret_cast<const float2*>(src);
         y[k][0] = x.x;
@@ -713,8 +715,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
         y[k][0] = *src;
       }
     }
-    // (nothing was written for a wavefront without a tile)
-    if (j >= n || lane >= kAhead || shares.begin(w0 + j_there) == shares.begin(w0 + j_there + 1)) ml = make_float2(-INFINITY, 0.f);
+    if (j >= n || lane >= kAhead) ml = make_float2(-INFINITY, 0.f);
     float top = ml.x;
 #pragma unroll
     for (int k = 32; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k, kWave));
@@ -780,7 +781,9 @@ PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch
   p.workers = p.groups * per_group;
   const size_t slots = (size_t)2 * p.groups * kWavesPerGroup;
   p.part_ml = (slots * p.unit_rows * head_dim * sizeof(float) + 255) & ~(size_t)255;
-  p.total = p.part_ml + slots * p.unit_rows * sizeof(float2);
+  p.whose = (p.part_ml + slots * p.unit_rows * sizeof(float2) + 255) & ~(size_t)255;
+  p.most_groups = (int)ceil_div64(rows, 16 * p.q_tiles);
+  p.total = p.whose + (size_t)b.n_req * n_heads * p.most_groups * sizeof(int2);
   return p;
 }
 
