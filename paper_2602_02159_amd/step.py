@@ -7,7 +7,8 @@ by one call are consumed on the device by the next.  Because a step is a fixed s
 fixed buffers it can also be captured into a HIP graph (`capture`) and replayed.
 
 FocusStep runs one step over layers whose K/V tensors are given; FocusDecoder owns the KV caches and sequences a
-whole generation block: the block entry, then steps with the per-layer cache updates of Eq. 3.
+whole generation block: the block entry, then steps with the per-layer cache updates of Eq. 3.  FocusPagedStep runs a step
+of many requests at once, whose caches are pages.
 """
 from __future__ import annotations
 
@@ -374,3 +375,102 @@ class FocusDecoder:
                 FocusStep._issue(calls, torch.cuda.current_stream().cuda_stream)
             graphs.append(g)
         self._g_entry, self._g_step = graphs
+
+
+class FocusPagedStep:
+    """A step of up to n_req requests over a stack of attention layers whose KV caches are pages: the new rows of every request go to its pages, K and
+    Q turned by their positions, and attend to what the request has there.  Nothing is computed here; the caller fills the buffers, whose places do
+    not change, so that the calls can be replayed as a HIP graph while requests come, grow and go:
+
+      seq_len [n_req] (0: nobody there), page_table [n_req, table_width] (-1: no page), with max_rows > 1 row_start [n_req + 1] and, with
+      `scattered`, positions [n_rows]: see focus_paged_batch
+      q[l] bf16 [n_rows, n_q_heads, d], k_new[l] / v_new[l] bf16 [n_rows, n_heads, d]   before the rotation
+      with vocab: logits bf16 [n_rows, vocab], targets int32 [n_rows], masked u8 [n_rows]
+
+    run():    per layer  focus_paged_append, focus_paged_attn -> out[l] bf16 [n_rows, n_q_heads, d], lse[l] [n_rows, n_q_heads]
+    score():  focus_token_logprobs -> logprob, entropy [n_rows], top_ids, top_logprobs [n_rows, top_n]
+    issue(l) enqueues the calls of one layer, for a model whose projections lie between them.
+    `rotation`: from make_rotation, or None.  `quantised`: pages of eight-bit rows.  The pages of layer l are caches[l]; all layers share the table.
+    """
+
+    def __init__(self, n_layers: int, n_pages: int, page: int, n_heads: int, n_q_heads: int, head_dim: int, n_req: int, table_width: int, device,
+                 max_rows: int = 1, n_rows: int | None = None, rotation=None, causal: bool = False, quantised: bool = False, scattered: bool = False,
+                 vocab: int | None = None, top_n: int = 0):
+        n_rows = n_req * max_rows if n_rows is None else n_rows
+        H, d, Hq = n_heads, head_dim, n_q_heads
+        zeros = lambda dtype, *shape: torch.zeros(shape, dtype=dtype, device=device)
+        bf16, f32, i32, u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+        self.n_layers, self.n_rows, self.rotation = n_layers, n_rows, rotation
+        self.seq_len = zeros(i32, n_req)
+        self.page_table = torch.full((n_req, table_width), -1, dtype=i32, device=device)
+        self.row_start = zeros(i32, n_req + 1) if max_rows > 1 else None
+        self.positions = torch.full((n_rows,), -1, dtype=i32, device=device) if scattered else None
+        rows = u8 if quantised else bf16
+        self.k_pages, self.v_pages = ([zeros(rows, n_pages, H, page, d) for _ in range(n_layers)] for _ in range(2))
+        self.k_exp, self.v_exp = ([zeros(u8, n_pages, H, page) if quantised else None for _ in range(n_layers)] for _ in range(2))
+        self.caches = [fb.make_paged_cache(*t) for t in zip(self.k_pages, self.v_pages, self.k_exp, self.v_exp)]
+        self.batch = fb.make_paged_batch(self.seq_len, self.page_table, self.row_start, max_rows, n_rows, self.positions)
+        self.q, self.out = ([zeros(bf16, n_rows, Hq, d) for _ in range(n_layers)] for _ in range(2))
+        self.k_new, self.v_new = ([zeros(bf16, n_rows, H, d) for _ in range(n_layers)] for _ in range(2))
+        self.lse = [zeros(f32, n_rows, Hq) for _ in range(n_layers)]
+        self.q_turned = zeros(bf16, n_rows, Hq, d)
+        need = fb.paged_attn_workspace(self.caches[0], self.batch, Hq)
+        if need == 0:
+            raise fb.FocusError(fb.FOCUS_EINVAL, fb.last_error())
+        self.workspace = torch.empty(need, dtype=u8, device=device)
+        lib, p, strides = fb.lib(), (lambda t: None if t is None else C.c_void_p(t.data_ptr())), (lambda t: (t.stride(1), t.stride(0)))
+        spin = None if rotation is None else C.byref(rotation)
+        self.layer_calls = []
+        for l in range(n_layers):
+            cache, batch = C.byref(self.caches[l]), C.byref(self.batch)
+            self.layer_calls.append([
+                (lib.focus_paged_append, (cache, batch, p(self.k_new[l]), p(self.v_new[l]), *strides(self.k_new[l]), spin, p(self.q[l]), *strides(self.q[l]),
+                                          p(self.q_turned), *strides(self.q_turned), Hq)),
+                (lib.focus_paged_attn, (p(self.q_turned), *strides(self.q_turned), Hq, cache, batch, int(causal), p(self.out[l]), *strides(self.out[l]),
+                                        p(self.lse[l]), p(self.workspace), self.workspace.numel()))])
+        self.score_calls = []
+        if vocab is not None:
+            self.logits = torch.zeros((n_rows, (vocab + 7) // 8 * 8), dtype=bf16, device=device)[:, :vocab]  # aligned rows
+            self.targets, self.masked = zeros(i32, n_rows), torch.ones(n_rows, dtype=u8, device=device)
+            self.logprob, self.entropy = zeros(f32, n_rows), zeros(f32, n_rows)
+            self.top_ids, self.top_logprobs = (zeros(i32, n_rows, top_n), zeros(f32, n_rows, top_n)) if top_n else (None, None)
+            self.score_space = torch.empty(max(fb.token_logprobs_workspace(n_rows, vocab, top_n), 256), dtype=u8, device=device)
+            self.score_calls.append((lib.focus_token_logprobs, (
+                p(self.logits), 0, self.logits.stride(0), p(self.targets), p(self.masked), n_rows, vocab, top_n, p(self.logprob), p(self.entropy),
+                p(self.top_ids), p(self.top_logprobs), p(self.score_space), self.score_space.numel())))
+        self._g_run = self._g_score = None
+
+    def issue(self, layer: int):
+        """Enqueue the calls of one layer on the current stream."""
+        FocusStep._issue(self.layer_calls[layer], torch.cuda.current_stream().cuda_stream)
+
+    def run(self):
+        """Enqueue all layers (eagerly, or by replaying the captured graph)."""
+        if self._g_run is not None:
+            self._g_run.replay()
+        else:
+            for l in range(self.n_layers):
+                self.issue(l)
+
+    def score(self):
+        if self._g_score is not None:
+            self._g_score.replay()
+        else:
+            FocusStep._issue(self.score_calls, torch.cuda.current_stream().cuda_stream)
+
+    def capture(self):
+        """Capture run and score into a HIP graph each, after one eager run of both on what the buffers hold (which writes rows to pages: call this
+        with seq_len or the page table empty, or before the pages hold anything)."""
+        self._g_run = self._g_score = None
+        self.run()
+        self.score()
+        torch.cuda.synchronize()
+        graphs = []
+        for enqueue, there in ((self.run, True), (self.score, bool(self.score_calls))):
+            graph = None
+            if there:
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph):
+                    enqueue()
+            graphs.append(graph)
+        self._g_run, self._g_score = graphs
