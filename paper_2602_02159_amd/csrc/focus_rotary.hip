@@ -15,7 +15,10 @@ namespace focus {
 // A workgroup has R = 512 / D rows, whose R * D / 2 angles are one a thread; cos and sin meet the heads in LDS.  The items of a workgroup are its
 // rows times its slots (heads of Q, of K, of V); D / 16 neighbouring threads have one item, sixteen values each: where pairs are halves
 // apart eight of each half (so that a pair is in one thread), else sixteen neighbours.  Values that are not turned are divided the same way.
-constexpr int kTurnItems = 4;  // under way per thread
+// Items under way per thread, read past the caches, where nothing else reads them.  Bound by HBM: 32 768 rows of 32 heads of 128, 537 MB, in 92.3 us =
+// 5.8 TB/s (a copy of a gigabyte: 5.2); prompts of 8 000 rows into eight-bit pages, 185 MB, in 41.6.  One, two, three, four, six items 99.9, 96.2, 99.2, 99.6, 95.7
+// and 45.8, 44.3, 46.5, 45.5, 51.4 us through the caches; past them two 92.3 and 41.6.  A few rows are one launch and two round trips: 2.9 us.
+constexpr int kTurnItems = 2;
 
 template <int D, bool QUANT, bool PAGES>
 __global__ __launch_bounds__(256) void turn_rows_kernel(const TurnRows p) {
@@ -65,8 +68,8 @@ __global__ __launch_bounds__(256) void turn_rows_kernel(const TurnRows p) {
         src = p.Q + row * p.qsn + (int64_t)x.slot * p.qsh;
       else
         src = (is_v ? p.Vn : p.Kn) + row * p.nsn + (int64_t)(x.slot - p.n_q_heads - (is_v ? p.n_heads : 0)) * p.nsh;
-      a[u] = *reinterpret_cast<const uint4*>(src + (is_v ? 16 * c : turn_a));
-      b[u] = *reinterpret_cast<const uint4*>(src + (is_v ? 16 * c + 8 : turn_b));
+      a[u] = load_stream16(src + (is_v ? 16 * c : turn_a));
+      b[u] = load_stream16(src + (is_v ? 16 * c + 8 : turn_b));
     }
   };
   load(tid / kThreads);
