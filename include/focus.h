@@ -430,7 +430,7 @@ typedef struct focus_rotation {
  *   positions [dev] int32[n_rows] or NULL (= 0, 1, 2, ...): row i is at position pos_base + positions[i].  Rows with positions[i] < 0 are
  *             left out (nothing is written), so that the active_idx of focus_select_queries may be handed over as it is, with pos_base =
  *             the position of the generation block's first token
- * n_rows >= 1, 1 <= n_heads <= 65535.
+ * 1 <= n_rows <= 2^25, 1 <= n_heads <= 65535.
  */
 int focus_rotary(const void* X, int64_t x_stride_h, int64_t x_stride_n, void* out, int64_t o_stride_h, int64_t o_stride_n, int32_t n_rows,
                  int32_t n_heads, int32_t head_dim, const int32_t* positions, int32_t pos_base, const focus_rotation* rot, void* stream);
@@ -483,7 +483,8 @@ typedef struct focus_paged_batch {
  *   Q, Q_out     [dev] bf16 [n_rows, n_q_heads, d], strides q_stride_* and qo_stride_*: Q_out = Q turned (Q itself with the same strides, or clear
  *                of it); both NULL with n_q_heads = 0
  * A row without a position (positions[i] < 0) is left out, Q included; of one whose cache row does not exist K and V are left out.  Of rows of
- * one request with the same position the last one's K and V stay.  A page that several requests list must not be written by two of them.
+ * one request with the same position the last one's K and V stay.  A page that is listed more than once must not be written through two entries.
+ * ceil(max_rows / 4) * n_req <= 2^25: max_rows is a bound that the launch is made for.
  */
 int focus_paged_append(const focus_paged_cache* cache, const focus_paged_batch* batch, const void* K_new, const void* V_new, int64_t new_stride_h,
                        int64_t new_stride_n, const focus_rotation* rot, const void* Q, int64_t q_stride_h, int64_t q_stride_n, void* Q_out,
@@ -500,7 +501,8 @@ int focus_paged_append(const focus_paged_cache* cache, const focus_paged_batch* 
  * written, leaving pages out of page_table (entries of -1) is the attention over the others.  Queries as for focus_quant_cache over rows of eight bits.
  *   workspace [dev] focus_paged_attn_workspace() bytes, 16-byte aligned; nothing is assumed about its contents
  * The same arguments give the same bits; in which order a row's keys are added up depends on the lengths of all requests.
- * ceil(n_q_heads / H * max_rows / 16) * ceil(table_width * page / 32) * max(n_req, n_q_heads) < 2^31, with table_width * page < 2^31.
+ * ceil(n_q_heads / H * max_rows / 16) * ceil(table_width * page / 32) * max(n_req, n_q_heads) < 2^31, with table_width * page < 2^31,
+ * and n_req * max_rows * n_q_heads <= 2^27.
  */
 int focus_paged_attn(const void* Q, int64_t q_stride_h, int64_t q_stride_n, int32_t n_q_heads, const focus_paged_cache* cache,
                      const focus_paged_batch* batch, int32_t causal, void* out, int64_t o_stride_h, int64_t o_stride_n, float* lse, void* workspace,

@@ -600,6 +600,8 @@ static int check_paged_queries(const char* who, const focus_paged_cache* c, cons
   const int64_t tiles = ceil_div64((int64_t)b->table_width * c->page, 32), groups = ceil_div64((int64_t)n_q_heads / c->n_heads * std::min(b->max_rows, b->n_rows), 16);
   if (groups > INT32_MAX / tiles || groups * tiles > INT32_MAX / std::max(b->n_req, n_q_heads))
     return fail(FOCUS_EUNSUPPORTED, "%s: %lld groups of 16 rows, %lld tiles of 32 keys, %d requests, %d heads are too many", who, (long long)groups, (long long)tiles, b->n_req, n_q_heads);
+  if ((int64_t)b->n_req * std::min(b->max_rows, b->n_rows) > kPagedMaxJoins / n_q_heads)
+    return fail(FOCUS_EUNSUPPORTED, "%s: n_req=%d requests of up to max_rows=%d rows of %d heads are too many", who, b->n_req, b->max_rows, n_q_heads);
   return FOCUS_OK;
 }
 
@@ -1088,7 +1090,7 @@ int focus_rotary(const void* X, int64_t x_stride_h, int64_t x_stride_n, void* ou
   if (!rot) return fail(FOCUS_EINVAL, "%s: NULL pointer", who);
   if (int rc = check_head_dim(who, head_dim)) return rc;
   if (int rc = check_rotation(who, rot, head_dim)) return rc;
-  if (n_rows < 1) return fail(FOCUS_EINVAL, "%s: n_rows=%d less than 1", who, n_rows);
+  if (n_rows < 1 || n_rows > kTurnMaxRows) return fail(FOCUS_EINVAL, "%s: n_rows=%d not in [1, %d]", who, n_rows, kTurnMaxRows);
   if (n_heads < 1 || n_heads > 65535) return fail(FOCUS_EINVAL, "%s: n_heads=%d not in [1, 65535]", who, n_heads);
   if (int rc = check_rows(who, "X", X, x_stride_h, x_stride_n)) return rc;
   if (int rc = check_rows(who, "out", out, o_stride_h, o_stride_n, n_heads, n_rows)) return rc;
@@ -1141,6 +1143,8 @@ int focus_paged_append(const focus_paged_cache* cache, const focus_paged_batch* 
     if (int rc = check_rows(who, "Q_out", Q_out, qo_stride_h, qo_stride_n, n_q_heads, batch->n_rows)) return rc;
     if (Q == Q_out && (q_stride_h != qo_stride_h || q_stride_n != qo_stride_n)) return fail(FOCUS_EINVAL, "%s: in place, but with other strides", who);
   }
+  if (ceil_div64(std::min(batch->max_rows, batch->n_rows), 4) * batch->n_req > kTurnMaxRows)
+    return fail(FOCUS_EUNSUPPORTED, "%s: n_req=%d requests of up to max_rows=%d rows are too many", who, batch->n_req, batch->max_rows);
   TurnRows p = {};
   p.Q = static_cast<const uint16_t*>(Q);
   p.Qo = static_cast<uint16_t*>(Q_out);

@@ -198,6 +198,7 @@ struct TurnRows {
   PagedBatch b;
   int pos_base, rot_dim, interleaved, n_q_heads, n_heads, page, n_pages;
 };
+constexpr int kTurnMaxRows = 1 << 25;  // one axis of a launch has fewer than 2^24 workgroups of 256, four rows each; and of a batch's launch, most of them empty, at most so many
 hipError_t launch_turn_rows(const TurnRows& p, int head_dim, bool pages, bool quant, hipStream_t st);
 struct PagedAttn {
   const uint16_t* Q;
@@ -227,6 +228,7 @@ struct PagedPlan {
   int most_groups;
   size_t part_ml, whose, total;
 };
+constexpr int64_t kPagedMaxJoins = int64_t(1) << 27;  // rows of a query head that a batch may have: workgroups of the second launch, most of them empty
 PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch& b, int page);
 hipError_t launch_paged_attn(const PagedAttn& a, const PagedPlan& p, int head_dim, hipStream_t st);
 // Log probabilities (focus_logprob.hip)

@@ -136,7 +136,7 @@ def test_rotation_refused(bad):
 
 @pytest.mark.parametrize("args,status", [
     (dict(X=None), -1), (dict(out=None), -1), (dict(X=C.c_void_p(8)), -1), (dict(xh=4), -1), (dict(on=12), -1), (dict(rows=0), -1), (dict(heads=0), -1),
-    (dict(heads=65536), -1), (dict(d=96), -2), (dict(d=256), -2), (dict(on=0), -1), (dict(oh=0), -1), (dict(xn=-256), -1), (dict(on=512), -1)])
+    (dict(heads=65536), -1), (dict(rows=(1 << 25) + 1), -1), (dict(d=96), -2), (dict(d=256), -2), (dict(on=0), -1), (dict(oh=0), -1), (dict(xn=-256), -1), (dict(on=512), -1)])
 def test_rotary_refused(args, status):
     a = dict(X=P, xh=64, xn=256, out=P, oh=64, on=256, rows=4, heads=4, d=64)
     a.update(args)
@@ -168,6 +168,8 @@ def test_paged_calls_refused():
     assert L.focus_paged_attn_workspace(c, b, 6) == 0 and L.focus_paged_attn_workspace(C.byref(_cache(head_dim=80)), b, 4) == 0
     many = C.byref(_batch(row_start=1 << 20, n_req=60000, max_rows=4096, n_rows=1 << 20, table_width=1 << 20, table_stride=1 << 20))
     assert L.focus_paged_attn_workspace(c, many, 4) == 0 and attn(bb=many) == fb.FOCUS_EUNSUPPORTED
+    wide = C.byref(_batch(row_start=1 << 20, n_req=30000, max_rows=5000, n_rows=1 << 20))
+    assert attn(bb=wide) == fb.FOCUS_EUNSUPPORTED and L.focus_paged_append(c, wide, P, P, 64, 256, None, None, 0, 0, None, 0, 0, 0, None) == fb.FOCUS_EUNSUPPORTED
     append = lambda k=P, v=P, q=None, qo=None, heads=0, h=64, qoh=64: L.focus_paged_append(c, b, k, v, h, 256, None, q, 64, 256, qo, qoh, 256, heads, None)
     assert append(k=None) == append(v=None) == append(q=P) == append(qo=P) == append(heads=4) == append(h=12) == fb.FOCUS_EINVAL
     assert append(q=P, qo=P, heads=0) == append(q=P, qo=P, heads=4, qoh=128) == append(q=P, qo=P, heads=4, qoh=0) == fb.FOCUS_EINVAL
@@ -546,6 +548,41 @@ def test_attention_of_far_pages():
         m = rows.stop - rows.start
         for h in range(8):
             check_attention(out[rows, h], lse[rows, h], attend64(q[rows, h], new_k[rows, h // 2], new_v[rows, h // 2], torch.ones((m, m)).tril().bool()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("page,d", [(16, 128), (24, 64)])
+def test_pages_and_tables_within_larger_tensors(page, d):
+    """K and V side by side in one pool with room between its rows, a table that is a part of a wider one, queries and results in wider rows."""
+    H, group, n_pages, lens, rows = 3, 2, 40, [130, 5, 77], [3, 1, 2]
+    pool = torch.full((n_pages, 2, page, H, d + 8), math.nan, dtype=torch.bfloat16, device=DEV)
+    k, v = (pool[:, i, :, :, :d].transpose(1, 2) for i in range(2))
+    cache = fb.make_paged_cache(k, v)
+    width = -(-130 // page)
+    g = torch.Generator().manual_seed(11)
+    wide = torch.full((3, width + 5), -7, dtype=torch.int32)
+    wide[:, 2:2 + width] = torch.randperm(n_pages, generator=g)[:3 * width].view(3, width).int()
+    table = wide.to(DEV)[:, 2:2 + width]
+    seq = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    history = [torch.randn((2, n, H, d), generator=g).bfloat16() for n in lens]
+    start = torch.tensor([0, *np.cumsum(lens)], dtype=torch.int32, device=DEV)
+    fill = fb.make_paged_batch(seq, table, start, max(lens), sum(lens))
+    new = torch.cat(history, 1).to(DEV)
+    fb.paged_append(cache, fill, new[0], new[1])
+    assert bool(pool[..., d:].isnan().all())
+    n = sum(rows)
+    batch = fb.make_paged_batch(seq, table, torch.tensor([0, *np.cumsum(rows)], dtype=torch.int32, device=DEV), max(rows), n)
+    q = torch.randn((n, H * group + 1, 2 * d), generator=g).bfloat16().to(DEV)[:, 1:, d:]
+    room = torch.full((n, 2 * H * group, d), 4.0, dtype=torch.bfloat16, device=DEV)
+    out, lse = room[:, ::2], torch.zeros((n, H * group), device=DEV)
+    fb.paged_attn(q, cache, batch, True, out, lse, workspace(cache, batch, H * group))
+    assert bool((room[:, 1::2] == 4.0).all())
+    for r, past in enumerate(history):
+        at = [i for i, s, _ in places(lens, rows) if s == r]
+        seen = torch.arange(lens[r])[None] <= torch.tensor([p for _, s, p in places(lens, rows) if s == r])[:, None]
+        for h in range(H * group):
+            ref = attend64(q[at, h].cpu().double(), past[0, :, h // group].double(), past[1, :, h // group].double(), seen)
+            check_attention(out[at, h].cpu(), lse[at, h].cpu(), ref)
 
 
 @pytest.mark.gpu
