@@ -501,8 +501,8 @@ int focus_paged_append(const focus_paged_cache* cache, const focus_paged_batch* 
  * written, leaving pages out of page_table (entries of -1) is the attention over the others.  Queries as for focus_quant_cache over rows of eight bits.
  *   workspace [dev] focus_paged_attn_workspace() bytes, 16-byte aligned; nothing is assumed about its contents
  * The same arguments give the same bits; in which order a row's keys are added up depends on the lengths of all requests.
- * ceil(n_q_heads / H * max_rows / 16) * ceil(table_width * page / 32) * max(n_req, n_q_heads) < 2^31, with table_width * page < 2^31,
- * and n_req * max_rows * n_q_heads <= 2^27.
+ * ceil(n_q_heads / H * max_rows / 16) * ceil(table_width * page / 32) * H * n_req < 2^31, table_width * page < 2^31 and
+ * n_req * max_rows * n_q_heads <= 2^27.
  */
 int focus_paged_attn(const void* Q, int64_t q_stride_h, int64_t q_stride_n, int32_t n_q_heads, const focus_paged_cache* cache,
                      const focus_paged_batch* batch, int32_t causal, void* out, int64_t o_stride_h, int64_t o_stride_n, float* lse, void* workspace,

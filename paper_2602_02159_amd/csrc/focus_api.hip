@@ -598,8 +598,8 @@ static PagedBatch paged_batch(const focus_paged_batch& b) {
 static int check_paged_queries(const char* who, const focus_paged_cache* c, const focus_paged_batch* b, int32_t n_q_heads) {
   if (n_q_heads < 1 || n_q_heads > 65535 || n_q_heads % c->n_heads) return fail(FOCUS_EINVAL, "%s: n_q_heads=%d not a multiple of n_heads=%d up to 65535", who, n_q_heads, c->n_heads);
   const int64_t tiles = ceil_div64((int64_t)b->table_width * c->page, 32), groups = ceil_div64((int64_t)n_q_heads / c->n_heads * std::min(b->max_rows, b->n_rows), 16);
-  if (groups > INT32_MAX / tiles || groups * tiles > INT32_MAX / std::max(b->n_req, n_q_heads))
-    return fail(FOCUS_EUNSUPPORTED, "%s: %lld groups of 16 rows, %lld tiles of 32 keys, %d requests, %d heads are too many", who, (long long)groups, (long long)tiles, b->n_req, n_q_heads);
+  if (groups > INT32_MAX / tiles || groups * tiles > INT32_MAX / c->n_heads || groups * tiles * c->n_heads > INT32_MAX / b->n_req)
+    return fail(FOCUS_EUNSUPPORTED, "%s: %lld groups of 16 rows, %lld tiles of 32 keys, %d requests, %d K/V heads are too many", who, (long long)groups, (long long)tiles, b->n_req, c->n_heads);
   if ((int64_t)b->n_req * std::min(b->max_rows, b->n_rows) > kPagedMaxJoins / n_q_heads)
     return fail(FOCUS_EUNSUPPORTED, "%s: n_req=%d requests of up to max_rows=%d rows of %d heads are too many", who, b->n_req, b->max_rows, n_q_heads);
   return FOCUS_OK;
@@ -1216,6 +1216,8 @@ int focus_paged_attn(const void* Q, int64_t q_stride_h, int64_t q_stride_n, int3
   p.page_shift = (cache->page & (cache->page - 1)) == 0 ? __builtin_ctz(cache->page) : -1;
   p.workers = plan.workers;
   p.log_bundle = plan.log_bundle;
+  p.per_worker = 1.0 / plan.workers;
+  p.per_bundle = 1.0 / (cache->n_heads >> plan.log_bundle);
   p.unit_rows = plan.unit_rows;
   p.most_groups = plan.most_groups;
   p.whose = reinterpret_cast<int2*>(static_cast<char*>(workspace) + plan.whose);

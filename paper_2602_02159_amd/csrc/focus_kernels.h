@@ -221,6 +221,7 @@ struct PagedAttn {
   int unit_rows;    // rows of a partial result
   int most_groups;  // groups of rows that a request may have
   float scale_log2;
+  double per_worker, per_bundle;  // 1 / workers, 1 / (H >> log_bundle)
 };
 struct PagedPlan {
   int q_tiles;      // 16-query tiles of a unit: 1 or 2

@@ -61,9 +61,17 @@ __device__ __forceinline__ uint32_t head_tiles(const PagedAttn& p, int r) {
 __device__ __forceinline__ uint32_t wave_total(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_readfirstlane((int)wave_reduce_u32(x, [](uint32_t a, uint32_t b) { return a + b; }));
 }
-// a number that is the same in all lanes, in scalar registers: what follows from it is worked out once a wavefront
-__device__ __forceinline__ int64_t same(int64_t x) {
-  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)((uint64_t)x >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+// a number that is the same in all lanes, in a scalar register: what follows from it is worked out once a wavefront
+__device__ __forceinline__ int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// sum of x over the lanes up to this one
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x, int lane) {
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, true);  // row_shr 1, 2, 4, 8: within sixteen lanes
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, true);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, true);
+  x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, true);
+  const uint32_t a = (uint32_t)__builtin_amdgcn_readlane((int)x, 15), b = (uint32_t)__builtin_amdgcn_readlane((int)x, 31), c = (uint32_t)__builtin_amdgcn_readlane((int)x, 47);
+  return x + (lane >= 16 ? a : 0u) + (lane >= 32 ? b : 0u) + (lane >= 48 ? c : 0u);
 }
 
 // The requests' tiles as one wavefront adds them up, 64 requests a turn; those of the first kKept turns stay in registers.
@@ -97,41 +105,22 @@ struct Prefix {
       if (t < done + sum) break;
       done += sum;
     }
-    uint32_t incl = mine;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const uint32_t y = __shfl_up(incl, o, kWave);
-      if (lane >= o) incl += y;
-    }
+    const uint32_t incl = wave_scan(mine, lane);
     const int at = __builtin_ctzll(__ballot(done + incl > t) | (1ull << 63));
     before = done + (uint32_t)__builtin_amdgcn_readlane((int)(incl - mine), at);
     return r0 + at;
   }
 };
 
-// The tiles of all requests, R of them, among W wavefronts: floor(i R / W) is the first one of wavefront i.  Quotients in 64-bit floating
-// point, put right by one where they are next to a whole number (a division of 64-bit integers takes longer than a round trip to L2).
+// The tiles of all requests, R < 2^31 of them, among W bundles of wavefronts: floor(i R / W) is the first one of the i-th.  In 64-bit floating point, where
+// products are exact and quotients are moved off the whole numbers by half of the least distance from them (a division of integers is as
+// long as a round trip to L2).
 struct Shares {
-  int64_t base;  // R = base * W + rest
-  int rest, workers;
-  double per_worker;  // 1 / W
-  __device__ __forceinline__ Shares(int64_t R, int W) : workers(W) {
-    per_worker = 1.0 / (double)W;
-    base = (int64_t)((double)R * per_worker);
-    rest = (int)(R - base * W);
-    if (rest < 0) rest += W, --base;
-    if (rest >= W) rest -= W, ++base;
-  }
-  // floor(rest i / W): rest i + 1/2 is at least 1 / (2 W) from the next multiple of W
-  __device__ __forceinline__ int64_t begin(int i) const { return base * i + (int)(((double)(rest * i) + 0.5) * per_worker); }
-  // the last wavefront that begins with tile s or before it
-  __device__ __forceinline__ int of(int64_t s) const {
-    int i = (int)(((double)s + 0.5) / ((double)base + (double)rest * per_worker));
-    i = min(max(i, 0), workers - 1);
-    while (i > 0 && begin(i) > s) --i;
-    while (i + 1 < workers && begin(i + 1) <= s) ++i;
-    return i;
-  }
+  double R, workers, per_worker;
+  __device__ __forceinline__ Shares(uint32_t tiles, int W, double reciprocal) : R((double)tiles), workers((double)W), per_worker(reciprocal) {}
+  __device__ __forceinline__ int begin(int i) const { return (int)((R * (double)i + 0.5) * per_worker); }
+  // the last one that begins with tile s or before it: floor(((s + 1) W - 1) / R)
+  __device__ __forceinline__ int of(int s) const { return (int)(((double)(s + 1) * workers - 0.5) / R); }
 };
 
 // A group of rows of a request and a bundle of K/V heads, one a wavefront
@@ -366,9 +355,8 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
   char* ring = ring_sh + wave * G::kBytes;
 
   const Prefix<NT> prefix(p, lane);
-  const Shares shares((int64_t)prefix.total * bundles, p.workers);
-  const int64_t begin = same(shares.begin(worker));
-  const int n_tiles = (int)(same(shares.begin(worker + 1)) - begin);
+  const Shares shares(prefix.total * (uint32_t)bundles, p.workers, p.per_worker);
+  const int begin = same(shares.begin(worker)), n_tiles = same(shares.begin(worker + 1)) - begin;
   if (n_tiles <= 0) {  // (its pieces count for nothing where the units of its neighbours are joined)
     for (int i = lane; i < p.unit_rows; i += kWave) p.part_ml[(int64_t)2 * wave_id * p.unit_rows + i] = make_float2(-INFINITY, 0.f);
     return;
@@ -378,9 +366,9 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
   int t;
   {
     uint32_t before;
-    u.r = prefix.find(p, (uint32_t)((uint64_t)begin / (uint32_t)bundles), before, lane);
+    u.r = prefix.find(p, (uint32_t)same((int)(((double)begin + 0.5) * p.per_bundle)), before, lane);  // begin / bundles
     u.q = load_request<NT>(p, u.r);
-    const uint32_t local = (uint32_t)(begin - (int64_t)before * bundles), unit = local / (uint32_t)u.q.tiles;
+    const uint32_t local = (uint32_t)begin - before * (uint32_t)bundles, unit = local / (uint32_t)u.q.tiles;
     t = (int)(local - unit * (uint32_t)u.q.tiles);
     u.b = (int)(unit / (uint32_t)u.q.groups);
     u.qg = (int)unit - u.b * u.q.groups;
