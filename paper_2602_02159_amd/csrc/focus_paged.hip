@@ -666,15 +666,15 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
   __shared__ float o_sh[NW][D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hq = p.H * p.group;
-  const int64_t at = NW == 1 ? (int64_t)list_index() * 4 + wave : (int64_t)list_index();
-  const int row_at = (int)(at / Hq), head = (int)(at - (int64_t)row_at * Hq);
-  const int r = row_at / p.b.max_rows, i = row_at - r * p.b.max_rows;
+  const uint32_t at = NW == 1 ? (uint32_t)list_index() * 4u + (uint32_t)wave : (uint32_t)list_index();  // < kPagedMaxJoins and a slice
+  const int row_at = (int)(at / (uint32_t)Hq), head = (int)(at - (uint32_t)row_at * (uint32_t)Hq);
+  const int r = (int)((uint32_t)row_at / (uint32_t)p.b.max_rows), i = row_at - r * p.b.max_rows;
   if (r >= p.b.n_req) return;  // (the same in the whole workgroup where it has a barrier)
-  const int h = head / p.group, unit_row = i * p.group + head - h * p.group, qg = unit_row / (16 * NT), in_unit = unit_row - qg * 16 * NT;
-  const int2 whose = p.whose[((int64_t)r * p.H + h) * p.most_groups + qg];
+  const int h = (int)((uint32_t)head / (uint32_t)p.group), unit_row = i * p.group + head - h * p.group, qg = unit_row / (16 * NT), in_unit = unit_row - qg * 16 * NT;
+  const int32_t* whose = reinterpret_cast<const int32_t*>(p.whose + ((int64_t)r * p.H + h) * p.most_groups + qg);
+  const int w0 = uniform_load(whose), n = uniform_load(whose + 1);
   const RequestRows q = request_rows(p.b, r);
   if (i >= q.n) return;  // (nor has anybody written `whose`)
-  const int w0 = __builtin_amdgcn_readfirstlane(whose.x), n = __builtin_amdgcn_readfirstlane(whose.y);
   if (n == 0) return;
   const int in_bundle = h & ((1 << p.log_bundle) - 1);
   // Wavefront w takes the pieces w, w + NW, ..., kAhead of them at a time: their statistics, lane by lane, and their rows, all requested at once.
