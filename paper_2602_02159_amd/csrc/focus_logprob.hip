@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256, 6) void logprob_part_kernel(const LogprobArgs 
 #pragma unroll
       for (int e = 0; e < E; ++e) {
         const float x = sizeof(T) == 4 ? __uint_as_float(u[e & 3]) : ((e & 1) ? bf16_hi(u[(e >> 1) & 3]) : bf16_lo(u[(e >> 1) & 3]));
-        z[k * E + e] = in ? tame(x) : -INFINITY;
+        z[k * E + e] = in ? x : -INFINITY;  // as it is: see below
       }
     }
     if (part == (int)gridDim.x - 1) {  // a row's last, shorter piece, logit by logit
@@ -184,20 +184,44 @@ __global__ __launch_bounds__(256, 6) void logprob_part_kernel(const LogprobArgs 
       }
     }
   }
+  // A NaN needs no care: the largest of it and a number is the number, its weight that of kNothing, and no comparison takes it.  (v_med3_f32 with
+  // an infinity is a maximum that asks for no other form of its operands.)  +inf is made the largest number where a part has one.
   float mine = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < kLogitsThread; ++i) mine = fmaxf(mine, z[i]);
-  const float m = block_max4(mine, max_sh), m_use = m == -INFINITY ? 0.f : m;
+  for (int i = 0; i < kLogitsThread; ++i) mine = __builtin_amdgcn_fmed3f(mine, z[i], INFINITY);
+  float m = block_max4(mine, max_sh);
+  if (m == INFINITY) {  // whole workgroup
+#pragma unroll
+    for (int i = 0; i < kLogitsThread; ++i) z[i] = tame(z[i]);
+    mine = tame(mine);
+    m = tame(m);
+  }
+  const float m_use = m == -INFINITY ? 0.f : m;
 
   float rest = 0.f, A = 0.f;  // of the logits below m;
   int equal = 0;              // how many equal it
+  auto weight = [&](float x, float& y) __attribute__((always_inline)) {
+    y = __builtin_amdgcn_fmed3f((x - m_use) * kLog2eF, kNothing, INFINITY);
+    return __builtin_amdgcn_exp2f(y);
+  };
+  if (__ballot(mine == m) != 0ull) {
 #pragma unroll
-  for (int i = 0; i < kLogitsThread; ++i) {
-    const float y = fmaxf((z[i] - m_use) * kLog2eF, kNothing), e = __builtin_amdgcn_exp2f(y);
-    A = __builtin_fmaf(e, y, A);
-    const bool top = z[i] == m;
-    rest += top ? 0.f : e;
-    equal += top ? 1 : 0;
+    for (int i = 0; i < kLogitsThread; ++i) {
+      float y;
+      const float e = weight(z[i], y);
+      A = __builtin_fmaf(e, y, A);
+      const bool top = z[i] == m;
+      rest += top ? 0.f : e;
+      equal += top ? 1 : 0;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kLogitsThread; ++i) {
+      float y;
+      const float e = weight(z[i], y);
+      A = __builtin_fmaf(e, y, A);
+      rest += e;
+    }
   }
   rest = wave_sum_fast(rest);
   A = wave_sum_fast(A);
@@ -209,7 +233,7 @@ __global__ __launch_bounds__(256, 6) void logprob_part_kernel(const LogprobArgs 
     if (__ballot(best >= threshold) != 0ull) {  // few wavefronts
       const float least = threshold < 0x00800000u ? -3.4028234663852886e38f : order_value(threshold);  // (0x00800000: the lowest number's key)
 #pragma unroll
-      for (int i = 0; i < kLogitsThread; ++i) some |= z[i] >= least && z[i] > -INFINITY ? 1u << i : 0u;
+      for (int i = 0; i < kLogitsThread; ++i) some |= z[i] >= least ? 1u << i : 0u;
       if (best < threshold) some = 0u;
       while (some != 0u) {  // one or two, which come from the cache
         const int id = id_at(__builtin_ctz(some));
