@@ -484,6 +484,7 @@ typedef struct focus_paged_batch {
  *                of it); both NULL with n_q_heads = 0
  * A row without a position (positions[i] < 0) is left out, Q included; of one whose cache row does not exist K and V are left out.  Of rows of
  * one request with the same position the last one's K and V stay.  A page that is listed more than once must not be written through two entries.
+ * A cache whose heads or pages share rows (strides of 0, v = k) can be read by focus_paged_attn, not written.
  * ceil(max_rows / 4) * n_req <= 2^25: max_rows is a bound that the launch is made for.
  */
 int focus_paged_append(const focus_paged_cache* cache, const focus_paged_batch* batch, const void* K_new, const void* V_new, int64_t new_stride_h,

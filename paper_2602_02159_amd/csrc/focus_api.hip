@@ -1145,6 +1145,10 @@ int focus_paged_append(const focus_paged_cache* cache, const focus_paged_batch* 
   }
   if (ceil_div64(std::min(batch->max_rows, batch->n_rows), 4) * batch->n_req > kTurnMaxRows)
     return fail(FOCUS_EUNSUPPORTED, "%s: n_req=%d requests of up to max_rows=%d rows are too many", who, batch->n_req, batch->max_rows);
+  const bool heads = cache->n_heads > 1, pages = cache->n_pages > 1;
+  if (cache->k == cache->v || (heads && (cache->k_stride_h == 0 || cache->v_stride_h == 0)) || (pages && (cache->k_stride_p == 0 || cache->v_stride_p == 0)) ||
+      (cache->k_exp && (cache->k_exp == cache->v_exp || (heads && cache->exp_stride_h == 0) || (pages && cache->exp_stride_p == 0))))
+    return fail(FOCUS_EINVAL, "%s: rows of the cache lie on one another", who);
   TurnRows p = {};
   p.Q = static_cast<const uint16_t*>(Q);
   p.Qo = static_cast<uint16_t*>(Q_out);

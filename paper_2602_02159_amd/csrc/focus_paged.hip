@@ -36,7 +36,7 @@ __device__ __forceinline__ Request make_request(const PagedAttn& p, const Reques
   x.n = q.n;
   x.count = q.count;
   x.len = (int)min((int64_t)max(len, 0), (int64_t)p.b.table_width * p.page);
-  x.tiles = max((x.len + kTile - 1) / kTile, 1);
+  x.tiles = max((int)(((uint32_t)x.len + kTile - 1) / kTile), 1);  // (len up to 2^31 - 1)
   x.groups = (x.n * p.group + 16 * NT - 1) / (16 * NT);
   return x;
 }

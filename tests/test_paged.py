@@ -175,6 +175,16 @@ def test_paged_calls_refused():
     assert append(q=P, qo=P, heads=0) == append(q=P, qo=P, heads=4, qoh=128) == append(q=P, qo=P, heads=4, qoh=0) == fb.FOCUS_EINVAL
 
 
+@pytest.mark.parametrize("cache", [
+    dict(), dict(v=1 << 24, k_stride_h=0), dict(v=1 << 24, v_stride_h=0), dict(v=1 << 24, k_stride_p=0), dict(v=1 << 24, v_stride_p=0),
+    dict(v=1 << 24, k_exp=1 << 25, v_exp=1 << 25, exp_stride_p=64, exp_stride_h=16, exp_stride_n=1), dict(v=1 << 24, k_exp=1 << 25, v_exp=1 << 26, exp_stride_p=64, exp_stride_n=1),
+    dict(v=1 << 24, k_exp=1 << 25, v_exp=1 << 26, exp_stride_h=16, exp_stride_n=1)])
+def test_shared_rows_are_not_written(cache):
+    L, c, b = fb.lib(), _cache(**cache), _batch()
+    assert L.focus_paged_append(C.byref(c), C.byref(b), P, P, 64, 256, None, None, 0, 0, None, 0, 0, 0, None) == fb.FOCUS_EINVAL
+    assert "on one another" in fb.last_error()
+
+
 def test_frequencies():
     f = fb.rotary_freqs(10000.0, 64)
     assert torch.allclose(f, 10000.0 ** (-torch.arange(0, 64, 2, dtype=torch.float64) / 64), rtol=1e-14)
@@ -548,6 +558,25 @@ def test_attention_of_far_pages():
         m = rows.stop - rows.start
         for h in range(8):
             check_attention(out[rows, h], lse[rows, h], attend64(q[rows, h], new_k[rows, h // 2], new_v[rows, h // 2], torch.ones((m, m)).tril().bool()))
+
+
+@pytest.mark.gpu
+def test_the_longest_table():
+    """Two pages short of 2^31 - 1 rows, of which the first and the last exist: the last tile of 32 keys ends behind the last 32-bit number."""
+    page, width = 42966, 49981
+    assert page * width == 2 ** 31 - 2
+    g = torch.Generator().manual_seed(11)
+    k, v = (torch.randn((2, 1, page, 64), generator=g).bfloat16().to(DEV) for _ in range(2))
+    q = torch.randn((1, 2, 64), generator=g).bfloat16().to(DEV)
+    cache = fb.make_paged_cache(k, v)
+    table = torch.full((1, width), -1, dtype=torch.int32, device=DEV)
+    table[0, 0], table[0, -1] = 0, 1
+    batch = fb.make_paged_batch(torch.tensor([2 ** 31 - 1], dtype=torch.int32, device=DEV), table)
+    out, lse = torch.empty_like(q), torch.empty((1, 2), device=DEV)
+    fb.paged_attn(q, cache, batch, False, out, lse, workspace(cache, batch, 2))
+    keys, vals = (t.cpu().double().reshape(2 * page, 64) for t in (k, v))
+    for h in range(2):
+        check_attention(out.cpu()[:, h], lse.cpu()[:, h], attend64(q.cpu().double()[:, h], keys, vals, torch.ones((1, 2 * page), dtype=torch.bool)))
 
 
 @pytest.mark.gpu
