@@ -388,6 +388,7 @@ class FocusPagedStep:
       with vocab: logits bf16 [n_rows, vocab], targets int32 [n_rows], masked u8 [n_rows]
 
     run():    per layer  focus_paged_append, focus_paged_attn -> out[l] bf16 [n_rows, n_q_heads, d], lse[l] [n_rows, n_q_heads]
+              (a row without a position leaves its row of q_turned as the layer before it left it: its out and lse say nothing)
     score():  focus_token_logprobs -> logprob, entropy [n_rows], top_ids, top_logprobs [n_rows, top_n]
     issue(l) enqueues the calls of one layer, for a model whose projections lie between them.
     `rotation`: from make_rotation, or None.  `quantised`: pages of eight-bit rows.  The pages of layer l are caches[l]; all layers share the table.
@@ -408,6 +409,8 @@ class FocusPagedStep:
         rows = u8 if quantised else bf16
         self.k_pages, self.v_pages = ([zeros(rows, n_pages, H, page, d) for _ in range(n_layers)] for _ in range(2))
         self.k_exp, self.v_exp = ([zeros(u8, n_pages, H, page) if quantised else None for _ in range(n_layers)] for _ in range(2))
+        if rotation is not None and rotation.device not in (None, self.seq_len.get_device()):
+            raise ValueError(f"rotation on device {rotation.device}, but the step is on {self.seq_len.device}")
         self.caches = [fb.make_paged_cache(*t) for t in zip(self.k_pages, self.v_pages, self.k_exp, self.v_exp)]
         self.batch = fb.make_paged_batch(self.seq_len, self.page_table, self.row_start, max_rows, n_rows, self.positions)
         self.q, self.out = ([zeros(bf16, n_rows, Hq, d) for _ in range(n_layers)] for _ in range(2))

@@ -113,3 +113,10 @@ def test_active_positions_of_a_block(quantised):
 def test_sizes_are_refused():
     with pytest.raises((fb.FocusError, ValueError, RuntimeError, AssertionError, TypeError)):
         FocusPagedStep(1, 4, 16, 2, 4, 80, 2, 2, "cpu")
+
+
+def test_a_rotation_of_another_device_is_refused():
+    rotation = fb.Rotation(1 << 20, 64, 0, 1.0)
+    rotation.device = 1
+    with pytest.raises(ValueError, match="rotation on device 1"):
+        FocusPagedStep(1, 4, 16, 2, 4, 64, 2, 2, "cpu", rotation=rotation)
