@@ -16,7 +16,7 @@
 namespace focus {
 
 constexpr int kLogitsThread = 32, kLogitsPart = 256 * kLogitsThread;
-constexpr int kTopCandidates = 512;
+constexpr int kTopCandidates = 1024, kTopFours = 1024;
 
 // NaN as -inf, +inf as the largest number
 __device__ __forceinline__ float tame(float x) { return fminf(fmaxf(x, -INFINITY), 3.4028234663852886e38f); }
@@ -32,7 +32,7 @@ struct LogprobArgs {
   int32_t* top_ids;
   float* top_logprobs;
   float4* part;     // [n_rows, n_parts] (m, r, A in units of log 2, -)
-  uint2* part_top;  // [n_rows, n_parts, top_n] (key, id), key 0: none
+  float* part_top;  // [n_rows, n_parts, 64] the largest logit of each four threads, -inf: none
   int64_t row_stride;
   int vocab, n_parts, top_n;
 };
@@ -45,16 +45,18 @@ __device__ __forceinline__ float logit(const T* row, int id) {
 
 // over the wavefront, in a fixed order; every lane receives the result
 __device__ __forceinline__ float wave_sum_fast(float x) { return group_sum(row_sum16(x)); }
-__device__ __forceinline__ float wave_max_fast(float x) {
+__device__ __forceinline__ float four_max(float x) {  // of four threads
   x = fmaxf(x, lane_dpp<0xB1>(x));
-  x = fmaxf(x, lane_dpp<0x4E>(x));
+  return fmaxf(x, lane_dpp<0x4E>(x));
+}
+__device__ __forceinline__ float wave_max_fours(float x) {
   x = fmaxf(x, lane_dpp<0x141>(x));
   x = fmaxf(x, lane_dpp<0x140>(x));
   return group_max(x);
 }
 // over the workgroup of four wavefronts; `sh` of four entries
 __device__ __forceinline__ float block_max4(float x, float* sh) {
-  x = wave_max_fast(x);
+  x = wave_max_fours(four_max(x));
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = x;
   __syncthreads();
   return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
@@ -63,20 +65,21 @@ __device__ __forceinline__ float block_max4(float x, float* sh) {
 struct TopShared256 {
   uint32_t best[64];
   unsigned long long list[kTopCandidates];
-  uint32_t count, threshold;
-  unsigned long long wave_best[4];
+  unsigned long long kept[kLogprobTop];
+  int fours[kTopFours];
+  uint32_t count, n_fours, threshold;
 };
 // (key, id) as one number: larger = earlier in the order, the lower id first
 __device__ __forceinline__ unsigned long long place_of(uint32_t key, int id) { return ((unsigned long long)key << 32) | (uint32_t)~id; }
 
 // A number that at least top_n entries reach, to sixteen bits: the top_n-th largest of the best of each four threads (1 where fewer have one).  64 of
-// them are one a lane, and the search one ballot a bit: with the best of every thread, four a lane, a part took 8.0 us and not 6.9.
+// them are one a lane, and the search one ballot a bit.
 __device__ __forceinline__ uint32_t top_threshold(TopShared256& sm, uint32_t best, int top_n) {
   const int tid = threadIdx.x;
   best = max(best, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)best, 0xB1, 0xF, 0xF, false));  // quad_perm [1,0,3,2]
   best = max(best, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)best, 0x4E, 0xF, 0xF, false));  // quad_perm [2,3,0,1]
   if ((tid & 3) == 0) sm.best[tid >> 2] = best;
-  if (tid == 0) sm.count = 0u;
+  if (tid == 0) sm.count = sm.n_fours = 0u;
   __syncthreads();
   if (tid < kWave) {
     const uint32_t k = sm.best[tid] >> 16;
@@ -97,46 +100,48 @@ __device__ __forceinline__ void list_candidate(TopShared256& sm, uint32_t key, i
   const uint32_t at = atomicAdd(&sm.count, 1u);  // (the list's order does not matter)
   if (at < (uint32_t)kTopCandidates) sm.list[at] = place_of(key, id);
 }
-// The top_n first of the listed candidates, in order, found by comparing each with all; emit(rank, key, id) is called once for every rank.  Where more than
-// the list holds came (equal logits), one is found after the other among the n_each entries that every thread has: key_at(i) (0: none), id_at(i).
-template <class Key, class Id, class Emit>
-__device__ __forceinline__ void emit_top(TopShared256& sm, int top_n, int n_each, const Key key_at, const Id id_at, const Emit emit) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  __syncthreads();
-  const int n = (int)sm.count;
-  if (n <= kTopCandidates) {
-    for (int i = tid; i < n; i += 256) {
-      const unsigned long long mine = sm.list[i];
-      int rank = 0;
+// The first top_n of the n listed candidates, found by comparing each with all: emit(rank, key, id)
+template <class Emit>
+__device__ __forceinline__ void rank_candidates(const TopShared256& sm, int n, int top_n, const Emit emit) {
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const unsigned long long mine = sm.list[i];
+    int rank = 0;
 #pragma unroll 8
-      for (int j = 0; j < n; ++j) rank += sm.list[j] > mine ? 1 : 0;
-      if (rank < top_n) emit(rank, (uint32_t)(mine >> 32), (int)~(uint32_t)mine);
-    }
-    for (int i = n + tid; i < top_n; i += 256) emit(i, 0u, -1);
-    return;
+    for (int j = 0; j < n; ++j) rank += sm.list[j] > mine ? 1 : 0;
+    if (rank < top_n) emit(rank, (uint32_t)(mine >> 32), (int)~(uint32_t)mine);
   }
-  unsigned long long last = ~0ull;
+}
+// More candidates than the list holds (equal logits): the row from its first id on.  Where the list fills up, its first top_n stay, and from there on only
+// larger logits come in, as equal ones have higher ids.  key_at(id): 0 for none
+template <class Key>
+__device__ __forceinline__ void list_in_turn(TopShared256& sm, uint32_t bound, int vocab, int top_n, const Key key_at) {
+  constexpr int U = 8;
+  const int tid = threadIdx.x;
+  __syncthreads();
+  if (tid == 0) sm.count = 0u;
+  __syncthreads();
 #pragma unroll 1
-  for (int k = 0; k < top_n; ++k) {
-    unsigned long long mine = 0ull;
-#pragma unroll 1
-    for (int i = 0; i < n_each; ++i) {
-      const uint32_t key = key_at(i);
-      const unsigned long long x = key == 0u ? 0ull : place_of(key, id_at(i));
-      if (x < last && x > mine) mine = x;
-    }
+  for (int base = 0; base < vocab; base += U * 256) {
+    uint32_t key[U], any = 0u;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const unsigned long long y = __shfl_xor(mine, o, kWave);
-      mine = y > mine ? y : mine;
-    }
-    __syncthreads();  // (wave_best is read in the turn before)
-    if (lane == 0) sm.wave_best[wave] = mine;
-    __syncthreads();
+    for (int u = 0; u < U; ++u) key[u] = base + u * 256 + tid < vocab ? key_at(base + u * 256 + tid) : 0u;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) mine = sm.wave_best[w] > mine ? sm.wave_best[w] : mine;
-    last = mine;
-    if (tid == 0) emit(k, (uint32_t)(mine >> 32), mine == 0ull ? -1 : (int)~(uint32_t)mine);
+    for (int u = 0; u < U; ++u) any |= key[u] >= bound ? 1u : 0u;
+    if (__syncthreads_or((int)any) == 0) continue;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (key[u] >= bound) list_candidate(sm, key[u], base + u * 256 + tid);
+      __syncthreads();
+      const int n = (int)sm.count;
+      if (n > kTopCandidates - 256) {  // whole workgroup
+        rank_candidates(sm, n, top_n, [&](int rank, uint32_t k, int id) { sm.kept[rank] = place_of(k, id); });
+        __syncthreads();
+        if (tid < top_n) sm.list[tid] = sm.kept[tid];
+        if (tid == 0) sm.count = (uint32_t)top_n;
+        bound = (uint32_t)(sm.kept[top_n - 1] >> 32) + 1u;
+      }
+      __syncthreads();
+    }
   }
 }
 
@@ -148,11 +153,9 @@ __global__ __launch_bounds__(256, 6) void logprob_part_kernel(const LogprobArgs 
   constexpr int E = 16 / sizeof(T), V = kLogitsThread / E;  // logits a load, loads
   __shared__ float max_sh[4];
   __shared__ float4 sum_sh[4];
-  __shared__ TopShared256 top_sh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.y, part = blockIdx.x;
   const T* z_row = static_cast<const T*>(p.logits) + (int64_t)row * p.row_stride;
   const int first = part * kLogitsPart + tid * E;
-  auto id_at = [&](int i) __attribute__((always_inline)) { return first + (i / E) * (256 * E) + i % E; };
   float z[kLogitsThread];
   {
     uint4 w[V];
@@ -189,7 +192,9 @@ __global__ __launch_bounds__(256, 6) void logprob_part_kernel(const LogprobArgs 
   float mine = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kLogitsThread; ++i) mine = __builtin_amdgcn_fmed3f(mine, z[i], INFINITY);
-  float m = block_max4(mine, max_sh);
+  const float best = four_max(mine);
+  if (p.top_n > 0 && (tid & 3) == 0) p.part_top[((int64_t)row * p.n_parts + part) * 64 + (tid >> 2)] = tame(best);
+  float m = block_max4(best, max_sh);
   if (m == INFINITY) {  // whole workgroup
 #pragma unroll
     for (int i = 0; i < kLogitsThread; ++i) z[i] = tame(z[i]);
@@ -227,27 +232,7 @@ __global__ __launch_bounds__(256, 6) void logprob_part_kernel(const LogprobArgs 
   A = wave_sum_fast(A);
   const float n_equal = wave_sum_fast((float)equal);
   if (lane == 0) sum_sh[wave] = make_float4(rest, A, n_equal, 0.f);
-  if (p.top_n > 0) {
-    const uint32_t best = top_key(mine), threshold = top_threshold(top_sh, best, p.top_n);
-    uint32_t some = 0u;
-    if (__ballot(best >= threshold) != 0ull) {  // few wavefronts
-      const float least = threshold < 0x00800000u ? -3.4028234663852886e38f : order_value(threshold);  // (0x00800000: the lowest number's key)
-#pragma unroll
-      for (int i = 0; i < kLogitsThread; ++i) some |= z[i] >= least ? 1u << i : 0u;
-      if (best < threshold) some = 0u;
-      while (some != 0u) {  // one or two, which come from the cache
-        const int id = id_at(__builtin_ctz(some));
-        some &= some - 1u;
-        list_candidate(top_sh, top_key(logit(z_row, id)), id);
-      }
-    }
-    uint2* list = p.part_top + ((int64_t)row * p.n_parts + part) * p.top_n;
-    emit_top(
-        top_sh, p.top_n, kLogitsThread, [&](int i) { return id_at(i) < p.vocab ? top_key(logit(z_row, id_at(i))) : 0u; }, id_at,
-        [&](int rank, uint32_t key, int id) { list[rank] = make_uint2(key, (uint32_t)id); });
-  } else {
-    __syncthreads();
-  }
+  __syncthreads();
   if (tid == 0) {
     float r = 0.f, a = 0.f, n = 0.f;
 #pragma unroll
@@ -262,6 +247,7 @@ __global__ __launch_bounds__(256, 6) void logprob_part_kernel(const LogprobArgs 
 
 template <class T>
 __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) {
+  constexpr int kFours = 4;
   __shared__ float max_sh[4];
   __shared__ float2 sum_sh[4];
   __shared__ TopShared256 top_sh;
@@ -288,11 +274,11 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
   }
   float4 s = make_float4(-INFINITY, 0.f, 0.f, 0.f);  // at most 256 parts: one a thread
   if (tid < p.n_parts) s = p.part[(int64_t)row * p.n_parts + tid];
-  const uint2* list = p.part_top + (int64_t)row * p.n_parts * p.top_n;
-  const int n = p.n_parts * p.top_n;  // at most 256 * 32
-  uint2 mine[2];
+  const float* tops = p.part_top + (int64_t)row * p.n_parts * 64;
+  const int n = p.top_n > 0 ? p.n_parts * 64 : 0;
+  float top_of[kFours];  // those of the first 16 parts, here before the statistics are
 #pragma unroll
-  for (int i = 0; i < 2; ++i) mine[i] = tid + 256 * i < n ? list[tid + 256 * i] : make_uint2(0u, 0u);
+  for (int i = 0; i < kFours; ++i) top_of[i] = tid + 256 * i < n ? tops[tid + 256 * i] : -INFINITY;
   const float m = block_max4(s.x, max_sh), m_use = m == -INFINITY ? 0.f : m;
   // Of the parts whose largest logit is the row's the first one's is left out of r
   const unsigned long long top = __ballot(s.x == m && m != -INFINITY);
@@ -317,29 +303,61 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
     if (p.entropy) p.entropy[row] = m == -INFINITY ? 0.f : log_sum - kLn2F * a / (1.f + r);
   }
   if (p.top_n == 0) return;
-  // (the first two entries of a thread are here since before the statistics)
-  const int n_each = (n + 255) / 256;
-  uint32_t best = max(mine[0].x, mine[1].x);
-  for (int i = tid + 512; i < n; i += 256) best = max(best, list[i].x);
+  // The threads that had a candidate, four by four, then their logits once more
+  uint32_t best = 0u;
+#pragma unroll
+  for (int i = 0; i < kFours; ++i) best = max(best, top_key(top_of[i]));
+  for (int i = tid + 256 * kFours; i < n; i += 256) best = max(best, top_key(tops[i]));
   const uint32_t threshold = top_threshold(top_sh, best, p.top_n);
   if (best >= threshold) {
-    for (int i = 0; i < n_each; ++i) {
-      const uint2 x = i < 2 ? mine[i] : (tid + 256 * i < n ? list[tid + 256 * i] : make_uint2(0u, 0u));
-      if (x.x >= threshold) list_candidate(top_sh, x.x, (int)x.y);
+    auto take = [&](float x, int i) __attribute__((always_inline)) {
+      if (top_key(x) < threshold) return;
+      const uint32_t at = atomicAdd(&top_sh.n_fours, 1u);
+      if (at < (uint32_t)kTopFours) top_sh.fours[at] = i;
+    };
+#pragma unroll
+    for (int i = 0; i < kFours; ++i) take(top_of[i], tid + 256 * i);
+    for (int i = tid + 256 * kFours; i < n; i += 256) take(tops[i], i);
+  }
+  __syncthreads();
+  constexpr int E = 16 / sizeof(T), V = kLogitsThread / E;
+  const T* z_row = static_cast<const T*>(p.logits) + (int64_t)row * p.row_stride;
+  const int n_fours = (int)top_sh.n_fours, n_loads = n_fours <= kTopFours ? n_fours * 4 * V : 0;
+  for (int i = tid; i < n_loads; i += 256) {
+    const int four = top_sh.fours[i / (4 * V)], k = i % (4 * V) / 4;
+    const int id = (four / 64) * kLogitsPart + k * (256 * E) + ((four % 64) * 4 + i % 4) * E;
+    if (id + E <= p.vocab) {
+      const uint4 w = *reinterpret_cast<const uint4*>(z_row + id);
+      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const uint32_t key = top_key(tame(sizeof(T) == 4 ? __uint_as_float(u[e & 3]) : ((e & 1) ? bf16_hi(u[(e >> 1) & 3]) : bf16_lo(u[(e >> 1) & 3]))));
+        if (key >= threshold) list_candidate(top_sh, key, id + e);
+      }
+    } else {
+      for (int e = id; e < p.vocab; ++e) {
+        const uint32_t key = top_key(logit(z_row, e));
+        if (key >= threshold) list_candidate(top_sh, key, e);
+      }
     }
   }
-  emit_top(
-      top_sh, p.top_n, n_each, [&](int i) { return tid + 256 * i < n ? list[tid + 256 * i].x : 0u; }, [&](int i) { return (int)list[tid + 256 * i].y; },
-      [&](int rank, uint32_t key, int id) {
-        p.top_ids[(int64_t)row * p.top_n + rank] = id;
-        p.top_logprobs[(int64_t)row * p.top_n + rank] = id < 0 ? -INFINITY : (order_value(key) - m) - log_sum;
-      });
+  __syncthreads();
+  if (n_fours > kTopFours || top_sh.count > (uint32_t)kTopCandidates)  // whole workgroup
+    list_in_turn(top_sh, threshold, p.vocab, p.top_n, [&](int id) __attribute__((always_inline)) { return top_key(logit(z_row, id)); });
+  __syncthreads();
+  auto emit = [&](int rank, uint32_t key, int id) __attribute__((always_inline)) {
+    p.top_ids[(int64_t)row * p.top_n + rank] = id;
+    p.top_logprobs[(int64_t)row * p.top_n + rank] = id < 0 ? -INFINITY : (order_value(key) - m) - log_sum;
+  };
+  const int listed = (int)top_sh.count;
+  rank_candidates(top_sh, listed, p.top_n, emit);
+  for (int i = listed + tid; i < p.top_n; i += 256) emit(i, 0u, -1);
 }
 
 static size_t logprob_parts_bytes(int n_rows, int n_parts) { return (size_t)n_rows * n_parts * sizeof(float4); }
 size_t token_logprobs_workspace(int n_rows, int vocab, int top_n) {
   const int n_parts = ceil_div(vocab, kLogitsPart);
-  return logprob_parts_bytes(n_rows, n_parts) + (size_t)n_rows * n_parts * top_n * sizeof(uint2);
+  return logprob_parts_bytes(n_rows, n_parts) + (top_n > 0 ? (size_t)n_rows * n_parts * 64 * sizeof(float) : 0);
 }
 
 template <class T>
@@ -363,7 +381,7 @@ hipError_t launch_token_logprobs(const void* logits, int dtype, int64_t row_stri
   p.n_parts = ceil_div(vocab, kLogitsPart);
   p.top_n = top_n;
   p.part = static_cast<float4*>(workspace);
-  p.part_top = reinterpret_cast<uint2*>(static_cast<char*>(workspace) + logprob_parts_bytes(n_rows, p.n_parts));
+  p.part_top = reinterpret_cast<float*>(static_cast<char*>(workspace) + logprob_parts_bytes(n_rows, p.n_parts));
   return dtype == FOCUS_F32 ? launch_logprobs_t<float>(p, n_rows, st) : launch_logprobs_t<uint16_t>(p, n_rows, st);
 }
 
