@@ -5,8 +5,15 @@
 //   log sum exp(z) = m + log1p(r)        log p_t = z_t - m - log1p(r)        entropy = log1p(r) - A / (1 + r)
 // Leaving the largest out of the sum keeps the digits of rows that are all but certain: 1 + r would round them away.
 //
-//   logprob_part_kernel  a workgroup has 8192 logits of a row, 32 a thread, in registers: their largest, r and A, and their likeliest tokens
-//   logprob_join_kernel  a workgroup a row: the parts together
+//   logprob_part_kernel  a workgroup has 8192 logits of a row, 32 a thread, in registers: their largest, r and A, and the largest of each four threads
+//   logprob_join_kernel  a workgroup a row: the parts together; the likeliest tokens
+// The likeliest: 64 numbers of a part, each the largest of 128 logits, are all that the first launch writes.  A number that top_n of all of them reach is
+// reached by top_n logits, and what reaches it lies in some 1.2 top_n of those 128s, which the second launch reads once more.  (Each part with a list of its own
+// likeliest: 500 rows of 126 464, 20 alternatives 43.4 us instead of 33.2.)
+// Every logit is read once.  What bounds it: many rows, HBM and the exponentials: 500 x 126 464 bf16, 126 MB, in 24.6 us = 5.1 TB/s
+// and 8.9 us for the rows' ends; 511 x 32 003 fp32 in 14.4 + 6.6.  One row (3.5 + 6.0 us): the chain of round trips in two launches that depend on each other.
+// Not better: parts of 2048 for few rows (one row 14.5 us instead of 14.0 at that time), 16 logits a thread (50 instead of 43), 24 (42.4 instead of 43.3, but
+// more parts than one a thread).
 #include <type_traits>
 
 #include "focus_common.h"
@@ -16,7 +23,9 @@
 namespace focus {
 
 constexpr int kLogitsThread = 32, kLogitsPart = 256 * kLogitsThread;
-constexpr int kTopCandidates = 1024, kTopFours = 1024;
+// candidates and fours that are listed at most (more: list_in_turn); up to 96 candidates are compared each with all (5 x 1000 logits, of which all are: 65 us
+// that way, 16 this)
+constexpr int kTopCandidates = 1024, kTopFours = 1024, kTopRanked = 96;
 
 // NaN as -inf, +inf as the largest number
 __device__ __forceinline__ float tame(float x) { return fminf(fmaxf(x, -INFINITY), 3.4028234663852886e38f); }
@@ -67,7 +76,7 @@ struct TopShared256 {
   unsigned long long list[kTopCandidates];
   unsigned long long kept[kLogprobTop];
   int fours[kTopFours];
-  uint32_t count, n_fours, threshold;
+  uint32_t count, n_fours;
 };
 // (key, id) as one number: larger = earlier in the order, the lower id first
 __device__ __forceinline__ unsigned long long place_of(uint32_t key, int id) { return ((unsigned long long)key << 32) | (uint32_t)~id; }
@@ -81,34 +90,36 @@ __device__ __forceinline__ uint32_t top_threshold(TopShared256& sm, uint32_t bes
   if ((tid & 3) == 0) sm.best[tid >> 2] = best;
   if (tid == 0) sm.count = sm.n_fours = 0u;
   __syncthreads();
-  if (tid < kWave) {
-    const uint32_t k = sm.best[tid] >> 16;
-    uint32_t t = 0u;
+  const uint32_t k = sm.best[tid & 63] >> 16;  // every wavefront searches for itself
+  uint32_t t = 0u;
 #pragma unroll 1
-    for (int bit = 15; bit >= 0; --bit) {
-      const uint32_t with = t | (1u << bit);
-      const int n = __popcll(__ballot(k >= with));
-      t = n >= top_n ? with : t;
-      if (n == top_n) break;  // exactly these
-    }
-    if (tid == 0) sm.threshold = max(t << 16, 1u);
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t with = t | (1u << bit);
+    const int n = __popcll(__ballot(k >= with));
+    t = n >= top_n ? with : t;
+    if (n == top_n) break;  // exactly these
   }
-  __syncthreads();
-  return sm.threshold;
+  return max(t << 16, 1u);
 }
 __device__ __forceinline__ void list_candidate(TopShared256& sm, uint32_t key, int id) {
   const uint32_t at = atomicAdd(&sm.count, 1u);  // (the list's order does not matter)
   if (at < (uint32_t)kTopCandidates) sm.list[at] = place_of(key, id);
 }
-// The first top_n of the n listed candidates, found by comparing each with all: emit(rank, key, id)
+// The first top_n of the n listed candidates, found by comparing each with all, four threads a candidate: emit(rank, key, id)
 template <class Emit>
 __device__ __forceinline__ void rank_candidates(const TopShared256& sm, int n, int top_n, const Emit emit) {
-  for (int i = threadIdx.x; i < n; i += 256) {
+  const int part = threadIdx.x & 3;
+  for (int i = threadIdx.x >> 2; i < n; i += 64) {
     const unsigned long long mine = sm.list[i];
-    int rank = 0;
-#pragma unroll 8
-    for (int j = 0; j < n; ++j) rank += sm.list[j] > mine ? 1 : 0;
-    if (rank < top_n) emit(rank, (uint32_t)(mine >> 32), (int)~(uint32_t)mine);
+    uint32_t rank = 0u;
+#pragma unroll 1
+    for (int j0 = part; j0 < n; j0 += 32) {
+#pragma unroll
+      for (int j = 0; j < 32; j += 4) rank += j0 + j < n && sm.list[min(j0 + j, kTopCandidates - 1)] > mine ? 1u : 0u;
+    }
+    rank += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)rank, 0xB1, 0xF, 0xF, false);
+    rank += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)rank, 0x4E, 0xF, 0xF, false);
+    if (part == 0 && (int)rank < top_n) emit((int)rank, (uint32_t)(mine >> 32), (int)~(uint32_t)mine);
   }
 }
 // More candidates than the list holds (equal logits): the row from its first id on.  Where the list fills up, its first top_n stay, and from there on only
@@ -247,7 +258,8 @@ __global__ __launch_bounds__(256, 6) void logprob_part_kernel(const LogprobArgs 
 
 template <class T>
 __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) {
-  constexpr int kFours = 4;
+  constexpr int E = 16 / sizeof(T), V = kLogitsThread / E;
+  constexpr int kFours = 4, kLoads = V / 2;  // (a logit of 32 bits has twice the loads)
   __shared__ float max_sh[4];
   __shared__ float2 sum_sh[4];
   __shared__ TopShared256 top_sh;
@@ -320,25 +332,41 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
     for (int i = tid + 256 * kFours; i < n; i += 256) take(tops[i], i);
   }
   __syncthreads();
-  constexpr int E = 16 / sizeof(T), V = kLogitsThread / E;
   const T* z_row = static_cast<const T*>(p.logits) + (int64_t)row * p.row_stride;
   const int n_fours = (int)top_sh.n_fours, n_loads = n_fours <= kTopFours ? n_fours * 4 * V : 0;
-  for (int i = tid; i < n_loads; i += 256) {
+  const float least = threshold < 0x00800000u ? -3.4028234663852886e38f : order_value(threshold);  // (0x00800000: the lowest number's key)
+  auto id_of = [&](int i) __attribute__((always_inline)) {
     const int four = top_sh.fours[i / (4 * V)], k = i % (4 * V) / 4;
-    const int id = (four / 64) * kLogitsPart + k * (256 * E) + ((four % 64) * 4 + i % 4) * E;
-    if (id + E <= p.vocab) {
-      const uint4 w = *reinterpret_cast<const uint4*>(z_row + id);
-      const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    return (four / 64) * kLogitsPart + k * (256 * E) + ((four % 64) * 4 + i % 4) * E;
+  };
+#pragma unroll 1
+  for (int i0 = tid; i0 < n_loads; i0 += 256 * kLoads) {
+    uint4 w[kLoads];
+    uint32_t some = 0u;  // those that reach the threshold, and all at a row's end
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+      w[l] = make_uint4(0u, 0u, 0u, 0u);
+      if (i0 - tid + 256 * l >= n_loads) continue;  // whole workgroup
+      const int i = i0 + 256 * l, id = id_of(min(i, n_loads - 1));
+      if (id + E <= p.vocab) w[l] = *reinterpret_cast<const uint4*>(z_row + id);
+      if (i < n_loads && id + E > p.vocab) some |= ((1u << E) - 1u) << (E * l);
+    }
+#pragma unroll
+    for (int l = 0; l < kLoads; ++l) {
+      const uint32_t u[4] = {w[l].x, w[l].y, w[l].z, w[l].w};
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const uint32_t key = top_key(tame(sizeof(T) == 4 ? __uint_as_float(u[e & 3]) : ((e & 1) ? bf16_hi(u[(e >> 1) & 3]) : bf16_lo(u[(e >> 1) & 3]))));
-        if (key >= threshold) list_candidate(top_sh, key, id + e);
+        const float x = sizeof(T) == 4 ? __uint_as_float(u[e & 3]) : ((e & 1) ? bf16_hi(u[(e >> 1) & 3]) : bf16_lo(u[(e >> 1) & 3]));
+        some |= x >= least ? 1u << (E * l + e) : 0u;
       }
-    } else {
-      for (int e = id; e < p.vocab; ++e) {
-        const uint32_t key = top_key(logit(z_row, e));
-        if (key >= threshold) list_candidate(top_sh, key, e);
-      }
+    }
+    while (some != 0u) {  // few, which come from the cache
+      const int bit = __builtin_ctz(some), i = i0 + bit / E * 256;
+      some &= some - 1u;
+      if (i >= n_loads) break;
+      const int id = id_of(i) + bit % E;
+      const uint32_t key = id < p.vocab ? top_key(logit(z_row, id)) : 0u;
+      if (key >= threshold) list_candidate(top_sh, key, id);
     }
   }
   __syncthreads();
@@ -349,7 +377,25 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
     p.top_ids[(int64_t)row * p.top_n + rank] = id;
     p.top_logprobs[(int64_t)row * p.top_n + rank] = id < 0 ? -INFINITY : (order_value(key) - m) - log_sum;
   };
-  const int listed = (int)top_sh.count;
+  int listed = (int)top_sh.count;
+  if (listed > kTopRanked) {  // the same once more among those that are listed: comparing each with all takes the square of their number
+    unsigned long long mine[kTopCandidates / 256];
+    best = 0u;
+#pragma unroll
+    for (int i = 0; i < kTopCandidates / 256; ++i) {
+      mine[i] = tid + 256 * i < listed ? top_sh.list[tid + 256 * i] : 0ull;
+      best = max(best, (uint32_t)(mine[i] >> 32));
+    }
+    __syncthreads();  // (the count is read)
+    const uint32_t bound = top_threshold(top_sh, best, p.top_n);
+#pragma unroll 1
+    for (int i = 0; i < kTopCandidates / 256; ++i) {
+      const unsigned long long x = i == 0 ? mine[0] : (i == 1 ? mine[1] : (i == 2 ? mine[2] : mine[3]));
+      if ((uint32_t)(x >> 32) >= bound) list_candidate(top_sh, (uint32_t)(x >> 32), (int)~(uint32_t)x);
+    }
+    __syncthreads();
+    listed = (int)top_sh.count;
+  }
   rank_candidates(top_sh, listed, p.top_n, emit);
   for (int i = listed + tid; i < p.top_n; i += 256) emit(i, 0u, -1);
 }

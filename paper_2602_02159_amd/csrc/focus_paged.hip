@@ -7,13 +7,17 @@
 // lies within one wavefront is written out by it, the pieces of the others go to the workspace, and a second launch joins them.  The wavefronts of
 // a workgroup take neighbouring heads of the same tiles: where the heads of a row lie side by side their rows are then fetched at about the same time.
 //
-// The products are those of the attention over the quantised cache: rows go from memory straight into the registers in which
-// v_mfma_f32_16x16x32_bf16 takes them.
-//   S^T = K Q^T   lane (c, g) has 16 bytes at a time of the rows c and 16 + c, 64 bytes of a row side by side
-//   O^T = V^T P^T column tile ct has the columns c * D / 16 + ct: lane (c, g) has D / 16 neighbouring values of the eight rows 4 g + i and
-//                 16 + 4 g + i whose probabilities it holds, and byte permutations put those of two rows next to each other
+// Products, from tiles of 32 rows that lie in LDS (Ring):
+//   S^T = K Q^T   v_mfma_f32_16x16x32_bf16, lane (c, g) with 16 bytes at a time of the rows c and 16 + c
+//   O^T = V^T P^T bf16: column tile ct has the columns 16 ct + c, by transposed reads; codes: c * D / 16 + ct, D / 16 neighbouring codes of each of the
+//                 rows 4 g + i and 16 + 4 g + i, of which byte permutations put those of two rows next to each other
 // P is split into two bf16 numbers, p = hi + lo to 2^-17, and multiplied twice: rounded to one it would cost the result as much
 // again as its own rounding, and the matrix unit has nothing else to do (a tile is 16 KB from memory and 24 products).
+//
+// What bounds it is HBM, every row read once: one request of 32 832 rows, 32 heads, 538 MB, in 83 us = 6.5 TB/s and 4.7 for the join; 64 of up to
+// 16 384 rows with 4 query heads on each of 8, 869 MB, in 135 and 6; eight-bit rows, 227 MB for 37 requests with 16 rows a unit, in 54 and 7: some 8 us are the
+// start, 8 the pieces of 16 rows each (16 KB a wavefront), and half as many bytes a tile leave the instructions half the time.  A thousand
+// rows of four heads: 6.0 + 4.1 us, dependent round trips (lengths, table, rows, products; pieces).
 #include <algorithm>
 
 #include "focus_codes.h"
@@ -129,9 +133,11 @@ struct Unit {
   int r, b, qg;
 };
 
-// The rows of a tile lie in LDS between memory and the products: every wavefront has a ring of its own, 32 KB of rows, whose loads go to LDS
-// directly and are waited for by their number.  (The same bytes under way in registers cost two more copies of the code, or wavefronts that wait
-// for one tile at a time: 32 heads, 32 832 keys 91.5 us.)
+// The rows of a tile lie in LDS between memory and the products: every wavefront has a ring of its own, 16 KB of rows (one tile of 128 bf16
+// columns, two of codes), whose loads go to LDS directly and are waited for by their number; K's place is asked for again while V is worked on.  Two workgroups
+// a compute unit hide each other's joints.  32 heads, 32 832 keys: 83 us; the same bytes under way in registers 91.5, and spills with 32 query rows.  Rings of
+// 32 KB and one workgroup: eight-bit rows 94 to 101 us instead of 64 to 73.  Past the caches (kStreamPolicy), as most rows are read once: 145 instead of
+// 164 us for 64 requests; where seven groups of rows share them (25 rows of 7 heads a request) it is 127 instead of 104, which is not what this is built for.
 template <int D, bool QUANT>
 struct Ring {
   static constexpr int kRow = QUANT ? D : 2 * D, kRows = kTile * kRow;  // bytes of a row, of a tile's K (or V)
@@ -409,8 +415,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
   int limit[NT];  // keys that the lane's row may attend to
   float m_run[NT], l_run[NT];
   floatx4 o[NT][kCT];
-  // Column tile ct of O^T: bf16 rows, the columns 16 ct + c; codes, the columns c * D / 16 + ct.  Rows of a tile are in lane (c, g) the columns ...
-  // ... of query row c.
+  // o[n][ct]: lane (c, g) has of query row 16 n + c four columns of column tile ct, see end_piece
   auto begin_unit = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -657,7 +662,8 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
   }
 }
 
-// Joins the pieces of the units that several wavefronts worked on: NW wavefronts for one row of one query head.  Whose pieces they are the wavefront with
+// Joins the pieces of the units that several wavefronts worked on: NW wavefronts for one row of one query head.  The pieces' largest logits are a lane each
+// and their sums of weights one reduction, so that 20 pieces are one round trip: 4 to 7 us.  Whose pieces they are the wavefront with
 // the last one has left (`whose`: the first of them, how many follow on one another; none: the unit is written).
 template <int D, int NT, int NW>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
@@ -754,7 +760,9 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
   if (p.lse && lane == 0) p.lse[(int64_t)(q.first + i) * Hq + head] = l_run == 0.f ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_run)) * kLn2;
 }
 
-// Wavefronts: a workgroup's rings take most of a compute unit's LDS.  No more than the batch may have tiles.
+// Two workgroups a compute unit, as their rings allow, and no more than the batch may have tiles.  Up to 16 query rows of a K/V head are one operand (NT = 1),
+// more are taken 32 at a time, which halves the passes over the rows: 25 rows of 7 heads, 16 requests of 4096 127 us and not 209.  Bundles of four heads where
+// they divide: 64 requests 145.6 us, without bundles 150, eight-bit rows 94 and 101.
 constexpr int kPagedGroups = 512;
 PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch& b, int page) {
   PagedPlan p;
@@ -775,7 +783,7 @@ PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch
   return p;
 }
 
-// Few rows: four wavefronts for each, so that all its pieces are requested at once.
+// Few rows: four wavefronts for each, so that all its pieces (512 of a single unit) are requested within a few round trips; many: one each, which fill the chip.
 constexpr int kJoinGroups = 1024;
 template <int D, int NT>
 static hipError_t launch_paged_t(const PagedAttn& a, const PagedPlan& p, hipStream_t st) {

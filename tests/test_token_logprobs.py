@@ -153,6 +153,23 @@ def test_ties(dtype, V):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V,top", [(1000, 32), (2040, 20), (40000, 32), (131071, 3)])
+def test_ordered_rows(dtype, V, top):
+    """Close logits in ascending order, each of them better than all before, and in descending; runs of neighbours that alone are above -inf."""
+    rows = torch.full((6, (V + 7) // 8 * 8), -math.inf)  # of which the kernels see V
+    z = rows[:, :V]
+    z[0] = 3.0 + torch.arange(V) * 1e-5
+    z[1] = z[0].flip(0)
+    z[2, 600:640] = torch.arange(40) * 0.25
+    z[3, V // 8:V // 2] = 1.0
+    z[4] = -1.0
+    z[4, -50:] = torch.arange(50) * 0.5
+    z[5] = (torch.arange(V) % 1500) * 1e-4
+    check(rows.to(dtype).to(DEV)[:, :V], [0, V - 1, 620, V // 4, V - 1, 7], None, top)
+
+
+@pytest.mark.gpu
 def test_rows_that_are_all_but_certain():
     """1 - p down to 2^-60: log1p keeps its digits."""
     z = torch.full((40, 5000), -math.inf)
