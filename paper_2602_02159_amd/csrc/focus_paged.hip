@@ -787,7 +787,7 @@ PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch
 constexpr int kJoinGroups = 1024;
 template <int D, int NT>
 static hipError_t launch_paged_t(const PagedAttn& a, const PagedPlan& p, hipStream_t st) {
-  const bool causal = a.causal && (a.b.max_rows > 1 || a.b.positions != nullptr);  // (the last row sees every key)
+  const bool causal = a.causal && (a.b.row_start != nullptr || a.b.positions != nullptr);  // (the last row sees every key)
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(p.groups), dim3(256), 0, st, a); };
   if (a.k_exp != nullptr)
     causal ? launch(paged_attn_kernel<D, true, true, NT>) : launch(paged_attn_kernel<D, true, false, NT>);

@@ -528,6 +528,31 @@ def test_keys_that_a_row_does_not_see_do_not_reach_it(group, quant):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("max_rows", [1, 2])
+def test_rows_past_the_most(max_rows, causal):
+    """Requests that list more rows than max_rows: the first ones are worked on, at the positions that they have among all of them."""
+    lens, rows = [40, 70, 5], [3, 4, 1]
+    pool = Pages(lens, 3, 32, 2, 64, False, False, seed=3).fill()
+    start = torch.tensor([0, 3, 7, 8], dtype=torch.int32, device=DEV)
+    batch = fb.make_paged_batch(torch.tensor(lens, dtype=torch.int32, device=DEV), pool.table.to(DEV), start, max_rows, 9)
+    q = torch.randn((9, 4, 64), generator=torch.Generator().manual_seed(1)).bfloat16().to(DEV)
+    out, lse = torch.full_like(q, 5.0), torch.full((9, 4), 6.0, device=DEV)
+    fb.paged_attn(q, pool.cache, batch, causal, out, lse, workspace(pool.cache, batch, 4))
+    out, lse, q, first, worked = out.cpu(), lse.cpu(), q.cpu().double(), [0, 3, 7], []
+    for r in range(3):
+        j, k, v = pool.rows(r, lens[r])
+        for i in range(min(rows[r], max_rows)):
+            at = first[r] + i
+            worked.append(at)
+            seen = j[None] <= lens[r] - rows[r] + i if causal else torch.ones((1, j.numel()), dtype=torch.bool)
+            for h in range(4):
+                check_attention(out[at:at + 1, h], lse[at:at + 1, h], attend64(q[at:at + 1, h], k[:, h // 2], v[:, h // 2], seen))
+    rest = [i for i in range(9) if i not in worked]
+    assert bool((out[rest] == 5.0).all()) and bool((lse[rest] == 6.0).all())
+
+
+@pytest.mark.gpu
 def test_attention_extreme_logits():
     """One key far above the others, all keys equal, logits that overflow an exponential."""
     pool = Pages([3000, 50], 94, 32, 1, 64, False, False).fill()
