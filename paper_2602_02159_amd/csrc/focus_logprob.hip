@@ -24,7 +24,7 @@ namespace focus {
 
 constexpr int kLogitsThread = 32, kLogitsPart = 256 * kLogitsThread;
 // candidates and fours that are listed at most (more: list_in_turn); up to 96 candidates are compared each with all (5 x 1000 logits, of which all are: 65 us
-// that way, 16 this)
+// that way, 17 narrowed first)
 constexpr int kTopCandidates = 1024, kTopFours = 1024, kTopRanked = 96;
 
 // NaN as -inf, +inf as the largest number
@@ -74,7 +74,7 @@ __device__ __forceinline__ float block_max4(float x, float* sh) {
 struct TopShared256 {
   uint32_t best[64];
   unsigned long long list[kTopCandidates];
-  unsigned long long kept[kLogprobTop];
+  unsigned long long shares[64];
   int fours[kTopFours];
   uint32_t count, n_fours;
 };
@@ -122,8 +122,42 @@ __device__ __forceinline__ void rank_candidates(const TopShared256& sm, int n, i
     if (part == 0 && (int)rank < top_n) emit((int)rank, (uint32_t)(mine >> 32), (int)~(uint32_t)mine);
   }
 }
-// More candidates than the list holds (equal logits): the row from its first id on.  Where the list fills up, its first top_n stay, and from there on only
-// larger logits come in, as equal ones have higher ids.  key_at(id): 0 for none
+// Drops listed candidates that cannot be among the first top_n of n: those behind the top_n-th of the best of 64 shares of the list, ids counted.  Returns that
+// one's place (0: fewer shares have any).  Up to 16 top_n stay, some 1.2 top_n where the list is in no order.
+__device__ __forceinline__ unsigned long long narrow_list(TopShared256& sm, int n, int top_n) {
+  constexpr int kEach = kTopCandidates / 256;
+  const int tid = threadIdx.x;
+  unsigned long long mine[kEach], best = 0ull;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    mine[i] = tid + 256 * i < n ? sm.list[tid + 256 * i] : 0ull;
+    best = mine[i] > best ? mine[i] : best;
+  }
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    const unsigned long long other = __shfl_xor(best, o, kWave);
+    best = other > best ? other : best;
+  }
+  if ((tid & 3) == 0) sm.shares[tid >> 2] = best;
+  __syncthreads();
+  if (tid == 0) sm.count = 0u;
+  const unsigned long long share = sm.shares[tid & 63];
+  int rank = 0;
+#pragma unroll 8
+  for (int j = 0; j < 64; ++j) rank += sm.shares[j] > share ? 1 : 0;
+  const unsigned long long last = __ballot(rank == top_n - 1 && share != 0ull);
+  const unsigned long long bound = last == 0ull ? 0ull : sm.shares[__builtin_ctzll(last)];
+  __syncthreads();
+#pragma unroll 1
+  for (int i = 0; i < kEach; ++i) {
+    const unsigned long long x = i == 0 ? mine[0] : (i == 1 ? mine[1] : (i == 2 ? mine[2] : mine[3]));
+    if (x != 0ull && x >= bound) sm.list[atomicAdd(&sm.count, 1u)] = x;
+  }
+  __syncthreads();
+  return bound;
+}
+// More candidates than the list holds (equal logits): the row from its first id on.  Where the list fills up it is narrowed, and from there on only larger logits
+// come in than the bound's, as equal ones have higher ids.  key_at(id): 0 for none
 template <class Key>
 __device__ __forceinline__ void list_in_turn(TopShared256& sm, uint32_t bound, int vocab, int top_n, const Key key_at) {
   constexpr int U = 8;
@@ -145,11 +179,7 @@ __device__ __forceinline__ void list_in_turn(TopShared256& sm, uint32_t bound, i
       __syncthreads();
       const int n = (int)sm.count;
       if (n > kTopCandidates - 256) {  // whole workgroup
-        rank_candidates(sm, n, top_n, [&](int rank, uint32_t k, int id) { sm.kept[rank] = place_of(k, id); });
-        __syncthreads();
-        if (tid < top_n) sm.list[tid] = sm.kept[tid];
-        if (tid == 0) sm.count = (uint32_t)top_n;
-        bound = (uint32_t)(sm.kept[top_n - 1] >> 32) + 1u;
+        bound = max((uint32_t)(narrow_list(sm, n, top_n) >> 32) + 1u, bound);
       }
       __syncthreads();
     }
@@ -287,10 +317,11 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
   float4 s = make_float4(-INFINITY, 0.f, 0.f, 0.f);  // at most 256 parts: one a thread
   if (tid < p.n_parts) s = p.part[(int64_t)row * p.n_parts + tid];
   const float* tops = p.part_top + (int64_t)row * p.n_parts * 64;
-  const int n = p.top_n > 0 ? p.n_parts * 64 : 0;
+  // Thread t has the (t / 4)-th of the parts t % 4, t % 4 + 4, ...: four threads together have one of every part, a part alone is spread over all
+  const int n = p.top_n > 0 ? p.n_parts * 64 : 0, mine0 = (tid & 3) * 64 + (tid >> 2);
   float top_of[kFours];  // those of the first 16 parts, here before the statistics are
 #pragma unroll
-  for (int i = 0; i < kFours; ++i) top_of[i] = tid + 256 * i < n ? tops[tid + 256 * i] : -INFINITY;
+  for (int i = 0; i < kFours; ++i) top_of[i] = mine0 + 256 * i < n ? tops[mine0 + 256 * i] : -INFINITY;
   const float m = block_max4(s.x, max_sh), m_use = m == -INFINITY ? 0.f : m;
   // Of the parts whose largest logit is the row's the first one's is left out of r
   const unsigned long long top = __ballot(s.x == m && m != -INFINITY);
@@ -319,7 +350,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
   uint32_t best = 0u;
 #pragma unroll
   for (int i = 0; i < kFours; ++i) best = max(best, top_key(top_of[i]));
-  for (int i = tid + 256 * kFours; i < n; i += 256) best = max(best, top_key(tops[i]));
+  for (int i = mine0 + 256 * kFours; i < n; i += 256) best = max(best, top_key(tops[i]));
   const uint32_t threshold = top_threshold(top_sh, best, p.top_n);
   if (best >= threshold) {
     auto take = [&](float x, int i) __attribute__((always_inline)) {
@@ -328,8 +359,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
       if (at < (uint32_t)kTopFours) top_sh.fours[at] = i;
     };
 #pragma unroll
-    for (int i = 0; i < kFours; ++i) take(top_of[i], tid + 256 * i);
-    for (int i = tid + 256 * kFours; i < n; i += 256) take(tops[i], i);
+    for (int i = 0; i < kFours; ++i) take(top_of[i], mine0 + 256 * i);
+    for (int i = mine0 + 256 * kFours; i < n; i += 256) take(tops[i], i);
   }
   __syncthreads();
   const T* z_row = static_cast<const T*>(p.logits) + (int64_t)row * p.row_stride;
@@ -378,22 +409,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(const LogprobArgs p) 
     p.top_logprobs[(int64_t)row * p.top_n + rank] = id < 0 ? -INFINITY : (order_value(key) - m) - log_sum;
   };
   int listed = (int)top_sh.count;
-  if (listed > kTopRanked) {  // the same once more among those that are listed: comparing each with all takes the square of their number
-    unsigned long long mine[kTopCandidates / 256];
-    best = 0u;
-#pragma unroll
-    for (int i = 0; i < kTopCandidates / 256; ++i) {
-      mine[i] = tid + 256 * i < listed ? top_sh.list[tid + 256 * i] : 0ull;
-      best = max(best, (uint32_t)(mine[i] >> 32));
-    }
-    __syncthreads();  // (the count is read)
-    const uint32_t bound = top_threshold(top_sh, best, p.top_n);
-#pragma unroll 1
-    for (int i = 0; i < kTopCandidates / 256; ++i) {
-      const unsigned long long x = i == 0 ? mine[0] : (i == 1 ? mine[1] : (i == 2 ? mine[2] : mine[3]));
-      if ((uint32_t)(x >> 32) >= bound) list_candidate(top_sh, (uint32_t)(x >> 32), (int)~(uint32_t)x);
-    }
-    __syncthreads();
+  if (listed > kTopRanked) {
+    narrow_list(top_sh, listed, p.top_n);
     listed = (int)top_sh.count;
   }
   rank_candidates(top_sh, listed, p.top_n, emit);
