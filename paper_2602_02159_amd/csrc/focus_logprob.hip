@@ -9,9 +9,9 @@
 //   logprob_join_kernel  a workgroup a row: the parts together; the likeliest tokens
 // The likeliest: 64 numbers of a part, each the largest of 128 logits, are all that the first launch writes.  A number that top_n of all of them reach is
 // reached by top_n logits, and what reaches it lies in some 1.2 top_n of those 128s, which the second launch reads once more.  (Each part with a list of its own
-// likeliest: 500 rows of 126 464, 20 alternatives 43.4 us instead of 33.2.)
+// likeliest: 500 rows of 126 464, 20 alternatives 43.4 us instead of 32.3.)
 // Every logit is read once.  What bounds it: many rows, HBM and the exponentials: 500 x 126 464 bf16, 126 MB, in 24.6 us = 5.1 TB/s
-// and 8.9 us for the rows' ends; 511 x 32 003 fp32 in 14.4 + 6.6.  One row (3.5 + 6.0 us): the chain of round trips in two launches that depend on each other.
+// and 8.9 us for the rows' ends; 511 x 32 003 fp32 in 13.5 + 6.6.  One row (3.5 + 6 us): the chain of round trips in two launches that depend on each other.
 // Not better: parts of 2048 for few rows (one row 14.5 us instead of 14.0 at that time), 16 logits a thread (50 instead of 43), 24 (42.4 instead of 43.3, but
 // more parts than one a thread).
 #include <type_traits>

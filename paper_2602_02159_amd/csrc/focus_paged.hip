@@ -15,7 +15,7 @@
 // again as its own rounding, and the matrix unit has nothing else to do (a tile is 16 KB from memory and 24 products).
 //
 // What bounds it is HBM, every row read once: one request of 32 832 rows, 32 heads, 538 MB, in 83 us = 6.5 TB/s and 4.7 for the join; 64 of up to
-// 16 384 rows with 4 query heads on each of 8, 869 MB, in 135 and 6; eight-bit rows, 227 MB for 37 requests with 16 rows a unit, in 54 and 7: some 8 us are the
+// 16 384 rows with 7 query heads on each of 4, 869 MB, in 135 and 6; eight-bit rows, 227 MB for 37 requests with 16 rows a unit, in 54 and 7: some 8 us are the
 // start, 8 the pieces of 16 rows each (16 KB a wavefront), and half as many bytes a tile leave the instructions half the time.  A thousand
 // rows of four heads: 6.0 + 4.1 us, dependent round trips (lengths, table, rows, products; pieces).
 #include <algorithm>
