@@ -136,8 +136,7 @@ struct Unit {
 // The rows of a tile lie in LDS between memory and the products: every wavefront has a ring of its own, 16 KB of rows (one tile of 128 bf16
 // columns, two of codes), whose loads go to LDS directly and are waited for by their number; K's place is asked for again while V is worked on.  Two workgroups
 // a compute unit hide each other's joints.  32 heads, 32 832 keys: 83 us; the same bytes under way in registers 91.5, and spills with 32 query rows.  Rings of
-// 32 KB and one workgroup: eight-bit rows 94 to 101 us instead of 64 to 73.  Past the caches (kStreamPolicy), as most rows are read once: 145 instead of
-// 164 us for 64 requests; where seven groups of rows share them (25 rows of 7 heads a request) it is 127 instead of 104, which is not what this is built for.
+// 32 KB and one workgroup: eight-bit rows 94 to 101 us instead of 64 to 73.
 template <int D, bool QUANT>
 struct Ring {
   static constexpr int kRow = QUANT ? D : 2 * D, kRows = kTile * kRow;  // bytes of a row, of a tile's K (or V)
@@ -206,8 +205,8 @@ __device__ __forceinline__ int64_t offset_of_slot(int64_t off, int slot) {
 }
 // The rows of a tile to `stage`.  Lane l of load i supplies the 16 bytes that land at stage + 1024 i + 16 l: place l mod kChunks of row
 // i * kPerLoad + l / kChunks.
-template <int D, bool QUANT>
-__device__ __forceinline__ void request_rows(const uint8_t* base, int64_t stride_p, int64_t stride_n, TilePlace x, char* stage, int lane) {
+template <int D, bool QUANT, int POLICY>
+__device__ __forceinline__ void request_rows_as(const uint8_t* base, int64_t stride_p, int64_t stride_n, TilePlace x, char* stage, int lane) {
   using G = Ring<D, QUANT>;
   const int sub = lane / G::kChunks, pos = lane % G::kChunks;
   if (x.plain) {
@@ -217,7 +216,7 @@ __device__ __forceinline__ void request_rows(const uint8_t* base, int64_t stride
     for (int i = 0; i < G::kLoads; ++i) {
       const int slot = i * G::kPerLoad + sub, first = i * G::kPerLoad;
       const uint8_t* src = rows[first >> 4] + (int64_t)(first & 15) * stride_n + (lane_row + (uint32_t)((pos ^ G::turn(slot)) << 4));
-      __builtin_amdgcn_global_load_lds((gptr_t)src, (lptr_t)(stage + i * 1024), 16, 0, kStreamPolicy);
+      __builtin_amdgcn_global_load_lds((gptr_t)src, (lptr_t)(stage + i * 1024), 16, 0, POLICY);
     }
     return;
   }
@@ -226,8 +225,17 @@ __device__ __forceinline__ void request_rows(const uint8_t* base, int64_t stride
   for (int i = 0; i < G::kLoads; ++i) {
     const int slot = i * G::kPerLoad + sub;
     const uint8_t* src = base + offset_of_slot(mine, slot) + ((pos ^ G::turn(slot)) << 4);
-    __builtin_amdgcn_global_load_lds((gptr_t)src, (lptr_t)(stage + i * 1024), 16, 0, kStreamPolicy);
+    __builtin_amdgcn_global_load_lds((gptr_t)src, (lptr_t)(stage + i * 1024), 16, 0, POLICY);
   }
+}
+// Past the caches, unless several groups of query rows read the same bf16 rows: 25 rows of 7 heads, 16 requests of 4096 149 us past them, 118 through them, 64 of 4,
+// 32 requests of 2048 375 and 337; one group (64 requests, 7 heads) 145 and 164; eight-bit rows of several groups 110 and 118
+template <int D, bool QUANT, int NT>
+__device__ __forceinline__ void request_rows(const PagedAttn& p, const uint8_t* base, int64_t stride_p, int64_t stride_n, TilePlace x, char* stage, int lane) {
+  if (!QUANT && NT > 1 && p.most_groups > 1)
+    request_rows_as<D, QUANT, 0>(base, stride_p, stride_n, x, stage, lane);
+  else
+    request_rows_as<D, QUANT, kStreamPolicy>(base, stride_p, stride_n, x, stage, lane);
 }
 // exponents of slot lane % 32, of K in the lower half of the wavefront, of V in the upper
 __device__ __forceinline__ void request_exponents(const PagedAttn& p, TilePlace x, int h, char* stage, int lane) {
@@ -400,11 +408,11 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
     place = locate(p, ahead, t_ahead, window, lane);
     char* stage = stage_of(asked);
     if constexpr (QUANT) request_exponents(p, place, head_of(ahead), stage + 2 * G::kRows, lane);
-    request_rows<D, QUANT>(p.K + (int64_t)head_of(ahead) * p.ksh, p.ksp, p.ksn, place, stage, lane);
+    request_rows<D, QUANT, NT>(p, p.K + (int64_t)head_of(ahead) * p.ksh, p.ksp, p.ksn, place, stage, lane);
     masks = lane == (asked & (kDepth - 1)) ? (int)place.mask : masks;
   };
   auto request_v = [&]() __attribute__((always_inline)) {
-    request_rows<D, QUANT>(p.V + (int64_t)head_of(ahead) * p.vsh, p.vsp, p.vsn, place, stage_of(asked) + G::kRows, lane);
+    request_rows<D, QUANT, NT>(p, p.V + (int64_t)head_of(ahead) * p.vsh, p.vsp, p.vsn, place, stage_of(asked) + G::kRows, lane);
     ++asked;
     if (++t_ahead >= ahead.q.tiles && asked < n_tiles) {
       t_ahead = 0;
@@ -534,7 +542,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
         const TilePlace here = locate(p, u, t, win, lane);
 #pragma unroll 1
         for (int which = 2; which >= 0; --which) {
-          request_rows<D, QUANT>(p.V + (int64_t)head_of(u) * p.vsh, p.vsp, p.vsn, here, stage, lane);
+          request_rows<D, QUANT, NT>(p, p.V + (int64_t)head_of(u) * p.vsh, p.vsp, p.vsn, here, stage, lane);
           wait_loads();
 #pragma unroll 1
           for (int i = 0; i < 4 * G::kLoads; ++i) rewrite_word<QUANT>(stage + i * 256 + lane * 4, which);
