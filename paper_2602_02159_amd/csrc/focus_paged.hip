@@ -297,7 +297,8 @@ __device__ __forceinline__ void read_v_codes(uint32_t (&v)[8][D / 64], const cha
         : "memory");
   }
 }
-// 2^E of the rows 4 g + i and 16 + 4 g + i, of K and of V
+// 2^E of the rows 4 g + i and 16 + 4 g + i, of K and of V.  A byte of 255, which rows that nobody has written may hold, is an infinity: logits of such rows
+// are masked afterwards, but a probability of zero times it would be NaN.
 __device__ __forceinline__ void read_exponents(floatx4 (&ek)[2], floatx4 (&ev)[2], const char* stage, int lane) {
   const uint32_t a = lds_address(stage) + 16 * (lane >> 4);
   uintx4 x[4];
@@ -311,7 +312,7 @@ __device__ __forceinline__ void read_exponents(floatx4 (&ek)[2], floatx4 (&ev)[2
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       ek[i][e] = exp_value(x[i][e]);
-      ev[i][e] = exp_value(x[2 + i][e]);
+      ev[i][e] = exp_value(min(x[2 + i][e], 254u));
     }
 }
 

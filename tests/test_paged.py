@@ -528,6 +528,29 @@ def test_keys_that_a_row_does_not_see_do_not_reach_it(group, quant):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("d,group,page", [(128, 4, 16), (128, 12, 7), (64, 1, 32), (64, 24, 16)])
+def test_memory_that_was_never_written_does_not_reach_earlier_rows(d, group, page):
+    """Eight-bit pages whose later positions hold the NaN code and exponent bytes of 255 (infinity as a factor), which no row that is written has: rows
+    before them get the attention over what is there."""
+    lens, written = [100, 300], [61, 37]
+    pool = Pages(lens, -(-300 // page), page, 2, d, True, False, seed=d + group)
+    assert bool((pool.k_exp == 255).all()) and bool((pool.v_exp == 255).all())
+    pool.lens = written
+    pool.fill()
+    positions = [60, 3, 0, 33, 36, 31, 20]
+    rows = [4, 3]
+    batch = batch_of(lens, pool.table, rows, positions)
+    q = torch.randn((7, 2 * group, d), generator=torch.Generator().manual_seed(3)).bfloat16()
+    out, lse = torch.empty((7, 2 * group, d), dtype=torch.bfloat16, device=DEV), torch.empty((7, 2 * group), device=DEV)
+    fb.paged_attn(q.to(DEV), pool.cache, batch, True, out, lse, workspace(pool.cache, batch, 2 * group))
+    for at, r, p in places(lens, rows, positions):
+        j, k, v = pool.rows(r, p + 1)
+        for h in range(2 * group):
+            ref = attend64(q[at:at + 1, h].double(), k[:, h // group], v[:, h // group], torch.ones((1, p + 1), dtype=torch.bool))
+            check_attention(out[at:at + 1, h].cpu(), lse[at:at + 1, h].cpu(), ref)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("max_rows", [1, 2])
 def test_rows_past_the_most(max_rows, causal):
