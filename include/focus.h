@@ -498,7 +498,8 @@ int focus_paged_append(const focus_paged_cache* cache, const focus_paged_batch* 
  *   Q    [dev] bf16 [n_rows, n_q_heads, d], strides q_stride_*; n_q_heads a multiple of H
  *   out  [dev] bf16 [n_rows, n_q_heads, d], strides o_stride_*
  *   lse  [dev] fp32 [n_rows, n_q_heads] natural-log sum of exp of the scaled logits, may be NULL
- * A row without a key gets zeros and -inf.  Keys that a row does not attend to do not reach it, whatever they hold (memory that was never written
+ * A row without a key gets zeros and -inf.  An infinity in V of a key that a row attends to comes out as it is, however small the key's weight, a NaN or
+ * infinities of both signs as NaN.  Keys that a row does not attend to do not reach it, whatever they hold (memory that was never written
  * among them, and exponent bytes of 255).  As K is turned when it is written, leaving pages out of page_table (entries of -1) is the attention
  * over the others.  Queries as for focus_quant_cache over rows of eight bits.
  *   workspace [dev] focus_paged_attn_workspace() bytes, 16-byte aligned; nothing is assumed about its contents

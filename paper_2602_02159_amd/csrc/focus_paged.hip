@@ -316,32 +316,14 @@ __device__ __forceinline__ void read_exponents(floatx4 (&ek)[2], floatx4 (&ev)[2
     }
 }
 
-// Sixteen bytes of a stage, as above; the reads and writes of a wavefront keep their order
-__device__ __forceinline__ uint4 read_chunk(const char* at) {
-  uintx4 x;
-  asm volatile("ds_read_b128 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(x) : "v"(lds_address(at)) : "memory");
-  return __builtin_bit_cast(uint4, x);
-}
-// Whether one of two bf16 numbers, or of four codes, is an infinity or a NaN
-template <bool QUANT>
-__device__ __forceinline__ bool beyond_finite(uint32_t w) {
-  if (QUANT) return ((~w & 0x7fu) == 0u) | ((~w & 0x7f00u) == 0u) | ((~w & 0x7f0000u) == 0u) | ((~w & 0x7f000000u) == 0u);
-  return ((~w & 0x7f80u) == 0u) | ((~w & 0x7f800000u) == 0u);
-}
-// Rewrites the numbers of a word of a stage: which = 0: zero in the place of infinities and NaN; 1: one where +inf or NaN is, zero elsewhere; 2: of
-// -inf or NaN
-template <bool QUANT>
-__device__ __forceinline__ void rewrite_word(const char* at, int which) {
-  constexpr int kBits = QUANT ? 8 : 16;
-  uint32_t w, y = 0u;
-  asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=&v"(w) : "v"(lds_address(at)) : "memory");
-#pragma unroll 1
-  for (int shift = 0; shift < 32; shift += kBits) {
-    const uint32_t z = (w >> shift) & ((1u << kBits) - 1u), size = z & ((1u << (kBits - 1)) - 1u), limit = QUANT ? 0x7fu : 0x7f80u;
-    const bool nan = QUANT ? size == limit : size > limit, mine = nan || (size == limit && (z != size) == (which == 2));
-    y |= (which == 0 ? (size < limit ? z : 0u) : (mine ? (QUANT ? 0x38u : 0x3f80u) : 0u)) << shift;
-  }
-  asm volatile("ds_write_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)" : : "v"(lds_address(at)), "v"(y) : "memory");
+// Of a pair of bf16 numbers: the finite ones, zero for the others (which = 0), or one where +inf (which = 2) or -inf (1) or a NaN is, zero elsewhere
+__device__ __forceinline__ uint32_t sorted_out(uint32_t w, int which) {
+  auto one = [&](uint32_t z) __attribute__((always_inline)) {
+    const uint32_t size = z & 0x7fffu;
+    if (which == 0) return size < 0x7f80u ? z : 0u;
+    return size > 0x7f80u || z == (which == 2 ? 0x7f80u : 0xff80u) ? 0x3f80u : 0u;
+  };
+  return one(w & 0xffffu) | one(w >> 16) << 16;
 }
 
 // Query rows of tile n of a unit: lane (c, g) has row 16 n + c in the order of the K rows' pieces, zeros past the unit's rows
@@ -358,12 +340,22 @@ __device__ __forceinline__ void load_queries(bf16x8 (&q)[D / 32], const PagedAtt
   }
 }
 
+// What a wavefront has of N operands of sixteen query rows: lane (c, g) of row c
+template <int D, int N>
+struct QueryRows {
+  static constexpr int kN = N;
+  bf16x8 q[N][D / 32];
+  int limit[N];  // keys that the lane's row may attend to
+  float m[N], l[N];
+  floatx4 o[N][D / 16];  // of query row 16 n + c four columns of column tile ct, see end_piece
+};
+
 template <int D, bool QUANT, bool CAUSAL, int NT>
 __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
   using G = Ring<D, QUANT>;
   constexpr int kKS = D / 32, kCT = D / 16, kDepth = G::kDepth;
   __shared__ __attribute__((aligned(256))) char ring_sh[kWavesPerGroup * G::kBytes];
-  const int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
+  int lane = threadIdx.x & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int in_bundle = wave & ((1 << p.log_bundle) - 1), bundles = p.H >> p.log_bundle;
   const int wave_id = (int)blockIdx.x * kWavesPerGroup + wave, worker = wave_id >> p.log_bundle;
@@ -420,35 +412,31 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
       next_unit(ahead);
     }
   };
-  bf16x8 q[NT][kKS];
-  int limit[NT];  // keys that the lane's row may attend to
-  float m_run[NT], l_run[NT];
-  floatx4 o[NT][kCT];
-  // o[n][ct]: lane (c, g) has of query row 16 n + c four columns of column tile ct, see end_piece
-  auto begin_unit = [&]() __attribute__((always_inline)) {
+  // w: the rows of operand n0 on
+  auto begin_unit = [&](auto& w, int n0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int at = (u.qg * NT + n) * 16 + c;
-      load_queries<D, QUANT>(q[n], p, u, head_of(u), at, lane);
-      limit[n] = u.q.len;
+    for (int n = 0; n < w.kN; ++n) {
+      const int at = (u.qg * NT + n0 + n) * 16 + c;
+      load_queries<D, QUANT>(w.q[n], p, u, head_of(u), at, lane);
+      w.limit[n] = u.q.len;
       if constexpr (CAUSAL) {
         const int i = min(at / p.group, max(u.q.n - 1, 0));
         const int position = p.b.positions ? p.b.positions[u.q.first + i] : max(p.b.seq_len[u.r], 0) - u.q.count + i;
-        limit[n] = min(position, u.q.len - 1) + 1;
+        w.limit[n] = min(position, u.q.len - 1) + 1;
       }
-      m_run[n] = -INFINITY;
-      l_run[n] = 0.f;
+      w.m[n] = -INFINITY;
+      w.l[n] = 0.f;
 #pragma unroll
-      for (int ct = 0; ct < kCT; ++ct) o[n][ct] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int ct = 0; ct < kCT; ++ct) w.o[n][ct] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
   };
 
   // S of a tile: lane (c, g) has the logits of row c and the keys 4 g + i, 16 + 4 g + i
-  auto multiply_k = [&](floatx4 (&acc)[NT][2], const char* stage) __attribute__((always_inline)) {
+  auto multiply_k = [&](auto& acc, const auto& w, const char* stage) __attribute__((always_inline)) {
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) acc[n][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int n = 0; n < w.kN; ++n) acc[n][kt] = floatx4{0.f, 0.f, 0.f, 0.f};
     if constexpr (QUANT) {
       uint4 k[2][D / 64];
       read_k_codes<D>(k, stage, lane);
@@ -456,12 +444,12 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
       for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int j = 0; j < D / 64; ++j) {
-          const uint4 w = k[kt][j];
-          const bf16x8 k0 = as_bf16x8(decode8(make_uint2(w.x, w.y), 1.f)), k1 = as_bf16x8(decode8(make_uint2(w.z, w.w), 1.f));
+          const uint4 x = k[kt][j];
+          const bf16x8 k0 = as_bf16x8(decode8(make_uint2(x.x, x.y), 1.f)), k1 = as_bf16x8(decode8(make_uint2(x.z, x.w), 1.f));
 #pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            acc[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[n][2 * j], acc[n][kt], 0, 0, 0);
-            acc[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[n][2 * j + 1], acc[n][kt], 0, 0, 0);
+          for (int n = 0; n < w.kN; ++n) {
+            acc[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, w.q[n][2 * j], acc[n][kt], 0, 0, 0);
+            acc[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, w.q[n][2 * j + 1], acc[n][kt], 0, 0, 0);
           }
         }
     } else {
@@ -472,34 +460,34 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-          for (int n = 0; n < NT; ++n) acc[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kt][j], q[n][j], acc[n][kt], 0, 0, 0);
+          for (int n = 0; n < w.kN; ++n) acc[n][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kt][j], w.q[n][j], acc[n][kt], 0, 0, 0);
     }
   };
 
   // The running softmax.  P as two bf16 numbers, see above
-  auto softmax = [&](floatx4 (&acc)[NT][2], uint32_t mask, const floatx4 (&ek)[2], const floatx4 (&ev)[2], bf16x8 (&hi)[NT], bf16x8 (&lo)[NT],
-                     uint32_t (&seen)[NT]) __attribute__((always_inline)) {
+  auto softmax = [&](auto& acc, auto& w, int tile, uint32_t mask, const floatx4 (&ek)[2], const floatx4 (&ev)[2], auto& hi, auto& lo,
+                     auto& seen) __attribute__((always_inline)) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < w.kN; ++n) {
       if constexpr (QUANT) {
         acc[n][0] *= ek[0];
         acc[n][1] *= ek[1];
       }
       seen[n] = mask;
-      if constexpr (CAUSAL) seen[n] &= low_mask(limit[n] - t * kTile);
+      if constexpr (CAUSAL) seen[n] &= low_mask(w.limit[n] - tile * kTile);
       float ps[8];
-      const float alpha = softmax_step(acc[n], seen[n], g, p.scale_log2, m_run[n], l_run[n], ps);
+      const float alpha = softmax_step(acc[n], seen[n], g, p.scale_log2, w.m[n], w.l[n], ps);
       if (__ballot(alpha != 1.f) != 0ull) {
 #pragma unroll
-        for (int ct = 0; ct < kCT; ++ct) o[n][ct] *= alpha;
+        for (int ct = 0; ct < kCT; ++ct) w.o[n][ct] *= alpha;
       }
       if constexpr (QUANT) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) ps[e] *= ev[e >> 2][e & 3];
       }
       hi[n] = pack_bf16x8(ps);
-      const uint4 w = __builtin_bit_cast(uint4, hi[n]);
-      const uint32_t h[4] = {w.x, w.y, w.z, w.w};
+      const uint4 x = __builtin_bit_cast(uint4, hi[n]);
+      const uint32_t h[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
       for (int e = 0; e < 8; ++e) ps[e] -= (e & 1) ? bf16_hi(h[e >> 1]) : bf16_lo(h[e >> 1]);
       lo[n] = pack_bf16x8(ps);
@@ -522,75 +510,110 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
       read_v_operands16<D>(v, stage, lane);
     }
   };
-  auto multiply_v = [&](char* stage, uint32_t mask, const bf16x8 (&hi)[NT], const bf16x8 (&lo)[NT], const uint32_t (&seen)[NT]) __attribute__((always_inline)) {
-    // A key that some rows of the unit may not see has probability zero there, and zero times an infinity or a NaN of its V would still reach
-    // them.  Where a tile holds such values its stage is rewritten, with ones for those that lead up, then down, whose products with ones for the
-    // keys that a row sees say where an infinity or a NaN has to come, and at last with zeros in their place.
-    bool apart = false;
-    if constexpr (CAUSAL) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) apart |= seen[n] != mask;
-    }
-    if (CAUSAL && __ballot(apart) != 0ull) {
-      bool any = false;
-#pragma unroll 1
-      for (int i = 0; i < G::kLoads; ++i) {
-        const uint4 w = read_chunk(stage + i * 1024 + lane * 16);
-        any |= beyond_finite<QUANT>(w.x) | beyond_finite<QUANT>(w.y) | beyond_finite<QUANT>(w.z) | beyond_finite<QUANT>(w.w);
-      }
-      if (__ballot(any) != 0ull) {
-        Window win{-1, 0, 0};
-        const TilePlace here = locate(p, u, t, win, lane);
-#pragma unroll 1
-        for (int which = 2; which >= 0; --which) {
-          request_rows<D, QUANT, NT>(p, p.V + (int64_t)head_of(u) * p.vsh, p.vsp, p.vsn, here, stage, lane);
-          wait_loads();
-#pragma unroll 1
-          for (int i = 0; i < 4 * G::kLoads; ++i) rewrite_word<QUANT>(stage + i * 256 + lane * 4, which);
-          if (which == 0) break;
-          bf16x8 v[kCT];
-          read_v(v, stage);
-          const float add = which == 1 ? INFINITY : -INFINITY;
-#pragma unroll
-          for (int n = 0; n < NT; ++n) {
-            uint32_t y[4];  // one for the keys that the row sees
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-              const uint32_t two = seen[n] >> (16 * (m >> 1) + 4 * g + 2 * (m & 1));
-              y[m] = (two & 1u) * 0x3f80u | ((two >> 1) & 1u) * 0x3f800000u;
-            }
-            const bf16x8 sees = as_bf16x8(make_uint4(y[0], y[1], y[2], y[3]));
-#pragma unroll
-            for (int ct = 0; ct < kCT; ++ct) {
-              const floatx4 found = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[ct], sees, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[n][ct][i] += found[i] > 0.f ? add : 0.f;
-            }
-          }
-        }
-      }
-    }
-    bf16x8 v[kCT];
-    read_v(v, stage);
+  auto multiply_v = [&](auto& w, const bf16x8 (&v)[kCT], const auto& hi, const auto& lo) __attribute__((always_inline)) {
 #pragma unroll
     for (int ct = 0; ct < kCT; ++ct)
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        o[n][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[ct], hi[n], o[n][ct], 0, 0, 0);
-        o[n][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[ct], lo[n], o[n][ct], 0, 0, 0);
+      for (int n = 0; n < w.kN; ++n) {
+        w.o[n][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[ct], hi[n], w.o[n][ct], 0, 0, 0);
+        w.o[n][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[ct], lo[n], w.o[n][ct], 0, 0, 0);
+      }
+  };
+
+  // Infinities and NaN in V.  Products with them are not what the definition says: lo may be zero or negative, and the probability of a key that a row does not
+  // see, or of one far below the largest, is zero.  Any of them in a tile leaves no finite sum in its column, for all rows, until the piece ends; there one look
+  // finds it (0.3 us of 9.7 for a thousand rows, 1 of 139 for 64 requests; a look at every tile would be 64 instructions and more each).  The wavefront then works on
+  // that piece once more, and on what else it has, tile by tile: with zeros in the place of such values, after it has found out for each sum whether one of
+  // them leads up or down among the keys that its row sees, as products of ones for those keys with ones for those values.
+  auto not_finite = [&](const auto& w) __attribute__((always_inline)) {
+    float x[2] = {0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < w.kN; ++n)
+#pragma unroll
+      for (int ct = 0; ct < kCT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2)  // (v_maximum3_f32: a NaN stays)
+          x[i / 2] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(w.o[n][ct][i]), fabsf(w.o[n][ct][i + 1])), x[i / 2]);
+    return __builtin_expect(__ballot(!(x[0] < INFINITY && x[1] < INFINITY)) != 0ull, 0);
+  };
+  auto same_lane = [&]() __attribute__((always_inline)) {  // what follows from the lane's number is worked out anew, and takes no registers of the loop before
+    asm volatile("" : "+v"(lane));
+    c = lane & 15;
+    g = lane >> 4;
+  };
+  // The tiles start .. end - 1 for the rows of operand n
+  auto repeat = [&](QueryRows<D, 1>& w, int n, int start, int end) __attribute__((always_inline)) {
+    uint32_t up = 0u, down = 0u;  // bit 4 ct + i
+#pragma unroll 1
+    for (int which = 2; which >= 0; --which) {  // whether one leads up, down; the sums
+      begin_unit(w, n);
+      Window win{-1, 0, 0};
+#pragma unroll 1
+      for (int tile = start; tile < end; ++tile) {
+        const TilePlace here = locate(p, u, tile, win, lane);
+        if (here.mask == 0u) continue;
+        if constexpr (QUANT) request_exponents(p, here, head_of(u), ring + 2 * G::kRows, lane);
+        request_rows_as<D, QUANT, 0>(p.K + (int64_t)head_of(u) * p.ksh, p.ksp, p.ksn, here, ring, lane);
+        request_rows_as<D, QUANT, 0>(p.V + (int64_t)head_of(u) * p.vsh, p.vsp, p.vsn, here, ring + G::kRows, lane);
+        wait_loads();
+        same_lane();
+        bf16x8 hi[1], lo[1], v[kCT];
+        uint32_t seen[1];
+        if (which == 0) {
+          floatx4 acc[1][2], ek[2], ev[2];
+          multiply_k(acc, w, ring);
+          if constexpr (QUANT) read_exponents(ek, ev, ring + 2 * G::kRows, lane);
+          softmax(acc, w, tile, here.mask, ek, ev, hi, lo, seen);
+        } else {  // ones for the keys that the row sees
+          seen[0] = here.mask;
+          if constexpr (CAUSAL) seen[0] &= low_mask(w.limit[0] - tile * kTile);
+          uint32_t y[4];
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            const uint32_t two = seen[0] >> (16 * (m >> 1) + 4 * g + 2 * (m & 1));
+            y[m] = (two & 1u) * 0x3f80u | ((two >> 1) & 1u) * 0x3f800000u;
+          }
+          hi[0] = as_bf16x8(make_uint4(y[0], y[1], y[2], y[3]));
+          lo[0] = as_bf16x8(make_uint4(0u, 0u, 0u, 0u));
+        }
+        read_v(v, ring + G::kRows);
+#pragma unroll
+        for (int ct = 0; ct < kCT; ++ct) {
+          const uint4 x = __builtin_bit_cast(uint4, v[ct]);
+          v[ct] = as_bf16x8(make_uint4(sorted_out(x.x, which), sorted_out(x.y, which), sorted_out(x.z, which), sorted_out(x.w, which)));
+          __builtin_amdgcn_sched_barrier(0);  // (one at a time: registers)
+        }
+        multiply_v(w, v, hi, lo);
+      }
+      if (which == 0) break;
+#pragma unroll
+      for (int ct = 0; ct < kCT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t bit = w.o[0][ct][i] > 0.f ? 1u << (4 * ct + i) : 0u;
+          up |= which == 2 ? bit : 0u;
+          down |= which == 2 ? 0u : bit;
+        }
+    }
+#pragma unroll
+    for (int ct = 0; ct < kCT; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t bit = 1u << (4 * ct + i);
+        w.o[0][ct][i] += ((up & bit) ? INFINITY : 0.f) + ((down & bit) ? -INFINITY : 0.f);
       }
   };
 
   // Writes out what the wavefront has of unit u.  Lane (c, g) has of row c the columns 16 ct + 4 g + i of bf16 rows, (4 g + i) * D / 16 + ct of codes.
-  auto end_piece = [&](int start, int end) __attribute__((always_inline)) {
+  auto end_piece = [&](const auto& w, int n0, int start, int end) __attribute__((always_inline)) {
     const bool whole = start == 0 && end == u.q.tiles;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int at = (u.qg * NT + n) * 16 + c, i = at / p.group, head = head_of(u) * p.group + at - i * p.group;
+    for (int n = 0; n < w.kN; ++n) {
+      const int at = (u.qg * NT + n0 + n) * 16 + c, i = at / p.group, head = head_of(u) * p.group + at - i * p.group;
       if (i >= u.q.n) continue;
-      const float inv = !whole ? 1.f : (l_run[n] == 0.f ? 0.f : 1.f / l_run[n]);
+      const float inv = !whole ? 1.f : (w.l[n] == 0.f ? 0.f : 1.f / w.l[n]);
       uint16_t* out = p.out + (int64_t)(u.q.first + i) * p.osn + (int64_t)head * p.osh;
-      const int64_t row = (int64_t)(2 * wave_id + (start == 0)) * p.unit_rows + 16 * n + c;
+      const int64_t row = (int64_t)(2 * wave_id + (start == 0)) * p.unit_rows + 16 * (n0 + n) + c;
       float* part = p.part_o + row * D;
       auto put = [&](int column, const floatx4& x) __attribute__((always_inline)) {  // four columns
         if (whole)
@@ -602,38 +625,50 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
-          for (int ct = 0; ct < kCT; ct += 4) put((4 * g + m) * kCT + ct, floatx4{o[n][ct][m], o[n][ct + 1][m], o[n][ct + 2][m], o[n][ct + 3][m]});
+          for (int ct = 0; ct < kCT; ct += 4) put((4 * g + m) * kCT + ct, floatx4{w.o[n][ct][m], w.o[n][ct + 1][m], w.o[n][ct + 2][m], w.o[n][ct + 3][m]});
       } else {
 #pragma unroll
-        for (int ct = 0; ct < kCT; ++ct) put(16 * ct + 4 * g, o[n][ct]);
+        for (int ct = 0; ct < kCT; ++ct) put(16 * ct + 4 * g, w.o[n][ct]);
       }
       if (g == 0) {
         if (!whole)
-          p.part_ml[row] = make_float2(m_run[n], l_run[n]);
+          p.part_ml[row] = make_float2(w.m[n], w.l[n]);
         else if (p.lse)
-          p.lse[(int64_t)(u.q.first + i) * (p.H * p.group) + head] = l_run[n] == 0.f ? -INFINITY : (m_run[n] + __builtin_amdgcn_logf(l_run[n])) * kLn2;
+          p.lse[(int64_t)(u.q.first + i) * (p.H * p.group) + head] = w.l[n] == 0.f ? -INFINITY : (w.m[n] + __builtin_amdgcn_logf(w.l[n])) * kLn2;
       }
     }
   };
 
+  // of whom the pieces of a unit are whose last tile is the one `last` of the wavefront
+  auto say_whose = [&](int start, int last) __attribute__((always_inline)) {
+    if (t < u.q.tiles || lane != 0) return;
+    int2 whose = make_int2(0, 0);
+    if (start > 0) {
+      whose.x = shares.of(begin + last - (u.q.tiles - 1));
+      whose.y = worker - whose.x + 1;
+    }
+    p.whose[((int64_t)u.r * p.H + head_of(u)) * p.most_groups + u.qg] = whose;
+  };
+
   // A stage's K is requested again as soon as it is in registers, its V likewise.  Loads return in order: a wait leaves those under way that were
   // requested behind what is waited for.  Where no more are requested it leaves none.
-  int start = t;
+  int start = t, i = -kDepth;
+  QueryRows<D, NT> w;
 #pragma unroll 1
-  for (int i = -kDepth; i < n_tiles; ++i) {
+  for (; i < n_tiles; ++i) {
     const bool more = asked < n_tiles, work = i >= 0;
     char* stage = stage_of(i);
     uint32_t mask = 0u;
     floatx4 acc[NT][2], ek[2], ev[2];
     if (work) {
       mask = (uint32_t)__builtin_amdgcn_readlane(masks, i & (kDepth - 1));
-      if (t == start) begin_unit();
+      if (t == start) begin_unit(w, 0);
       if (i + kDepth <= n_tiles)
         wait_loads_but<G::kLoads + (kDepth - 1) * G::kTileLoads>();
       else
         wait_loads();
       if (mask != 0u) {
-        multiply_k(acc, stage);
+        multiply_k(acc, w, stage);
         if constexpr (QUANT) read_exponents(ek, ev, stage + 2 * G::kRows, lane);
       }
     }
@@ -643,31 +678,48 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
     if (work) {
       bf16x8 hi[NT], lo[NT];
       uint32_t seen[NT];
-      if (mask != 0u) softmax(acc, mask, ek, ev, hi, lo, seen);
+      if (mask != 0u) softmax(acc, w, t, mask, ek, ev, hi, lo, seen);
       if (more)
         wait_loads_but<(kDepth - 1) * G::kTileLoads + G::kTileLoads - G::kLoads>();
       else
         wait_loads();
-      if (mask != 0u) multiply_v(stage + G::kRows, mask, hi, lo, seen);
+      if (mask != 0u) {
+        bf16x8 v[kCT];
+        read_v(v, stage + G::kRows);
+        multiply_v(w, v, hi, lo);
+      }
     }
     __builtin_amdgcn_sched_barrier(0);
     if (more) request_v();
     if (work) {
       ++t;
       if (t >= u.q.tiles || i == n_tiles - 1) {
-        if (t >= u.q.tiles && lane == 0) {  // of whom the pieces are
-          int2 whose = make_int2(0, 0);
-          if (start > 0) {
-            whose.x = shares.of(begin + i - (u.q.tiles - 1));
-            whose.y = worker - whose.x + 1;
-          }
-          p.whose[((int64_t)u.r * p.H + head_of(u)) * p.most_groups + u.qg] = whose;
-        }
-        end_piece(start, t);
+        if (not_finite(w)) break;
+        say_whose(start, i);
+        end_piece(w, 0, start, t);
         start = t = 0;
         if (i < n_tiles - 1) next_unit(u);
       }
     }
+  }
+  if (i == n_tiles) return;
+
+  wait_loads();  // those of tiles behind, which are requested again
+  same_lane();
+#pragma unroll 1
+  for (;;) {
+#pragma unroll 1
+    for (int n = 0; n < NT; ++n) {
+      QueryRows<D, 1> one;
+      repeat(one, n, start, t);
+      end_piece(one, n, start, t);
+    }
+    say_whose(start, i);
+    if (i == n_tiles - 1) return;
+    next_unit(u);
+    start = 0;
+    t = min(u.q.tiles, n_tiles - 1 - i);
+    i += t;
   }
 }
 
@@ -697,9 +749,9 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
 #pragma unroll
   for (int v = 0; v < kVec; ++v) o[v] = 0.f;
   const int mine = NW == 1 ? n : (n - wave + NW - 1) / NW, first = NW == 1 ? 0 : wave;
+  auto slot_row = [&](int j) __attribute__((always_inline)) { return (int64_t)(2 * (((w0 + j) << p.log_bundle) + in_bundle) + (j == 0)) * p.unit_rows + in_unit; };
 #pragma unroll 1
   for (int k0 = 0; k0 < mine; k0 += kAhead) {
-    auto slot_row = [&](int j) __attribute__((always_inline)) { return (int64_t)(2 * (((w0 + j) << p.log_bundle) + in_bundle) + (j == 0)) * p.unit_rows + in_unit; };
     const int j = first + (k0 + min(lane, kAhead - 1)) * NW;
     const int j_there = min(j, n - 1);
     float2 ml = p.part_ml[slot_row(j_there)];
@@ -737,6 +789,26 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
       for (int v = 0; v < kVec; ++v) o[v] = take ? __builtin_fmaf(w, y[k][v], o[v]) : o[v];
     }
   }
+  // An infinity or a NaN of a piece stays one, also where the piece's weight is zero in 32 bits.  One look at the end: they are rare
+  auto stays = [](float x) __attribute__((always_inline)) { return !(fabsf(x) < INFINITY); };
+  auto spoilt = [&]() __attribute__((always_inline)) {
+    bool some = false;
+#pragma unroll
+    for (int v = 0; v < kVec; ++v) some |= stays(o[v]);
+    return __builtin_expect(__ballot(some) != 0ull, 0);
+  };
+  if (spoilt()) {
+#pragma unroll
+    for (int v = 0; v < kVec; ++v) o[v] = 0.f;
+#pragma unroll 1
+    for (int j = first; j < n; j += NW) {
+      const float2 ml = p.part_ml[slot_row(j)];
+      if (ml.y == 0.f) continue;
+      const float f = __builtin_amdgcn_exp2f(ml.x - m_run), *src = p.part_o + slot_row(j) * D + lane * kVec;
+#pragma unroll
+      for (int v = 0; v < kVec; ++v) o[v] += stays(src[v]) ? src[v] : f * src[v];
+    }
+  }
   if constexpr (NW > 1) {
     if (lane == 0) ml_sh[wave] = make_float2(m_run, l_run);
 #pragma unroll
@@ -758,6 +830,20 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
       l_run += f * ml.y;
 #pragma unroll
       for (int v = 0; v < kVec; ++v) o[v] += f * o_sh[w][lane * kVec + v];
+    }
+    if (spoilt()) {
+#pragma unroll
+      for (int v = 0; v < kVec; ++v) o[v] = 0.f;
+#pragma unroll 1
+      for (int w = 0; w < NW; ++w) {
+        const float2 ml = ml_sh[w];
+        const float f = ml.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml.x - m_use);
+#pragma unroll
+        for (int v = 0; v < kVec; ++v) {
+          const float x = o_sh[w][lane * kVec + v];
+          o[v] += stays(x) ? x : f * x;
+        }
+      }
     }
   }
   const float inv = l_run == 0.f ? 0.f : 1.f / l_run;

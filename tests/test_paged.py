@@ -550,6 +550,85 @@ def test_memory_that_was_never_written_does_not_reach_earlier_rows(d, group, pag
             check_attention(out[at:at + 1, h].cpu(), lse[at:at + 1, h].cpu(), ref)
 
 
+def spoil(pool, r, j, column, value):
+    """Writes an infinity or a NaN into V of position j of request r (codes: the NaN code)."""
+    page, at = int(pool.table[r, j // pool.page]), j % pool.page
+    pool.v[page, :, at, column] = 0x7f if pool.quant else value
+
+
+def check_not_finite(out, lse, q, k, v, seen):
+    """One row and head against the definition: an infinity or a NaN of V comes out where a key that the row sees has it, infinities of both signs as NaN."""
+    up, down = ((seen[:, None] & ((v == x) | v.isnan())).any(0) for x in (math.inf, -math.inf))
+    assert torch.equal(out == math.inf, up & ~down) and torch.equal(out == -math.inf, down & ~up) and torch.equal(out.isnan(), up & down)
+    finite = torch.where(v.isfinite(), v, 0.0)
+    check_attention(out.masked_fill(up | down, 0.0)[None], lse[None], attend64(q[None].double(), k, finite.masked_fill((up | down)[None], 0.0), seen[None]))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("lens,rows,H,group,d,page,far", [
+    ([100], None, 1, 1, 128, 16, False),
+    ([64, 33], [3, 1], 2, 4, 64, 32, False),
+    ([100, 7], [25, 2], 1, 7, 128, 5, False),  # 32 query rows at a time, pages that end within sixteen rows
+    ([5000], None, 4, 2, 128, 100, False),  # pieces of many wavefronts
+    ([3000, 40], [20, 1], 2, 2, 64, 16, True),  # keys of later tiles far above those with the infinities, whose weights are zero in 32 bits
+    ([3000], None, 1, 1, 128, 16, True),
+])
+def test_values_that_are_not_finite(lens, rows, H, group, d, page, far, causal, quant):
+    """Infinities and NaN in V, in whole tiles and in cut ones, at the first key, in the middle, at the last: the same result wherever the borders of tiles, pieces
+    and limits lie."""
+    pool = Pages(lens, -(-max(lens) // page), page, H, d, quant, False, seed=3).fill()
+    if far and not quant:
+        pool.k[:, :, :, 0] = torch.where(pool.k[:, :, :, 0].isnan(), math.nan, 0.0).bfloat16()
+        for j in (2000, 2990):
+            pool.k[int(pool.table[0, j // page]), :, j % page, 0] = 90.0 if j == 2000 else 120.0
+    n = lens[0]
+    for j, column, value in ((0, 1, math.inf), (n // 2, 2, -math.inf), (n // 2 + 1, 3, math.nan), (n - 1, 4, math.inf), (3, 5, math.inf), (n - 2, 5, -math.inf),
+                             (2, d - 1, -math.inf), (n // 3, d // 2, math.inf), (n // 3 + 40 if n > 200 else n // 3, d // 2 + 1, math.inf)):
+        spoil(pool, 0, j, column, value)
+    batch = batch_of(lens, pool.table, rows)
+    total, heads = batch.n_rows, H * group
+    q = torch.randn((total, heads, d), generator=torch.Generator().manual_seed(2)).bfloat16()
+    if far:
+        q[:, :, 0] = 64.0
+    out, lse = torch.empty((total, heads, d), dtype=torch.bfloat16, device=DEV), torch.empty((total, heads), device=DEV)
+    fb.paged_attn(q.to(DEV), pool.cache, batch, causal, out, lse, workspace(pool.cache, batch, heads))
+    out, lse = out.cpu(), lse.cpu()
+    for r in range(len(lens)):
+        j, k, v = pool.rows(r, lens[r])
+        for at, _, p in [x for x in places(lens, rows) if x[1] == r]:
+            for h in range(heads):
+                check_not_finite(out[at, h], lse[at, h], q[at, h], k[:, h // group], v[:, h // group], j <= p if causal else j >= 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group,rows", [(1, 1), (9, 3)])
+def test_requests_beside_one_that_is_not_finite(group, rows):
+    """600 requests, several to a wavefront: those with infinities and NaN get them, those before and behind are as without."""
+    n, H, d, page = 600, 8, 64, 16
+    lens = [70 + i % 50 for i in range(n)]
+    pool = Pages(lens, 8, page, H, d, False, True, seed=1, spare=0).fill()
+    batch = batch_of(lens, pool.table, [rows] * n if rows > 1 else None)
+    q = torch.randn((n * rows, H * group, d), generator=torch.Generator().manual_seed(2)).bfloat16()
+    results = []
+    for spoilt in (False, True):
+        if spoilt:
+            for r, j, column, value in ((3, 0, 1, math.inf), (4, 69, 2, math.nan), (100, 40, 0, -math.inf), (101, 1, 63, math.inf), (350, 33, 7, math.inf), (599, 1, 9, -math.inf)):
+                spoil(pool, r, j, column, value)
+        out, lse = torch.empty((n * rows, H * group, d), dtype=torch.bfloat16, device=DEV), torch.empty((n * rows, H * group), device=DEV)
+        fb.paged_attn(q.to(DEV), pool.cache, batch, True, out, lse, workspace(pool.cache, batch, H * group))
+        results.append((out.cpu().view(n, rows, H * group, d), lse.cpu().view(n, rows, H * group)))
+    there = torch.tensor([r in (3, 4, 100, 101, 350, 599) for r in range(n)])
+    (clean, clean_lse), (out, lse) = results
+    assert torch.equal(lse, clean_lse) and torch.equal(out[~there], clean[~there])
+    for r in there.nonzero()[:, 0].tolist() + [0, 2, 5, 99, 349, 598]:
+        j, k, v = pool.rows(r, lens[r])
+        for i in range(rows):
+            for h in range(0, H * group, 5):
+                check_not_finite(out[r, i, h], lse[r, i, h], q[r * rows + i, h], k[:, h // group], v[:, h // group], j <= lens[r] - rows + i)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("max_rows", [1, 2])
