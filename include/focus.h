@@ -426,7 +426,8 @@ typedef struct focus_rotation {
 /*
  * Rows turned by their positions: the Q and K_new that the other entry points take.
  *   X    [dev] bf16 [n_rows, n_heads, d], strides x_stride_* in elements, multiples of 8;  d = head_dim: 64 or 128
- *   out  [dev] bf16 [n_rows, n_heads, d], strides o_stride_* (a head-major [H, n, d] is one of them); it may be X itself with the same strides
+ *   out  [dev] bf16 [n_rows, n_heads, d], strides o_stride_* (a head-major [H, n, d] is one of them); it may be X itself with the same strides.  Rows
+ *             that are written, by this call or the next two, are clear of one another: each stride is at least what the rows along the smaller ones span
  *   positions [dev] int32[n_rows] or NULL (= 0, 1, 2, ...): row i is at position pos_base + positions[i].  Rows with positions[i] < 0 are
  *             left out (nothing is written), so that the active_idx of focus_select_queries may be handed over as it is, with pos_base =
  *             the position of the generation block's first token
@@ -484,7 +485,7 @@ typedef struct focus_paged_batch {
  *                of it); both NULL with n_q_heads = 0
  * A row without a position (positions[i] < 0) is left out, Q included; of one whose cache row does not exist K and V are left out.  Of rows of
  * one request with the same position the last one's K and V stay.  A page that is listed more than once must not be written through two entries.
- * A cache whose heads or pages share rows (strides of 0, v = k) can be read by focus_paged_attn, not written.
+ * A cache whose heads or pages share rows (strides of 0, or less than the rows along the smaller ones span, v = k) can be read by focus_paged_attn, not written.
  * ceil(max_rows / 4) * n_req <= 2^25: max_rows is a bound that the launch is made for.
  */
 int focus_paged_append(const focus_paged_cache* cache, const focus_paged_batch* batch, const void* K_new, const void* V_new, int64_t new_stride_h,

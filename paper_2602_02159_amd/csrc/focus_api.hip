@@ -543,11 +543,30 @@ static int check_head_dim(const char* who, int32_t head_dim) {
   return FOCUS_OK;
 }
 
-// bf16 rows [n_rows, heads, d] in any order
-static int check_rows(const char* who, const char* name, const void* t, int64_t stride_h, int64_t stride_n, int32_t heads = 1, int32_t n_rows = 1) {
-  if ((heads > 1 && stride_h == 0) || (n_rows > 1 && stride_n == 0)) return fail(FOCUS_EINVAL, "%s: rows of %s lie on one another", who, name);
+// Whether rows of `size` elements are clear of one another: every stride is at least what the rows along the smaller ones span, as in any tensor that is
+// a permuted part of a contiguous one.  Strides along a single row mean nothing.
+struct Axis {
+  int64_t n, stride;
+};
+template <int N>
+static bool rows_apart(int64_t size, Axis (&axes)[N]) {
+  std::sort(axes, axes + N, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+  __int128 span = size;
+  for (const Axis& a : axes) {
+    if (a.n <= 1) continue;
+    if (a.stride < span) return false;
+    span += (__int128)(a.n - 1) * a.stride;
+  }
+  return true;
+}
+
+// bf16 rows [n_rows, heads, d] in any order; of a tensor that is only read they may lie on one another (heads = n_rows = 1)
+static int check_rows(const char* who, const char* name, const void* t, int64_t stride_h, int64_t stride_n, int32_t heads = 1, int32_t n_rows = 1,
+                      int32_t head_dim = 0) {
   if (!t) return fail(FOCUS_EINVAL, "%s: %s is NULL", who, name);
   if ((stride_h & 7) || (stride_n & 7) || stride_h < 0 || stride_n < 0) return fail(FOCUS_EINVAL, "%s: strides of %s invalid or not multiples of 8", who, name);
+  Axis axes[2] = {{heads, stride_h}, {n_rows, stride_n}};
+  if (!rows_apart(head_dim, axes)) return fail(FOCUS_EINVAL, "%s: rows of %s lie on one another", who, name);
   if (!aligned16(t)) return fail(FOCUS_EINVAL, "%s: pointers must be 16-byte aligned", who);
   return FOCUS_OK;
 }
@@ -1093,7 +1112,7 @@ int focus_rotary(const void* X, int64_t x_stride_h, int64_t x_stride_n, void* ou
   if (n_rows < 1 || n_rows > kTurnMaxRows) return fail(FOCUS_EINVAL, "%s: n_rows=%d not in [1, %d]", who, n_rows, kTurnMaxRows);
   if (n_heads < 1 || n_heads > 65535) return fail(FOCUS_EINVAL, "%s: n_heads=%d not in [1, 65535]", who, n_heads);
   if (int rc = check_rows(who, "X", X, x_stride_h, x_stride_n)) return rc;
-  if (int rc = check_rows(who, "out", out, o_stride_h, o_stride_n, n_heads, n_rows)) return rc;
+  if (int rc = check_rows(who, "out", out, o_stride_h, o_stride_n, n_heads, n_rows, head_dim)) return rc;
   if (X == out && (x_stride_h != o_stride_h || x_stride_n != o_stride_n)) return fail(FOCUS_EINVAL, "%s: in place, but with other strides", who);
   TurnRows p = {};
   p.Q = static_cast<const uint16_t*>(X);
@@ -1140,15 +1159,18 @@ int focus_paged_append(const focus_paged_cache* cache, const focus_paged_batch* 
   if (Q) {
     if (n_q_heads < 1 || n_q_heads > 65535) return fail(FOCUS_EINVAL, "%s: n_q_heads=%d not in [1, 65535]", who, n_q_heads);
     if (int rc = check_rows(who, "Q", Q, q_stride_h, q_stride_n)) return rc;
-    if (int rc = check_rows(who, "Q_out", Q_out, qo_stride_h, qo_stride_n, n_q_heads, batch->n_rows)) return rc;
+    if (int rc = check_rows(who, "Q_out", Q_out, qo_stride_h, qo_stride_n, n_q_heads, batch->n_rows, cache->head_dim)) return rc;
     if (Q == Q_out && (q_stride_h != qo_stride_h || q_stride_n != qo_stride_n)) return fail(FOCUS_EINVAL, "%s: in place, but with other strides", who);
   }
   if (ceil_div64(std::min(batch->max_rows, batch->n_rows), 4) * batch->n_req > kTurnMaxRows)
     return fail(FOCUS_EUNSUPPORTED, "%s: n_req=%d requests of up to max_rows=%d rows are too many", who, batch->n_req, batch->max_rows);
-  const bool heads = cache->n_heads > 1, pages = cache->n_pages > 1;
-  if (cache->k == cache->v || (heads && (cache->k_stride_h == 0 || cache->v_stride_h == 0)) || (pages && (cache->k_stride_p == 0 || cache->v_stride_p == 0)) ||
-      (cache->k_exp && (cache->k_exp == cache->v_exp || (heads && cache->exp_stride_h == 0) || (pages && cache->exp_stride_p == 0))))
-    return fail(FOCUS_EINVAL, "%s: rows of the cache lie on one another", who);
+  Axis k_axes[3] = {{cache->n_pages, cache->k_stride_p}, {cache->n_heads, cache->k_stride_h}, {cache->page, cache->k_stride_n}};
+  Axis v_axes[3] = {{cache->n_pages, cache->v_stride_p}, {cache->n_heads, cache->v_stride_h}, {cache->page, cache->v_stride_n}};
+  Axis e_axes[3] = {{cache->n_pages, cache->exp_stride_p}, {cache->n_heads, cache->exp_stride_h}, {cache->page, cache->exp_stride_n}};
+  const char* what = !rows_apart(cache->head_dim, k_axes) ? "rows of k" : (!rows_apart(cache->head_dim, v_axes) ? "rows of v" : nullptr);
+  if (!what && cache->k_exp && !rows_apart(1, e_axes)) what = "exponents";
+  if (!what && (cache->k == cache->v || (cache->k_exp && cache->k_exp == cache->v_exp))) what = "k and v";
+  if (what) return fail(FOCUS_EINVAL, "%s: %s lie on one another", who, what);
   TurnRows p = {};
   p.Q = static_cast<const uint16_t*>(Q);
   p.Qo = static_cast<uint16_t*>(Q_out);
@@ -1192,7 +1214,7 @@ int focus_paged_attn(const void* Q, int64_t q_stride_h, int64_t q_stride_n, int3
   if (int rc = check_paged(who, cache, batch)) return rc;
   if (int rc = check_paged_queries(who, cache, batch, n_q_heads)) return rc;
   if (int rc = check_rows(who, "Q", Q, q_stride_h, q_stride_n)) return rc;
-  if (int rc = check_rows(who, "out", out, o_stride_h, o_stride_n, n_q_heads, batch->n_rows)) return rc;
+  if (int rc = check_rows(who, "out", out, o_stride_h, o_stride_n, n_q_heads, batch->n_rows, cache->head_dim)) return rc;
   const PagedBatch b = paged_batch(*batch);
   const PagedPlan plan = plan_paged_attn(cache->n_heads, n_q_heads / cache->n_heads, cache->head_dim, b, cache->page);
   if (!workspace || ws_bytes < plan.total || !aligned16(workspace))

@@ -185,6 +185,44 @@ def test_shared_rows_are_not_written(cache):
     assert "on one another" in fb.last_error()
 
 
+@pytest.mark.parametrize("heads,rows,d,sh,sn,fine", [
+    (4, 4, 64, 64, 256, True), (4, 4, 64, 256, 64, True), (4, 5, 64, 320, 64, True), (2, 4, 128, 136, 264, True), (2, 3, 128, 400, 128, True), (1, 4, 64, 0, 64, True),
+    (4, 1, 64, 64, 0, True), (1, 1, 128, 0, 0, True), (4, 4, 64, 8, 256, False), (2, 4, 128, 8, 128, False), (4, 4, 64, 64, 248, False), (4, 4, 64, 64, 192, False),
+    (4, 5, 64, 312, 64, False), (4, 4, 64, 256, 56, False), (1, 2, 128, 0, 120, False), (2, 1, 128, 120, 0, False), (3, 3, 64, 64, 64, False),
+    (2, 1 << 25, 64, 1 << 31, 64, True), (2, 1 << 25, 64, (1 << 31) - 8, 64, False), (65535, 2, 64, 1 << 58, 64, True)])
+def test_rows_that_are_written_are_clear_of_one_another(heads, rows, d, sh, sn, fine):
+    """Strides less than what the rows along the smaller ones span are refused, others are not: by brute force where there are few rows.  The calls that go past this
+    check end at a later one."""
+    if heads * rows < 1000:
+        at = sorted(h * sh + i * sn for h in range(heads) for i in range(rows))
+        assert fine == all(b - a >= d for a, b in zip(at, at[1:]))
+    L, at_8 = fb.lib(), C.c_void_p((1 << 20) + 8)  # (not aligned: the next check)
+    b = _batch(n_rows=rows, n_req=1, row_start=1 << 20, max_rows=1)
+    c = _cache(head_dim=d, n_heads=1, v=1 << 24, k_stride_n=d, v_stride_n=d, k_stride_p=16 * d, v_stride_p=16 * d)
+    calls = [lambda: L.focus_rotary(P, 64, 256, at_8, sh, sn, rows, heads, d, None, 0, C.byref(_rot()), None),
+             lambda: L.focus_paged_append(C.byref(c), C.byref(b), P, P, 64, 256, None, P, 64, 256, at_8, sh, sn, heads, None),
+             lambda: L.focus_paged_attn(P, 64, 256, heads, C.byref(c), C.byref(b), 0, at_8, sh, sn, None, P, 1 << 40, None)]
+    for call in calls:
+        assert call() == fb.FOCUS_EINVAL and ("aligned" if fine else "on one another") in fb.last_error()
+
+
+@pytest.mark.parametrize("kw,fine", [
+    (dict(), True), (dict(k_stride_p=64, k_stride_h=8 * 64, k_stride_n=8 * 4 * 64), True), (dict(k_stride_h=64, k_stride_n=4 * 64), True), (dict(k_stride_p=8192, k_stride_n=72, k_stride_h=1152), True),
+    (dict(k_stride_h=8), False), (dict(k_stride_h=960), False), (dict(v_stride_p=2048), False), (dict(k_stride_p=4088), False), (dict(v_stride_h=64), False), (dict(v_stride_n=72), False),
+    (dict(n_heads=1, v_stride_h=8), True), (dict(n_pages=1, v_stride_p=0), True), (dict(page=1, k_stride_n=1 << 20), True)])
+def test_caches_whose_rows_lie_on_one_another_are_not_written(kw, fine):
+    c = _cache(**kw)  # k = v, which is refused last
+    assert fb.lib().focus_paged_append(C.byref(c), C.byref(_batch()), P, P, 64, 256, None, None, 0, 0, None, 0, 0, 0, None) == fb.FOCUS_EINVAL
+    assert ("k and v" if fine else "rows of " + next(iter(kw))[0]) + " lie on one another" in fb.last_error()
+
+
+@pytest.mark.parametrize("strides,fine", [((64, 16, 1), True), ((64, 1, 4), True), ((1, 128, 8), True), ((64, 15, 1), False), ((63, 16, 1), False), ((64, 16, 4), False), ((64, 2, 1), False)])
+def test_exponents_that_lie_on_one_another_are_not_written(strides, fine):
+    c = _cache(k_exp=1 << 25, v_exp=1 << 26, exp_stride_p=strides[0], exp_stride_h=strides[1], exp_stride_n=strides[2])
+    assert fb.lib().focus_paged_append(C.byref(c), C.byref(_batch()), P, P, 64, 256, None, None, 0, 0, None, 0, 0, 0, None) == fb.FOCUS_EINVAL
+    assert ("k and v" if fine else "exponents") + " lie on one another" in fb.last_error()
+
+
 def test_frequencies():
     f = fb.rotary_freqs(10000.0, 64)
     assert torch.allclose(f, 10000.0 ** (-torch.arange(0, 64, 2, dtype=torch.float64) / 64), rtol=1e-14)
