@@ -8,6 +8,7 @@ if the HIP library is not built, importing this module's `lib()` fails.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 import torch
@@ -569,8 +570,8 @@ def quant_layer(q, focus_idx, active_idx, counts, cache: QuantCache, kbar, shape
 
 
 # ---- requests over a paged cache
-def rotary_freqs(base: float, rot_dim: int, factor: float = 1.0, orig_len: int = 1, turns_low: float = 0.0, turns_high: float = 0.0) -> torch.Tensor:
-    """Frequencies for make_rotation, float64 on the host: see focus_helper_rotary."""
+def rotary_freqs(base: float, rot_dim: int, factor: float = 1.0, orig_len: int = 1, turns_low: float = math.inf, turns_high: float = math.inf) -> torch.Tensor:
+    """Frequencies for make_rotation, float64 on the host: see focus_helper_rotary.  Without turns_low and turns_high all are divided by `factor`."""
     values = (C.c_double * max(rot_dim // 2, 1))()
     _check(lib().focus_helper_rotary(base, rot_dim, factor, orig_len, turns_low, turns_high, values))
     return torch.tensor(list(values)[:rot_dim // 2], dtype=torch.float64)

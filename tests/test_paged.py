@@ -239,6 +239,14 @@ def test_frequencies():
             fb.rotary_freqs(*bad)
 
 
+def test_frequencies_are_all_divided_where_no_turns_are_given():
+    f = fb.rotary_freqs(10000.0, 64)
+    assert torch.allclose(fb.rotary_freqs(10000.0, 64, 4.0), f / 4, rtol=1e-14) and torch.allclose(fb.rotary_freqs(10000.0, 64, 4.0, 8192), f / 4, rtol=1e-14)
+    assert torch.allclose(fb.rotary_freqs(10000.0, 64, 4.0, 8192, 0.0, 0.0), f, rtol=1e-14)  # a step at no turn at all: none is
+    with pytest.raises(fb.FocusError):
+        fb.rotary_freqs(10000.0, 64, 4.0, 8192, turns_high=4.0)  # half of a range
+
+
 # ---- rotation ---------------------------------------------------------------------------------------------------------------
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,heads,d,rot,interleaved,scale,first", [
