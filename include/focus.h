@@ -439,7 +439,8 @@ int focus_rotary(const void* X, int64_t x_stride_h, int64_t x_stride_n, void* ou
 /*
  * Frequencies of focus_rotation, [host]: freq[j] = base^(-2j / rot_dim), of which those that turn fewer than turns_low times in orig_len positions are
  * divided by `factor`, those that turn more than turns_high times stay, and those between are mixed in proportion (a context longer than
- * the one that was trained on).  turns_low = turns_high: a step there; infinite ones: all are divided; factor = 1: none is changed.
+ * the one that was trained on).  turns_low = turns_high: a step there; infinite ones: all are divided; factor = 1: none is changed.  Refused: a range without
+ * a lower end (turns_low = -inf < turns_high), and what gives frequencies that are not finite.
  */
 int focus_helper_rotary(double base, int32_t rot_dim, double factor, int32_t orig_len, double turns_low, double turns_high, double* freq);
 

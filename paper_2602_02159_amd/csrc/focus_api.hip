@@ -1138,11 +1138,15 @@ int focus_helper_rotary(double base, int32_t rot_dim, double factor, int32_t ori
   if (rot_dim < 2 || (rot_dim & 1)) return fail(FOCUS_EINVAL, "%s: rot_dim=%d", who, rot_dim);
   if (!(base > 0.0) || !(factor > 0.0) || std::isinf(base) || std::isinf(factor) || orig_len < 1 || !(turns_low <= turns_high))
     return fail(FOCUS_EINVAL, "%s: base and factor are positive numbers, orig_len at least 1, turns_low <= turns_high", who);
-  for (int32_t j = 0; j < rot_dim / 2; ++j) {
+  if (std::isinf(turns_low) && turns_low < 0.0 && turns_high > turns_low) return fail(FOCUS_EINVAL, "%s: a range of turns without a lower end has no proportions", who);
+  auto frequency = [&](int32_t j) {
     const double f = std::pow(base, -2.0 * j / rot_dim), turns = orig_len * f / (2.0 * 3.14159265358979323846);
     const double whole = turns >= turns_high ? 1.0 : (turns <= turns_low ? 0.0 : (turns - turns_low) / (turns_high - turns_low));  // share that stays
-    freq[j] = f * (whole + (1.0 - whole) / factor);
-  }
+    return f * (whole + (1.0 - whole) / factor);
+  };
+  for (int32_t j = 0; j < rot_dim / 2; ++j)
+    if (!std::isfinite(frequency(j))) return fail(FOCUS_EINVAL, "%s: frequency %d is not a finite number", who, j);
+  for (int32_t j = 0; j < rot_dim / 2; ++j) freq[j] = frequency(j);
   return FOCUS_OK;
 }
 

@@ -247,6 +247,24 @@ def test_frequencies_are_all_divided_where_no_turns_are_given():
         fb.rotary_freqs(10000.0, 64, 4.0, 8192, turns_high=4.0)  # half of a range
 
 
+@pytest.mark.parametrize("bad", [(10000.0, 16, 4.0, 8192, -math.inf, 4.0), (10000.0, 16, 4.0, 8192, -math.inf, math.inf), (10000.0, 16, 4.0, 8192, -math.inf, -1.0),
+                                 (5e-324, 64), (10000.0, 64, 5e-324, 8192, 1.0, 4.0), (10000.0, 64, 4.0, 8192, math.nan, 4.0), (10000.0, 64, 4.0, 8192, 1.0, math.nan)])
+def test_frequencies_are_finite_or_refused(bad):
+    with pytest.raises(fb.FocusError):
+        fb.rotary_freqs(*bad)
+
+
+@pytest.mark.parametrize("low,high", [(-math.inf, -math.inf), (-1.0, 4.0), (1.0, math.inf), (0.0, 0.0), (math.inf, math.inf), (-1e300, 1e300)])
+def test_frequencies_of_unusual_ranges(low, high):
+    """Between what stays and what is divided, in order, for every range with two ends."""
+    f, g = fb.rotary_freqs(10000.0, 64), fb.rotary_freqs(10000.0, 64, 4.0, 8192, low, high)
+    assert bool(((g >= f / 4 * (1 - 1e-14)) & (g <= f * (1 + 1e-14))).all())
+    share = (g / f - 0.25) / 0.75
+    assert bool((share.diff() <= 1e-12).all())  # fewer turns, less of it stays
+    if low == high:
+        assert torch.allclose(g, f / 4 if low > 0 else f, rtol=1e-14)
+
+
 # ---- rotation ---------------------------------------------------------------------------------------------------------------
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,heads,d,rot,interleaved,scale,first", [
