@@ -19,6 +19,11 @@ import torch
 from . import binding as fb
 
 
+def _current_stream(buffers: torch.Tensor) -> int:
+    """The current stream.  Its kernels run on the current device, so that an object's buffers have to be there.  (A graph runs where it was captured.)"""
+    return fb._raw_stream(fb._device_of(buffers, "buffers"))
+
+
 class FocusStep:
     """Buffers and call sequence for one step.
 
@@ -139,7 +144,7 @@ class FocusStep:
     def issue(self, stage: str, layer: int | None = None):
         """Enqueue one stage (all layers, or one) on the current stream."""
         calls = self.calls[stage]
-        self._issue(calls if layer is None else calls[layer:layer + 1], torch.cuda.current_stream().cuda_stream)
+        self._issue(calls if layer is None else calls[layer:layer + 1], _current_stream(self.focus_idx))
 
     def sequence(self):
         """The step's calls in order: [confidence,] queries once, sinks once at the probe layer, then every layer."""
@@ -165,7 +170,7 @@ class FocusStep:
         if self._graph is not None:
             self._graph.replay()
         else:
-            self._issue(self.sequence(), torch.cuda.current_stream().cuda_stream)
+            self._issue(self.sequence(), _current_stream(self.focus_idx))
 
     def capture(self):
         """Capture the step into a HIP graph; later `run` calls replay it."""
@@ -174,7 +179,7 @@ class FocusStep:
         torch.cuda.synchronize()
         g = torch.cuda.CUDAGraph()
         with torch.cuda.graph(g):
-            self._issue(self.sequence(), torch.cuda.current_stream().cuda_stream)
+            self._issue(self.sequence(), _current_stream(self.focus_idx))
         self._graph = g
 
     def release_graph(self):
@@ -352,13 +357,13 @@ class FocusDecoder:
         if self._g_entry is not None:
             self._g_entry.replay()
         else:
-            FocusStep._issue(self.entry_calls, torch.cuda.current_stream().cuda_stream)
+            FocusStep._issue(self.entry_calls, _current_stream(self.focus_idx))
 
     def run_step(self):
         if self._g_step is not None:
             self._g_step.replay()
         else:
-            FocusStep._issue(self.step_calls, torch.cuda.current_stream().cuda_stream)
+            FocusStep._issue(self.step_calls, _current_stream(self.focus_idx))
 
     def capture(self):
         """Capture the block entry and the step into one HIP graph each (after one eager run of both, so that no module
@@ -372,7 +377,7 @@ class FocusDecoder:
         for calls in (self.entry_calls, self.step_calls):
             g = torch.cuda.CUDAGraph()
             with torch.cuda.graph(g):
-                FocusStep._issue(calls, torch.cuda.current_stream().cuda_stream)
+                FocusStep._issue(calls, _current_stream(self.focus_idx))
             graphs.append(g)
         self._g_entry, self._g_step = graphs
 
@@ -445,7 +450,7 @@ class FocusPagedStep:
 
     def issue(self, layer: int):
         """Enqueue the calls of one layer on the current stream."""
-        FocusStep._issue(self.layer_calls[layer], torch.cuda.current_stream().cuda_stream)
+        FocusStep._issue(self.layer_calls[layer], _current_stream(self.seq_len))
 
     def run(self):
         """Enqueue all layers (eagerly, or by replaying the captured graph)."""
@@ -459,7 +464,7 @@ class FocusPagedStep:
         if self._g_score is not None:
             self._g_score.replay()
         else:
-            FocusStep._issue(self.score_calls, torch.cuda.current_stream().cuda_stream)
+            FocusStep._issue(self.score_calls, _current_stream(self.seq_len))
 
     def capture(self):
         """Capture run and score into a HIP graph each, after one eager run of both on what the buffers hold (which writes rows to pages: call this
