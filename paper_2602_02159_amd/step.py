@@ -403,6 +403,9 @@ class FocusPagedStep:
                  max_rows: int = 1, n_rows: int | None = None, rotation=None, causal: bool = False, quantised: bool = False, scattered: bool = False,
                  vocab: int | None = None, top_n: int = 0):
         n_rows = n_req * max_rows if n_rows is None else n_rows
+        score_bytes = 0 if vocab is None else fb.token_logprobs_workspace(n_rows, vocab, top_n)
+        if vocab is not None and score_bytes == 0:
+            raise fb.FocusError(fb.FOCUS_EINVAL, f"focus_token_logprobs does not take n_rows={n_rows}, vocab={vocab}, top_n={top_n}")
         H, d, Hq = n_heads, head_dim, n_q_heads
         zeros = lambda dtype, *shape: torch.zeros(shape, dtype=dtype, device=device)
         bf16, f32, i32, u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
@@ -442,7 +445,7 @@ class FocusPagedStep:
             self.targets, self.masked = zeros(i32, n_rows), torch.ones(n_rows, dtype=u8, device=device)
             self.logprob, self.entropy = zeros(f32, n_rows), zeros(f32, n_rows)
             self.top_ids, self.top_logprobs = (zeros(i32, n_rows, top_n), zeros(f32, n_rows, top_n)) if top_n else (None, None)
-            self.score_space = torch.empty(max(fb.token_logprobs_workspace(n_rows, vocab, top_n), 256), dtype=u8, device=device)
+            self.score_space = torch.empty(max(score_bytes, 256), dtype=u8, device=device)
             self.score_calls.append((lib.focus_token_logprobs, (
                 p(self.logits), 0, self.logits.stride(0), p(self.targets), p(self.masked), n_rows, vocab, top_n, p(self.logprob), p(self.entropy),
                 p(self.top_ids), p(self.top_logprobs), p(self.score_space), self.score_space.numel())))

@@ -120,3 +120,17 @@ def test_a_rotation_of_another_device_is_refused():
     rotation.device = 1
     with pytest.raises(ValueError, match="rotation on device 1"):
         FocusPagedStep(1, 4, 16, 2, 4, 64, 2, 2, "cpu", rotation=rotation)
+
+
+@pytest.mark.parametrize("vocab,top_n", [(1000, 33), (1000, -1), (0, 0), ((1 << 21) + 1, 5)])
+def test_scores_of_unsupported_sizes_are_refused_at_once(vocab, top_n):
+    with pytest.raises(fb.FocusError, match=f"vocab={vocab}, top_n={top_n}"):
+        FocusPagedStep(1, 4, 16, 2, 4, 64, 2, 2, "cpu", vocab=vocab, top_n=top_n)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("head_dim,n_q_heads,page", [(80, 4, 16), (64, 5, 16), (64, 4, 65537)])
+def test_unsupported_sizes_are_refused_at_once(head_dim, n_q_heads, page):
+    FocusPagedStep(1, 4, 16, 2, 4, 64, 2, 2, DEV)  # this one is not
+    with pytest.raises(fb.FocusError):
+        FocusPagedStep(1, 4, page, 2, n_q_heads, head_dim, 2, 2, DEV)
