@@ -588,6 +588,7 @@ def make_rotation(freq: torch.Tensor, interleaved: bool = False, scale: float = 
 
 
 def _page_strides(t: torch.Tensor):
+    """Of a page, a head and a row (those of a single one mean nothing)."""
     return [0 if n == 1 else s for n, s in zip(t.shape[:3], t.stride()[:3])]
 
 
@@ -613,10 +614,11 @@ def make_paged_cache(k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor | Non
     if k_exp is not None:
         for t, name in ((k_exp, "k_exp"), (v_exp, "v_exp")):
             _need(t, torch.uint8, name)
-            if t.shape != k.shape[:3] or t.stride() != k_exp.stride() or t.get_device() != k.get_device():
+            if t.shape != k.shape[:3] or _page_strides(t) != _page_strides(k_exp) or t.get_device() != k.get_device():
                 raise ValueError(f"{name}: expected {list(k.shape[:3])} with common strides on {k.device}, got {list(t.shape)}, strides {t.stride()}")
         cache.k_exp, cache.v_exp = _ptr(k_exp), _ptr(v_exp)
-        cache.exp_stride_p, cache.exp_stride_h, cache.exp_stride_n = k_exp.stride()
+        cache.exp_stride_p, cache.exp_stride_h, n = _page_strides(k_exp)
+        cache.exp_stride_n = n if k_exp.shape[2] > 1 else 1
     cache.tensors, cache.device = (k, v, k_exp, v_exp), k.get_device()
     return cache
 

@@ -894,3 +894,22 @@ def test_binding_refuses():
         fb.paged_attn(x, pool.cache, batch, False, torch.empty_like(x), None, None)
     with pytest.raises(ValueError):
         fb.paged_attn(x, pool.cache, batch, False, torch.empty_like(x), torch.empty((1, 1), device=DEV), workspace(pool.cache, batch, 2))
+
+
+@pytest.mark.gpu
+def test_exponents_of_single_heads_and_rows():
+    """Strides along an axis of one mean nothing: exponents that differ in those alone are common, and an expanded one is no stride of zero."""
+    k, v = (torch.zeros((6, 1, 1, 64), dtype=torch.uint8, device=DEV) for _ in range(2))
+    k_exp = torch.zeros((6, 5, 7), dtype=torch.uint8, device=DEV)[:, :1, :1]
+    v_exp = torch.as_strided(torch.zeros(6 * 35, dtype=torch.uint8, device=DEV), (6, 1, 1), (35, 0, 0))
+    assert k_exp.stride() != v_exp.stride() and v_exp.stride(2) == 0
+    cache = fb.make_paged_cache(k, v, k_exp, v_exp)
+    table = torch.tensor([[4, 2, 5]], dtype=torch.int32, device=DEV)
+    batch = fb.make_paged_batch(torch.tensor([3], dtype=torch.int32, device=DEV), table, torch.tensor([0, 3], dtype=torch.int32, device=DEV), 3, 3)
+    x = torch.randn((2, 3, 1, 64), generator=torch.Generator().manual_seed(1)).bfloat16()
+    fb.paged_append(cache, batch, x[0].to(DEV), x[1].to(DEV))
+    for t, e, rows in ((k, k_exp, x[0]), (v, v_exp, x[1])):
+        codes, exps = e4m3_rows(rows[:, 0].float().numpy())
+        assert np.array_equal(t[[4, 2, 5], 0, 0].cpu().numpy(), codes) and np.array_equal(e[[4, 2, 5], 0, 0].cpu().numpy(), exps)
+    with pytest.raises(ValueError, match="common strides"):
+        fb.make_paged_cache(k, v, k_exp, torch.zeros((6, 1, 1), dtype=torch.uint8, device=DEV))
