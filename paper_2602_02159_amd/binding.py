@@ -690,6 +690,8 @@ def rotary(x, out, positions, pos_base: int, rotation: Rotation) -> None:
             raise ValueError(f"x: expected [rows, heads, d], got {list(shape)}")
         _explain_heads(device, shape[0], shape[2], (x, "x", shape[1]), (out, "out", shape[1]))
         _check_values(device, (positions, "positions", _I32, 0 if positions is None else shape[0]))
+    if not -0x80000000 <= pos_base <= 0x7fffffff:  # (ctypes would take the lower 32 bits)
+        raise ValueError(f"pos_base: {pos_base} is not a number of 32 bits")
     n, heads, d = shape
     status = lib().focus_rotary(x.data_ptr(), *_strides(shape, xs), out.data_ptr(), *_strides(shape, outs), n, heads, d, _ptr(positions), pos_base,
                                 C.byref(rotation), _raw_stream(device))

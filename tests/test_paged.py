@@ -913,3 +913,17 @@ def test_exponents_of_single_heads_and_rows():
         assert np.array_equal(t[[4, 2, 5], 0, 0].cpu().numpy(), codes) and np.array_equal(e[[4, 2, 5], 0, 0].cpu().numpy(), exps)
     with pytest.raises(ValueError, match="common strides"):
         fb.make_paged_cache(k, v, k_exp, torch.zeros((6, 1, 1), dtype=torch.uint8, device=DEV))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("first,fine", [(2 ** 31 - 1, True), (-2 ** 31, True), (2 ** 31, False), (2 ** 32, False), (-2 ** 31 - 1, False)])
+def test_positions_past_32_bits(first, fine):
+    x = torch.randn((2, 1, 64), generator=torch.Generator().manual_seed(1)).bfloat16().to(DEV)
+    out = torch.full_like(x, 3.0)
+    if not fine:
+        with pytest.raises(ValueError, match="pos_base"):
+            fb.rotary(x, out, None, first, rotation(64))
+        assert bool((out == 3.0).all())
+        return
+    fb.rotary(x, out, None, first, rotation(64))
+    assert np.array_equal(bits(out), bf16_bits(turned32(x.float().cpu().numpy(), np.arange(2) + first, freqs(64), False)))
