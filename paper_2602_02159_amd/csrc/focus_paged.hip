@@ -12,12 +12,15 @@
 //   O^T = V^T P^T bf16: column tile ct has the columns 16 ct + c, by transposed reads; codes: c * D / 16 + ct, D / 16 neighbouring codes of each of the
 //                 rows 4 g + i and 16 + 4 g + i, of which byte permutations put those of two rows next to each other
 // P is split into two bf16 numbers, p = hi + lo to 2^-17, and multiplied twice: rounded to one it would cost the result as much
-// again as its own rounding, and the matrix unit has nothing else to do (a tile is 16 KB from memory and 24 products).
+// again as its own rounding.  Of few query rows a tile is 16 KB from memory and 24 products, and the matrix unit has nothing else to do; of many, where the
+// products count, it is a third of them.
 //
-// What bounds it is HBM, every row read once: one request of 32 832 rows, 32 heads, 538 MB, in 83 us = 6.5 TB/s and 4.7 for the join; 64 of up to
-// 16 384 rows with 7 query heads on each of 4, 869 MB, in 135 and 6; eight-bit rows, 227 MB for 37 requests with 16 rows a unit, in 54 and 7: some 8 us are the
+// What bounds it is HBM, every row read once: one request of 32 832 rows, 32 heads, 538 MB, in 85 us = 6.4 TB/s and 4.7 for the join; 64 of up to
+// 16 384 rows with 7 query heads on each of 4, 869 MB, in 136 and 6; eight-bit rows, 227 MB for 37 requests with 16 rows a unit, in 60 and 6: some 8 us are the
 // start, 8 the pieces of 16 rows each (16 KB a wavefront), and half as many bytes a tile leave the instructions half the time.  A thousand
-// rows of four heads: 6.0 + 4.1 us, dependent round trips (lengths, table, rows, products; pieces).
+// rows of four heads: 6.2 + 4.1 us, dependent round trips (lengths, table, rows, products; pieces).  Many query rows of a K/V head are far from their bounds: each
+// 32 of them read all rows of the request again, those that causal limits hide from all 32 among them (64 rows of 4 query heads on each of 8, 32 requests of
+// 2048: 268 MB and 69 GFLOP, either 55 us, in 328, causal or not).
 #include <algorithm>
 
 #include "focus_codes.h"
@@ -228,8 +231,9 @@ __device__ __forceinline__ void request_rows_as(const uint8_t* base, int64_t str
     __builtin_amdgcn_global_load_lds((gptr_t)src, (lptr_t)(stage + i * 1024), 16, 0, POLICY);
   }
 }
-// Past the caches, unless several groups of query rows read the same bf16 rows: 25 rows of 7 heads, 16 requests of 4096 149 us past them, 118 through them, 64 of 4,
-// 32 requests of 2048 375 and 337; one group (64 requests, 7 heads) 145 and 164; eight-bit rows of several groups 110 and 118
+// Past the caches, unless several groups of query rows read the same bf16 rows: 25 rows of 7 query heads on each of 4, 16 requests of 4096 121 us past them, 99 through
+// them (causal 123 and 100), 64 of 4 on each of 8, 32 requests of 2048 358 and 327; one group (64 requests, 7 on each of 4) 140 and 159, eight-bit rows (37 requests) 65
+// and 70; eight-bit rows of several groups (the 25 rows of 7, causal) 117 and 112
 template <int D, bool QUANT, int NT>
 __device__ __forceinline__ void request_rows(const PagedAttn& p, const uint8_t* base, int64_t stride_p, int64_t stride_n, TilePlace x, char* stage, int lane) {
   if (!QUANT && NT > 1 && p.most_groups > 1)
@@ -856,8 +860,9 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
 }
 
 // Two workgroups a compute unit, as their rings allow, and no more than the batch may have tiles.  Up to 16 query rows of a K/V head are one operand (NT = 1),
-// more are taken 32 at a time, which halves the passes over the rows: 25 rows of 7 heads, 16 requests of 4096 127 us and not 209.  Bundles of four heads where
-// they divide: 64 requests 145.6 us, without bundles 150, eight-bit rows 94 and 101.
+// more are taken 32 at a time, which halves the passes over the rows: 25 rows of 7 query heads on each of 4, 16 requests of 4096 99 us and not 232, causal 100 and 234,
+// 64 of 4 on each of 8, 32 requests of 2048 327 and 611.  Bundles of four heads where they divide: 64 requests 140 us, without bundles 150, eight-bit rows 64 and
+// 70, the 25 rows of 7 99 and 148; but the 64 rows of 4 327 and 205, and 256 requests of 128 rows, 32 heads whose rows lie side by side 115 and 93.
 constexpr int kPagedGroups = 512;
 PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch& b, int page) {
   PagedPlan p;
