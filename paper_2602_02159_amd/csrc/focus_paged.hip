@@ -15,12 +15,12 @@
 // again as its own rounding.  Of few query rows a tile is 16 KB from memory and 24 products, and the matrix unit has nothing else to do; of many, where the
 // products count, it is a third of them.
 //
-// What bounds it is HBM, every row read once: one request of 32 832 rows, 32 heads, 538 MB, in 85 us = 6.4 TB/s and 4.7 for the join; 64 of up to
-// 16 384 rows with 7 query heads on each of 4, 869 MB, in 136 and 6; eight-bit rows, 227 MB for 37 requests with 16 rows a unit, in 60 and 6: some 8 us are the
+// What bounds it is HBM, every row read once: one request of 32 832 rows, 32 heads, 538 MB, in 84 us = 6.4 TB/s and 4.7 for the join; 64 of up to
+// 16 384 rows with 7 query heads on each of 4, 869 MB, in 136 and 6; eight-bit rows, 227 MB for 37 requests with 16 rows a unit, in 58 and 6: some 8 us are the
 // start, 8 the pieces of 16 rows each (16 KB a wavefront), and half as many bytes a tile leave the instructions half the time.  A thousand
-// rows of four heads: 6.2 + 4.1 us, dependent round trips (lengths, table, rows, products; pieces).  Many query rows of a K/V head are far from their bounds: each
+// rows of four heads: 5.9 + 3.9 us, dependent round trips (lengths, table, rows, products; pieces).  Many query rows of a K/V head are far from their bounds: each
 // 32 of them read all rows of the request again, those that causal limits hide from all 32 among them (64 rows of 4 query heads on each of 8, 32 requests of
-// 2048: 268 MB and 69 GFLOP, either 55 us, in 328, causal or not).
+// 2048: 268 MB and 69 GFLOP, either 55 us, in 312 to 334, causal or not).
 #include <algorithm>
 
 #include "focus_codes.h"
@@ -231,9 +231,9 @@ __device__ __forceinline__ void request_rows_as(const uint8_t* base, int64_t str
     __builtin_amdgcn_global_load_lds((gptr_t)src, (lptr_t)(stage + i * 1024), 16, 0, POLICY);
   }
 }
-// Past the caches, unless several groups of query rows read the same bf16 rows: 25 rows of 7 query heads on each of 4, 16 requests of 4096 121 us past them, 99 through
-// them (causal 123 and 100), 64 of 4 on each of 8, 32 requests of 2048 358 and 327; one group (64 requests, 7 on each of 4) 140 and 159, eight-bit rows (37 requests) 65
-// and 70; eight-bit rows of several groups (the 25 rows of 7, causal) 117 and 112
+// Past the caches, unless several groups of query rows read the same bf16 rows: 25 rows of 7 query heads on each of 4, 16 requests of 4096 120 us past them, 98 through
+// them (causal 122 and 100), 64 of 4 on each of 8, 32 requests of 2048 358 and 334; one group (64 requests, 7 on each of 4) 139 and 159, eight-bit rows (37 requests) 64
+// and 69; eight-bit rows of several groups (the 25 rows of 7, causal) 112 and 107
 template <int D, bool QUANT, int NT>
 __device__ __forceinline__ void request_rows(const PagedAttn& p, const uint8_t* base, int64_t stride_p, int64_t stride_n, TilePlace x, char* stage, int lane) {
   if (!QUANT && NT > 1 && p.most_groups > 1)
@@ -526,7 +526,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
 
   // Infinities and NaN in V.  Products with them are not what the definition says: lo may be zero or negative, and the probability of a key that a row does not
   // see, or of one far below the largest, is zero.  Any of them in a tile leaves no finite sum in its column, for all rows, until the piece ends; there one look
-  // finds it (0.3 us of 9.7 for a thousand rows, 1 of 139 for 64 requests; a look at every tile would be 64 instructions and more each).  The wavefront then works on
+  // finds it (0.1 us of 9.6 for a thousand rows, 0.3 of 138 for 64 requests; a look at every tile would be 64 instructions and more each).  The wavefront then works on
   // that piece once more, and on what else it has, tile by tile: with zeros in the place of such values, after it has found out for each sum whether one of
   // them leads up or down among the keys that its row sees, as products of ones for those keys with ones for those values.
   auto not_finite = [&](const auto& w) __attribute__((always_inline)) {
@@ -538,7 +538,7 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
 #pragma unroll
         for (int i = 0; i < 4; i += 2)  // (v_maximum3_f32: a NaN stays)
           x[i / 2] = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(w.o[n][ct][i]), fabsf(w.o[n][ct][i + 1])), x[i / 2]);
-    return __builtin_expect(__ballot(!(x[0] < INFINITY && x[1] < INFINITY)) != 0ull, 0);
+    return __ballot(!(x[0] < INFINITY && x[1] < INFINITY)) != 0ull;
   };
   auto same_lane = [&]() __attribute__((always_inline)) {  // what follows from the lane's number is worked out anew, and takes no registers of the loop before
     asm volatile("" : "+v"(lane));
@@ -655,55 +655,54 @@ __global__ __launch_bounds__(256, 2) void paged_attn_kernel(const PagedAttn p) {
   };
 
   // A stage's K is requested again as soon as it is in registers, its V likewise.  Loads return in order: a wait leaves those under way that were
-  // requested behind what is waited for.  Where no more are requested it leaves none.
-  int start = t, i = -kDepth;
+  // requested behind what is waited for.  Where no more are requested it leaves none.  (The first requests in turns of the loop that do nothing else are half the code,
+  // but with the second way out of it the compiler saw no loop there: 0.4 us of 9.6 for a thousand rows, 1 of 138 for 64 requests.)
+  int start = t, i = 0;
   QueryRows<D, NT> w;
 #pragma unroll 1
+  while (asked < min(n_tiles, kDepth)) {
+    request_k();
+    request_v();
+  }
+#pragma unroll 1
   for (; i < n_tiles; ++i) {
-    const bool more = asked < n_tiles, work = i >= 0;
+    const bool more = asked < n_tiles;
     char* stage = stage_of(i);
-    uint32_t mask = 0u;
+    const uint32_t mask = (uint32_t)__builtin_amdgcn_readlane(masks, i & (kDepth - 1));
     floatx4 acc[NT][2], ek[2], ev[2];
-    if (work) {
-      mask = (uint32_t)__builtin_amdgcn_readlane(masks, i & (kDepth - 1));
-      if (t == start) begin_unit(w, 0);
-      if (i + kDepth <= n_tiles)
-        wait_loads_but<G::kLoads + (kDepth - 1) * G::kTileLoads>();
-      else
-        wait_loads();
-      if (mask != 0u) {
-        multiply_k(acc, w, stage);
-        if constexpr (QUANT) read_exponents(ek, ev, stage + 2 * G::kRows, lane);
-      }
+    if (t == start) begin_unit(w, 0);
+    if (i + kDepth <= n_tiles)
+      wait_loads_but<G::kLoads + (kDepth - 1) * G::kTileLoads>();
+    else
+      wait_loads();
+    if (mask != 0u) {
+      multiply_k(acc, w, stage);
+      if constexpr (QUANT) read_exponents(ek, ev, stage + 2 * G::kRows, lane);
     }
     __builtin_amdgcn_sched_barrier(0);
     if (more) request_k();
     __builtin_amdgcn_sched_barrier(0);
-    if (work) {
-      bf16x8 hi[NT], lo[NT];
-      uint32_t seen[NT];
-      if (mask != 0u) softmax(acc, w, t, mask, ek, ev, hi, lo, seen);
-      if (more)
-        wait_loads_but<(kDepth - 1) * G::kTileLoads + G::kTileLoads - G::kLoads>();
-      else
-        wait_loads();
-      if (mask != 0u) {
-        bf16x8 v[kCT];
-        read_v(v, stage + G::kRows);
-        multiply_v(w, v, hi, lo);
-      }
+    bf16x8 hi[NT], lo[NT];
+    uint32_t seen[NT];
+    if (mask != 0u) softmax(acc, w, t, mask, ek, ev, hi, lo, seen);
+    if (more)
+      wait_loads_but<(kDepth - 1) * G::kTileLoads + G::kTileLoads - G::kLoads>();
+    else
+      wait_loads();
+    if (mask != 0u) {
+      bf16x8 v[kCT];
+      read_v(v, stage + G::kRows);
+      multiply_v(w, v, hi, lo);
     }
     __builtin_amdgcn_sched_barrier(0);
     if (more) request_v();
-    if (work) {
-      ++t;
-      if (t >= u.q.tiles || i == n_tiles - 1) {
-        if (not_finite(w)) break;
-        say_whose(start, i);
-        end_piece(w, 0, start, t);
-        start = t = 0;
-        if (i < n_tiles - 1) next_unit(u);
-      }
+    ++t;
+    if (t >= u.q.tiles || i == n_tiles - 1) {
+      if (__builtin_expect(not_finite(w), 0)) break;
+      say_whose(start, i);
+      end_piece(w, 0, start, t);
+      start = t = 0;
+      if (i < n_tiles - 1) next_unit(u);
     }
   }
   if (i == n_tiles) return;
@@ -799,9 +798,9 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
     bool some = false;
 #pragma unroll
     for (int v = 0; v < kVec; ++v) some |= stays(o[v]);
-    return __builtin_expect(__ballot(some) != 0ull, 0);
+    return __ballot(some) != 0ull;
   };
-  if (spoilt()) {
+  if (__builtin_expect(spoilt(), 0)) {
 #pragma unroll
     for (int v = 0; v < kVec; ++v) o[v] = 0.f;
 #pragma unroll 1
@@ -835,7 +834,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
 #pragma unroll
       for (int v = 0; v < kVec; ++v) o[v] += f * o_sh[w][lane * kVec + v];
     }
-    if (spoilt()) {
+    if (__builtin_expect(spoilt(), 0)) {
 #pragma unroll
       for (int v = 0; v < kVec; ++v) o[v] = 0.f;
 #pragma unroll 1
@@ -860,9 +859,9 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedAttn p) {
 }
 
 // Two workgroups a compute unit, as their rings allow, and no more than the batch may have tiles.  Up to 16 query rows of a K/V head are one operand (NT = 1),
-// more are taken 32 at a time, which halves the passes over the rows: 25 rows of 7 query heads on each of 4, 16 requests of 4096 99 us and not 232, causal 100 and 234,
-// 64 of 4 on each of 8, 32 requests of 2048 327 and 611.  Bundles of four heads where they divide: 64 requests 140 us, without bundles 150, eight-bit rows 64 and
-// 70, the 25 rows of 7 99 and 148; but the 64 rows of 4 327 and 205, and 256 requests of 128 rows, 32 heads whose rows lie side by side 115 and 93.
+// more are taken 32 at a time, which halves the passes over the rows: 25 rows of 7 query heads on each of 4, 16 requests of 4096 98 us and not 229, 64 of 4
+// on each of 8, 32 requests of 2048 334 and not 626.  Bundles of four heads where they divide: 64 requests 139 us, without bundles 149, eight-bit rows 64 and 70,
+// the 25 rows of 7 98 and 146; but the 64 rows of 4 334 and 200, and 256 requests of 128 rows, 32 heads side by side 93 to 118, by where the pages lie, and 92.
 constexpr int kPagedGroups = 512;
 PagedPlan plan_paged_attn(int n_heads, int group, int head_dim, const PagedBatch& b, int page) {
   PagedPlan p;
