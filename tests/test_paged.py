@@ -927,3 +927,45 @@ def test_positions_past_32_bits(first, fine):
         return
     fb.rotary(x, out, None, first, rotation(64))
     assert np.array_equal(bits(out), bf16_bits(turned32(x.float().cpu().numpy(), np.arange(2) + first, freqs(64), False)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("quant", [False, True])
+@pytest.mark.parametrize("group,rows", [(2, 3), (12, 3)])
+def test_rows_beside_a_query_that_is_not_finite(group, rows, quant):
+    """A NaN or an infinity in one query row: that row is NaN, those of the same request and of the others are as without it."""
+    lens = [100, 45]
+    pool = Pages(lens, 7, 16, 2, 64, quant, False).fill()
+    batch = batch_of(lens, pool.table, [rows] * 2)
+    q = torch.randn((2 * rows, 2 * group, 64), generator=torch.Generator().manual_seed(2)).bfloat16().to(DEV)
+    results = []
+    for bad in (None, math.nan, math.inf):
+        x = q.clone()
+        if bad is not None:
+            x[1, group - 1, 7] = bad
+        out, lse = torch.empty_like(x), torch.empty((2 * rows, 2 * group), device=DEV)
+        fb.paged_attn(x, pool.cache, batch, True, out, lse, workspace(pool.cache, batch, 2 * group))
+        results.append((out, lse))
+    there = torch.zeros((2 * rows, 2 * group), dtype=torch.bool, device=DEV)
+    there[1, group - 1] = True
+    for out, lse in results[1:]:
+        assert bool(out[there].isnan().all()) and torch.equal(out[~there], results[0][0][~there]) and torch.equal(lse[~there], results[0][1][~there])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group", [4, 12])
+def test_bf16_memory_that_was_never_written_does_not_reach_earlier_rows(group):
+    """NaN in K and V of all positions behind the rows, in their own tiles and in whole ones."""
+    lens, positions, rows = [100, 300], [60, 3, 0, 33, 36, 31, 20], [4, 3]
+    pool = Pages(lens, 19, 16, 2, 128, False, True, seed=group)
+    pool.lens = [61, 37]
+    pool.fill()
+    batch = batch_of(lens, pool.table, rows, positions)
+    q = torch.randn((7, 2 * group, 128), generator=torch.Generator().manual_seed(3)).bfloat16()
+    out, lse = torch.empty((7, 2 * group, 128), dtype=torch.bfloat16, device=DEV), torch.empty((7, 2 * group), device=DEV)
+    fb.paged_attn(q.to(DEV), pool.cache, batch, True, out, lse, workspace(pool.cache, batch, 2 * group))
+    for at, r, p in places(lens, rows, positions):
+        j, k, v = pool.rows(r, p + 1)
+        for h in range(2 * group):
+            check_attention(out[at:at + 1, h].cpu(), lse[at:at + 1, h].cpu(),
+                            attend64(q[at:at + 1, h].double(), k[:, h // group], v[:, h // group], torch.ones((1, p + 1), dtype=torch.bool)))
